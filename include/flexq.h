@@ -283,6 +283,80 @@ int fq_gemm(fq_ctx* ctx, int layer, const uint16_t* X_dev, int M, int ldx,
 int fq_gemm_two_pass(fq_ctx* ctx, int layer, const uint16_t* X_dev, int M, int ldx,
                      uint16_t* Y_dev, int ldy, void* stream);
 
+/* 8-bit layers ------------------------------------------------------------------------ */
+
+enum { FQ_DT_F16 = 0, FQ_DT_BF16 = 1, FQ_DT_F32 = 2 };     /* types of the buffers that cross as void* */
+
+/* The calls from here to fq_distill_topk_grad take their matrices with a row pitch (in elements), allocate nothing, use none of the
+ * context's workspaces and keep nothing from one call for the next: they may run on any stream of the context's device, several at
+ * a time, and be captured and replayed.  Only the status word (fq_status) is shared.  An output may not overlap an input or
+ * another output, except where that is said. */
+
+/* Symmetric 8-bit quantiser of matrix rows (tokens, or the output channels of a weight matrix):
+ *   a = max |x|,  scale = fp32(a / 127),  code = rint(127 x / a) of the exact quotient, ties to even; all in [-127, 127].
+ *   A row of zeros gets codes 0 and scale 0; a row that holds an infinity or a NaN codes 0 and scale NaN.
+ *   x_dev      dtype [rows][ldx >= cols], aligned to its type        (read)
+ *   codes_dev  int8  [rows][ldc >= cols]                              (written; columns behind `cols` are left as they are)
+ *   scales_dev float [rows]                                           (written)
+ * 1 <= rows, cols <= 2^20. */
+int fq_quantize_rows(fq_ctx* ctx, const void* x_dev, int dtype, int rows, int cols, long long ldx, int8_t* codes_dev, long long ldc,
+                     float* scales_dev, void* stream);
+
+/* Product of 8-bit codes with a scale for every token and every output channel:
+ *   Y[m][n] = (fp32(sum_k xc[m][k] * wc[n][k]) * x_scales[m]) * w_scales[n]
+ * The sum is exact (32-bit integers; k_in <= 131071); fp32 products, Y rounded once to y_dtype.
+ *   x_codes_dev int8 [M][ldx >= k_in], w_codes_dev int8 [n_out][ldw >= k_in]: 16-byte aligned, ldx and ldw multiples of 16.
+ *   Y_dev       y_dtype [M][ldy >= n_out]: 16-byte aligned, rows a multiple of 16 bytes apart.
+ * 1 <= M, n_out <= 2^20. */
+int fq_gemm_i8(fq_ctx* ctx, const int8_t* x_codes_dev, const float* x_scales_dev, int M, long long ldx, const int8_t* w_codes_dev,
+               const float* w_scales_dev, int n_out, int k_in, long long ldw, void* Y_dev, int y_dtype, long long ldy, void* stream);
+
+/* A linear layer with 8-bit weights: fq_quantize_rows of the tokens, then fq_gemm_i8, with the same results.
+ *   X_dev x_dtype [M][ldx >= k_in], aligned to its type;  Y_dev as in fq_gemm_i8.
+ *   codes_dev int8 [M][ldc >= k_in] (16-byte aligned, ldc a multiple of 16) and scales_dev float [M]: scratch of the caller's, whose contents are
+ *   undefined afterwards (a few tokens are quantised where they are used).  Calls that may overlap need scratch of their own. */
+int fq_linear_i8(fq_ctx* ctx, const void* X_dev, int x_dtype, int M, long long ldx, const int8_t* w_codes_dev, const float* w_scales_dev,
+                 int n_out, int k_in, long long ldw, int8_t* codes_dev, long long ldc, float* scales_dev, void* Y_dev, int y_dtype,
+                 long long ldy, void* stream);
+
+/* What a model answers (Sec. III-B: candidates are evaluated by perplexity) ------------- */
+
+#define FQ_MAX_TOP 128          /* alternatives per row */
+#define FQ_MAX_VOCAB 393216     /* entries of a row of logits */
+#define FQ_MAX_ROWS (1 << 20)
+
+/* Log probabilities of given tokens, entropies and most likely tokens.  With m = max z, d_i = (z_i - m) / T and S = sum exp(d_i)
+ * over a row z of logits:
+ *   logprob = d_token - log S,   entropy = log S - sum exp(d_i) d_i / S,
+ *   top_ids = the n_top tokens with the largest z (equal ones: the lower id first),   top_logprobs = their d - log S.
+ * A logit of -inf has probability 0 and is never among the top ones; where fewer are left, the remaining places get id -1 and -inf.
+ * A row of nothing but -inf: logprob -inf, entropy 0.  A row that holds a NaN or +inf: NaN, ids -1.
+ * token < 0: none asked, logprob 0.  token >= vocab: logprob NaN.
+ *   logits_dev dtype [rows][ld >= vocab], aligned to its type (rows may start anywhere);  tokens_dev int32 or int64 [rows] (id_bytes 4 or 8);
+ *   logprob_dev, entropy_dev float [rows];  top_ids_dev int32, top_logprobs_dev float [rows][n_top] (n_top <= FQ_MAX_TOP; may be NULL if it is 0).
+ * 0 < temperature < inf.  Sums in fp32: errors of a few 2^-24 of the largest |d| that counts. */
+int fq_token_logprobs(fq_ctx* ctx, const void* logits_dev, int dtype, int rows, int vocab, long long ld, const void* tokens_dev, int id_bytes,
+                      float temperature, float* logprob_dev, float* entropy_dev, int n_top, int* top_ids_dev, float* top_logprobs_dev,
+                      void* stream);
+
+/* Distillation from a teacher's top logits: with p = softmax(teacher / T) over a row's slots and q = softmax(z / T) over its whole vocabulary,
+ *   loss = sum_j p_j (log p_j - log q_[ids_j]),     d loss / d z_i = (q_i - sum_{j: ids_j = i} p_j) / T.
+ * A slot whose id is negative or whose teacher logit is -inf is empty; ids may repeat (their p add up).  A row without a slot: loss 0,
+ * gradient 0.  A slot on a logit of -inf: loss +inf.  An id >= vocab: loss NaN, gradient NaN.  A row that holds a NaN or +inf: NaN.
+ * A row of nothing but -inf has q = 0.
+ *   logits_dev, tokens as in fq_token_logprobs;  ids_dev int32 or int64, teacher_dev float [rows][n_top], 1 <= n_top <= FQ_MAX_TOP;
+ *   grad_loss_dev float [rows]: upstream gradient of every row's loss (a row whose is 0 gets a gradient of 0 whatever it holds);
+ *   loss_dev float [rows];  lse_dev float [rows][2], 8-byte aligned: (m, log S), so that m / T + log S is the log-sum-exp;
+ *   grad_dev dtype [rows][ldg >= vocab]: may be logits_dev itself, with the same pitch (the gradient then replaces the logits).
+ * fq_distill_topk writes loss and lse and, if grad_dev is not NULL, the gradient in the same pass over the logits;
+ * fq_distill_topk_grad writes the gradient alone, from the lse of an earlier call on the same logits, temperature and slots. */
+int fq_distill_topk(fq_ctx* ctx, const void* logits_dev, int dtype, int rows, int vocab, long long ld, const void* ids_dev, int id_bytes,
+                    const float* teacher_dev, int n_top, float temperature, const float* grad_loss_dev, float* loss_dev, float* lse_dev,
+                    void* grad_dev, long long ldg, void* stream);
+int fq_distill_topk_grad(fq_ctx* ctx, const void* logits_dev, int dtype, int rows, int vocab, long long ld, const void* ids_dev, int id_bytes,
+                         const float* teacher_dev, int n_top, float temperature, const float* grad_loss_dev, const float* lse_dev,
+                         void* grad_dev, long long ldg, void* stream);
+
 /* Test / reporting support ------------------------------------------------------------ */
 
 /* How fq_gemm runs M tokens through `layer`.  Host only. */

@@ -21,19 +21,6 @@ constexpr int kMaxPhases = 4096;
 // tag equals the tag of the running launch.
 constexpr size_t kPartialBase = kWsHead + 192;
 
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = false;
-    explicit DeviceGuard(int dev)
-    {
-        if (cudaGetDevice(&prev) != cudaSuccess) return;
-        ok = prev == dev || cudaSetDevice(dev) == cudaSuccess;
-    }
-    ~DeviceGuard() { if (ok && prev >= 0) cudaSetDevice(prev); }
-};
-
 FieldList active_fields(const Layer& L, int bits) { return L.fmt == FQ_FMT_PLANES ? plane_fields(bits) : packed_fields(bits); }
 
 const Variant* active_variant(const Layer& L, int bits)

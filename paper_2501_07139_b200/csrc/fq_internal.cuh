@@ -101,6 +101,20 @@ struct Ctx {
 // Device word that is not 0 once a zero point above 1023 has been stored by any call on the context (it is never cleared).
 inline unsigned* high_zeros_word(const Ctx* ctx) { return reinterpret_cast<unsigned*>(ctx->status_dev) + 1; }
 
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// Makes `dev` the current device for a scope.
+struct DeviceGuard {
+    int prev = -1;
+    bool ok = false;
+    explicit DeviceGuard(int dev)
+    {
+        if (cudaGetDevice(&prev) != cudaSuccess) return;
+        ok = prev == dev || cudaSetDevice(dev) == cudaSuccess;
+    }
+    ~DeviceGuard() { if (ok && prev >= 0) cudaSetDevice(prev); }
+};
+
 // Is the work that is enqueued on `st` recorded into a graph?
 bool is_capturing(cudaStream_t st);
 // Bytes of device workspace for `n_ops` ops whose split-K needs are summed by the caller.
@@ -193,6 +207,10 @@ struct CtaWork {
         return rp_last - rp_first + 1 - (lo - rp_first * n_chunks > 0 ? 1 : 0);
     }
 };
+
+// 8-bit layers
+int launch_quantize_rows(const void* x, int dtype, int rows, int cols, long long ldx, int8_t* codes, long long ldc, float* scales,
+                         cudaStream_t st);
 
 int launch_gemm(Ctx* ctx, const void* store, int blob_stride, const FieldList& fl, int zero_adjust, int n_out, int k_in,
                 const uint16_t* X, int M, int ldx, uint16_t* Y, int ldy, void* w_scratch, cudaStream_t st);
