@@ -21,10 +21,11 @@
 namespace fq {
 namespace {
 
-constexpr int kRowThreads = 512;
+constexpr int kRowThreads = 256;
 constexpr int kRowWarps = kRowThreads / 32;
 constexpr int kMaxTop = FQ_MAX_TOP;
 constexpr int kCandidates = 512;
+constexpr int kBins = 256;
 constexpr int kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNegInf = -INFINITY;
@@ -153,12 +154,6 @@ __device__ __forceinline__ void fetch_slice(const T* row, const Slice& s, uint4*
     }
 }
 
-__device__ __forceinline__ float warp_max(float v)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
-}
 __device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll
@@ -171,33 +166,22 @@ struct RowSums { float m, s, s1; };       // maximum, sum of exp(d), sum of exp(
 struct RowShared {
     unsigned long long bar;
     RowSums sums;                         // of this CTA's slice, read by the others
-    float red[2][kRowWarps];
+    float4 warp[kRowWarps];               // the warps' sums, and the least of their threads' keys
     int failed;
 };
 
-// Maximum of the slice; `mine` is that of this thread's entries.
-template <class T>
-__device__ __forceinline__ float slice_max(const uint4* buf, int groups, RowShared& sh, float& mine)
-{
-    float m = kNegInf;
-    for (int i = threadIdx.x; i < groups; i += kRowThreads) m = fmaxf(m, Group<T>::max_of(buf[i]));
-    mine = m;
-    m = warp_max(m);
-    if ((threadIdx.x & 31) == 0) sh.red[0][threadIdx.x >> 5] = m;
-    __syncthreads();
-    m = sh.red[0][0];
-#pragma unroll
-    for (int w = 1; w < kRowWarps; w++) m = fmaxf(m, sh.red[0][w]);
-    return m;
-}
-
-// Sums of the slice against its own maximum (0 if that is -inf); every thread gets them.
+// Sums of the entries of this thread, against their own maximum (0 if that is -inf).  Nobody waits for the slice's maximum: the
+// threads' sums are put on a common one when they are added up.
 template <class T, bool ENTROPY>
-__device__ __forceinline__ RowSums slice_sums(const uint4* buf, int groups, float m, float c2, RowShared& sh)
+__device__ __forceinline__ RowSums thread_sums(const uint4* buf, int groups, float c2)
 {
     constexpr int P = Group<T>::N / 2;
-    const float mm = m == kNegInf ? 0.0f : m;
+    typename Group<T>::Max best = Group<T>::lowest();
+#pragma unroll 4
+    for (int i = threadIdx.x; i < groups; i += kRowThreads) Group<T>::take_max(best, buf[i]);
+    const float m = Group<T>::of_max(best), mm = m == kNegInf ? 0.0f : m;
     float2 s = make_float2(0.0f, 0.0f), s1 = make_float2(0.0f, 0.0f);
+#pragma unroll 2
     for (int i = threadIdx.x; i < groups; i += kRowThreads) {
         float2 f[P];
         Group<T>::unpack(buf[i], f);
@@ -213,19 +197,40 @@ __device__ __forceinline__ RowSums slice_sums(const uint4* buf, int groups, floa
             if (ENTROPY) s1 = fma2(e, t, s1);
         }
     }
-    const float a = warp_sum(s.x + s.y), b = ENTROPY ? warp_sum(s1.x + s1.y) : 0.0f;
-    __syncthreads();                                             // slice_max's words have been read
-    if ((threadIdx.x & 31) == 0) {
-        sh.red[0][threadIdx.x >> 5] = a;
-        sh.red[1][threadIdx.x >> 5] = b;
-    }
+    return RowSums{m, s.x + s.y, ENTROPY ? s1.x + s1.y : 0.0f};
+}
+
+// `part`, which is against its own maximum, added to `r` against `r.m`, the larger one.
+__device__ __forceinline__ void add_part(RowSums& r, const RowSums& part, float c2)
+{
+    if (part.s == 0.0f) return;                                  // nothing but -inf (NaN goes on)
+    const float t = part.m == r.m ? 0.0f : (part.m - r.m) * c2, f = ex2(t);
+    r.s += f * part.s;
+    if (f > 0.0f) r.s1 += f * (part.s1 + part.s * t);
+}
+
+// Sums of the slice, in every thread; `least` is the smallest of the threads' keys (of those that have an entry).
+template <bool ENTROPY>
+__device__ __forceinline__ RowSums slice_sums(const RowSums& mine, uint32_t my_key, float c2, RowShared& sh, uint32_t& least)
+{
+    // (a thread without entries, or whose entries are all NaN, has m = -inf; its sum, 0 or NaN, counts as it is)
+    const uint32_t key = __reduce_max_sync(0xffffffffu, my_key);
+    RowSums w{key ? of_key(key) : kNegInf, 0.0f, 0.0f};
+    add_part(w, mine, c2);
+    w.s = warp_sum(w.s);
+    if (ENTROPY) w.s1 = warp_sum(w.s1);
+    const uint32_t low = __reduce_min_sync(0xffffffffu, my_key ? my_key : 0xffffffffu);
+    if ((threadIdx.x & 31) == 0) sh.warp[threadIdx.x >> 5] = make_float4(w.m, w.s, w.s1, __uint_as_float(low));
     __syncthreads();
-    RowSums r{m, 0.0f, 0.0f};
+    RowSums r{kNegInf, 0.0f, 0.0f};
+    least = 0xffffffffu;
 #pragma unroll
-    for (int w = 0; w < kRowWarps; w++) {
-        r.s += sh.red[0][w];
-        if (ENTROPY) r.s1 += sh.red[1][w];
+    for (int i = 0; i < kRowWarps; i++) {
+        r.m = fmaxf(r.m, sh.warp[i].x);
+        least = min(least, __float_as_uint(sh.warp[i].w));
     }
+#pragma unroll
+    for (int i = 0; i < kRowWarps; i++) add_part(r, RowSums{sh.warp[i].x, sh.warp[i].y, sh.warp[i].z}, c2);
     return r;
 }
 
@@ -243,11 +248,7 @@ __device__ __forceinline__ RowSums join(const RowShared& sh, int n_cta, float c2
         }
 #pragma unroll
     for (int i = 0; i < kMaxCluster; i++)
-        if (i < n_cta && part[i].s != 0.0f) {                    // (a slice of nothing but -inf has none)
-            const float t = part[i].m == r.m ? 0.0f : (part[i].m - r.m) * c2, f = ex2(t);
-            r.s += f * part[i].s;
-            if (f > 0.0f || part[i].s != part[i].s) r.s1 += f * (part[i].s1 + part[i].s * t);
-        }
+        if (i < n_cta) add_part(r, part[i], c2);
     return r;
 }
 
@@ -266,14 +267,16 @@ __device__ __forceinline__ void await_slice(RowShared& sh, const RowArgs& a)
 struct TopShared {
     unsigned long long cand[kCandidates];     // (key, ~index): larger is earlier
     unsigned long long top[kMaxTop];
-    int n, n_top;
-    int count[32 + 32];
+    int bins[kBins];                          // zeroed before
+    int n, n_top;                             // n: zeroed before
+    int count[64];
 };
 
 template <class T, class Fn>
 __device__ __forceinline__ void each_entry(const uint4* buf, const Slice& s, Fn&& fn)
 {
     constexpr int N = Group<T>::N;
+#pragma unroll 1
     for (int i = threadIdx.x; i < s.groups; i += kRowThreads) {
         float2 f[N / 2];
         Group<T>::unpack(buf[i], f);
@@ -292,72 +295,113 @@ __device__ __forceinline__ int block_count(int mine, int& word)
     return word;
 }
 __device__ __forceinline__ unsigned long long entry_word(uint32_t key, int index) { return (unsigned long long)key << 32 | (0xffffffffu - (uint32_t)index); }
+// Where a bin lies: those of a lane (eight in a row, from the top) in different banks from the other lanes'.
+__device__ __forceinline__ int bin_at(int bin) { return (bin & 7) * 32 + (bin >> 3); }
+__device__ __forceinline__ void add_candidate(TopShared& sh, uint32_t key, int index)
+{
+    const int at = atomicAdd(&sh.n, 1);
+    if (at < kCandidates) sh.cand[at] = entry_word(key, index);
+}
 
-// Leaves the k largest entries, in order, in sh.top and their number in sh.n_top.
-//   The threads' own maxima bound the k-th largest entry from below (k of them are entries): the k-th largest of them, cut to its
-//   upper 16 bits, is found by halving, with one vote of the CTA per bit.  What reaches it is collected, usually a few
-//   more than k, and ordered by counting.  Entries that are alike in great number (a row of equal logits) overflow the list: then
-//   the k-th largest key, and among its bearers the last index that belongs to the k, are found by halving over all entries.
+// Too many entries reach the bound (a row of equal logits): the k-th largest key and, among its bearers, the last index that belongs
+// to the k are found by halving, a pass over the slice each.  Leaves exactly k candidates.
 template <class T>
-__device__ void slice_top(const uint4* buf, const Slice& s, int k, float mine, TopShared& sh)
+__device__ __noinline__ void exact_candidates(const uint4* buf, const Slice& s, int k, TopShared& sh)
 {
     for (int i = threadIdx.x; i < 64; i += kRowThreads) sh.count[i] = 0;
-    if (threadIdx.x == 0) sh.n = 0;
-    const uint32_t my = mine > kNegInf ? key_of(mine) >> 16 : 0u;
-    uint32_t least = 0;
-    for (int b = 15; b >= 0; b--) {
-        const uint32_t q = least | 1u << b;
-        if (__syncthreads_count(my >= q) >= k) least = q;
+    __syncthreads();
+    uint32_t kth = 0;
+    for (int b = 31; b >= 0; b--) {
+        const uint32_t q = kth | 1u << b;
+        int c = 0;
+        each_entry<T>(buf, s, [&](float v, int) { c += key_of(v) >= q; });
+        if (block_count(c, sh.count[b]) >= k) kth = q;
     }
-    if (my >= least && my > 0)
-        each_entry<T>(buf, s, [&](float v, int index) {
-            const uint32_t key = key_of(v);
-            if (key >> 16 >= least) {
-                const int at = atomicAdd(&sh.n, 1);
-                if (at < kCandidates) sh.cand[at] = entry_word(key, index);
-            }
-        });
+    int c = 0;
+    each_entry<T>(buf, s, [&](float v, int) { c += key_of(v) > kth; });
+    const int above = block_count(c, sh.count[32]);                    // fewer than k
+    int last = 0;                                                      // the bearers below this index are too few, that at it completes the k
+    for (int b = 30; b >= 0; b--) {
+        if ((1 << b) > s.first + s.n) continue;
+        const int q = last | 1 << b;
+        c = 0;
+        each_entry<T>(buf, s, [&](float v, int index) { c += key_of(v) == kth && index < q; });
+        if (block_count(c, sh.count[33 + b]) < k - above) last = q;
+    }
+    if (threadIdx.x == 0) sh.n = 0;
+    __syncthreads();
+    each_entry<T>(buf, s, [&](float v, int index) {
+        const uint32_t key = key_of(v);
+        if (key > kth || (key == kth && index <= last)) add_candidate(sh, key, index);
+    });
+    __syncthreads();
+}
+
+// Calls place(rank, word) for the k largest entries, once each, and returns how many there are (fewer than k if the slice has no more).
+//   The threads' own maxima bound the k-th largest entry from below, k of them being entries.  A histogram of them over
+//   [least, most] gives a bound within 1/256 of that range; what reaches it, usually a few more entries than k, is collected by the
+//   warps whose threads' maxima do, and ordered by counting, eight lanes to a candidate.
+template <class T, class Fn>
+__device__ __forceinline__ int slice_top(const uint4* buf, const Slice& s, int k, uint32_t my_key, uint32_t least, uint32_t most, TopShared& sh, Fn&& place)
+{
+    constexpr int N = Group<T>::N;
+    const int lane = threadIdx.x & 31;
+    const int span = 32 - __clz((int)(most - least)), shift = span > 8 ? span - 8 : 0;
+    if (my_key) atomicAdd(&sh.bins[bin_at((int)((my_key - least) >> shift))], 1);
+    __syncthreads();
+    // bins from the top, eight to a lane
+    int sum = 0, in_bin[kBins / 32];
+#pragma unroll
+    for (int i = 0; i < kBins / 32; i++) {
+        in_bin[i] = sh.bins[bin_at(kBins - 1 - (lane * (kBins / 32) + i))];
+        sum += in_bin[i];
+    }
+    int upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+    }
+    const unsigned enough = __ballot_sync(0xffffffffu, upto >= k);
+    uint32_t bound = 1;                                                // fewer than k threads have an entry: all entries are candidates
+    if (enough) {
+        const int who = __ffs((int)enough) - 1;
+        int before = upto - sum, bin = 0;
+#pragma unroll
+        for (int i = 0; i < kBins / 32; i++) {
+            if (before < k) bin = kBins - 1 - (lane * (kBins / 32) + i);
+            before += in_bin[i];
+        }
+        bound = least + ((uint32_t)__shfl_sync(0xffffffffu, bin, who) << shift);
+    }
+    // a warp goes through the entries of each of its threads that has a candidate, all lanes together
+    const T* el = reinterpret_cast<const T*>(buf);
+    const int rounds = (s.groups + kRowThreads - 1) / kRowThreads;
+    for (unsigned have = __ballot_sync(0xffffffffu, my_key >= bound); have; have &= have - 1) {
+        const int first_group = (threadIdx.x & ~31) + __ffs((int)have) - 1;
+        for (int i = lane; i < rounds * N; i += 32) {
+            const int group = first_group + (i / N) * kRowThreads, e = group * N + i % N;
+            if (group >= s.groups) continue;
+            const float v = Group<T>::to_f(el[e]);
+            if (v > kNegInf && key_of(v) >= bound) add_candidate(sh, key_of(v), s.first + e - s.shift);
+        }
+    }
     __syncthreads();
     int n = sh.n;
     if (n > kCandidates) {
-        uint32_t kth = 0;
-        for (int b = 31; b >= 0; b--) {
-            const uint32_t q = kth | 1u << b;
-            int c = 0;
-            each_entry<T>(buf, s, [&](float v, int) { c += key_of(v) >= q; });
-            if (block_count(c, sh.count[b]) >= k) kth = q;
-        }
-        int c = 0;
-        each_entry<T>(buf, s, [&](float v, int) { c += key_of(v) > kth; });
-        const int above = block_count(c, sh.count[32]);                    // fewer than k
-        int before = 0;                                                    // the bearers of `kth` below this index are too few ...
-        for (int b = 30; b >= 0; b--) {
-            if ((1 << b) > s.first + s.n) continue;
-            const int q = before | 1 << b;
-            c = 0;
-            each_entry<T>(buf, s, [&](float v, int index) { c += key_of(v) == kth && index < q; });
-            if (block_count(c, sh.count[33 + b]) < k - above) before = q;  // ... so that the last that counts is at it
-        }
-        if (threadIdx.x == 0) sh.n = 0;
-        __syncthreads();
-        each_entry<T>(buf, s, [&](float v, int index) {
-            const uint32_t key = key_of(v);
-            if (key > kth || (key == kth && index <= before)) {
-                const int at = atomicAdd(&sh.n, 1);
-                if (at < kCandidates) sh.cand[at] = entry_word(key, index);
-            }
-        });
-        __syncthreads();
+        exact_candidates<T>(buf, s, k, sh);
         n = sh.n;
     }
-    for (int i = threadIdx.x; i < n; i += kRowThreads) {
-        const unsigned long long w = sh.cand[i];
+    for (int c0 = 0; c0 < n; c0 += kRowThreads / 8) {
+        const int c = c0 + (threadIdx.x >> 3);
+        const unsigned long long w = c < n ? sh.cand[c] : ~0ull;
         int rank = 0;
-        for (int j = 0; j < n; j++) rank += sh.cand[j] > w;
-        if (rank < k) sh.top[rank] = w;
+        for (int j = threadIdx.x & 7; j < n; j += 8) rank += sh.cand[j] > w;
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+        if ((threadIdx.x & 7) == 0 && c < n && rank < k) place(rank, w);
     }
-    if (threadIdx.x == 0) sh.n_top = n < k ? n : k;
-    __syncthreads();
+    return n < k ? n : k;
 }
 
 // ------------------------------------------------------------------------------- log probabilities
@@ -371,8 +415,33 @@ struct LogprobArgs {
     float* top_logprobs;
 };
 
+// What a row's sums make of its entries.
+struct RowAnswer {
+    float zm, log_s, t;
+    bool nan;
+    __device__ __forceinline__ RowAnswer(const RowSums& sum, float temperature)
+        : zm(sum.m == kNegInf ? 0.0f : sum.m), log_s(sum.s == 0.0f ? 0.0f : logf(sum.s)), t(temperature), nan(sum.s != sum.s) {}
+    __device__ __forceinline__ float logprob(float z) const { return (z - zm) / t - log_s; }
+    __device__ __forceinline__ void put(const LogprobArgs& o, long long r, int vocab, long long token, float z, const RowSums& sum) const
+    {
+        o.logprob[r] = token < 0 ? 0.0f : token >= vocab || nan ? NAN : logprob(z);
+        o.entropy[r] = sum.s == 0.0f ? 0.0f : log_s - kLn2 * (sum.s1 / sum.s);
+    }
+    __device__ __forceinline__ void put_top(const LogprobArgs& o, long long r, int place, unsigned long long w) const
+    {
+        if (nan) return put_none(o, r, place);
+        o.top_ids[r * o.n_top + place] = (int)(0xffffffffu - (uint32_t)w);
+        o.top_logprobs[r * o.n_top + place] = logprob(of_key((uint32_t)(w >> 32)));
+    }
+    __device__ __forceinline__ void put_none(const LogprobArgs& o, long long r, int place) const
+    {
+        o.top_ids[r * o.n_top + place] = -1;
+        o.top_logprobs[r * o.n_top + place] = nan ? NAN : kNegInf;
+    }
+};
+
 template <class T>
-__global__ void __launch_bounds__(kRowThreads, 2) token_logprobs_kernel(const RowArgs a, const LogprobArgs o)
+__global__ void __launch_bounds__(kRowThreads, 4) token_logprobs_kernel(const RowArgs a, const LogprobArgs o)
 {
     extern __shared__ __align__(16) uint4 buf[];
     __shared__ RowShared sh;
@@ -381,91 +450,84 @@ __global__ void __launch_bounds__(kRowThreads, 2) token_logprobs_kernel(const Ro
     const long long r = blockIdx.x / a.n_cta;
     const T* row = static_cast<const T*>(a.z) + r * a.ld;
     const Slice s = slice_of<T>(a, row, rank);
-    if (threadIdx.x == 0) sh.failed = 0;
+    for (int i = threadIdx.x; i < kBins; i += kRowThreads) top.bins[i] = 0;
+    if (threadIdx.x == kRowThreads - 1) {
+        sh.failed = 0;
+        top.n = 0;
+    }
     fetch_slice<T>(row, s, buf, smem_u32(&sh.bar));
+    __syncthreads();
+    // the last warp fetches the token's logit while the slice is on its way
+    const bool scalar = rank == 0 && threadIdx.x == kRowThreads - 32;
     long long token = -1;
     float z_token = 0.0f;
-    if (rank == 0 && threadIdx.x == 0) {
+    if (scalar) {
         token = load_id(o.tokens, o.wide, r);
         if (token >= 0 && token < a.vocab) z_token = Group<T>::to_f(row[token]);
     }
-    __syncthreads();
     await_slice(sh, a);
-    float mine;
-    const float m = slice_max<T>(buf, s.groups, sh, mine);
-    RowSums sum = slice_sums<T, true>(buf, s.groups, m, a.c2, sh);
-    if (o.n_top > 0) slice_top<T>(buf, s, o.n_top, mine, top);
-    int n_top = o.n_top > 0 ? top.n_top : 0;
-    const unsigned long long* best = top.top;
-    if (a.n_cta > 1) {
-        if (threadIdx.x == 0) sh.sums = sum;
-        __syncthreads();
-        cluster_arrive();
-        cluster_wait();
-        if (rank == 0) {
-            sum = join(sh, a.n_cta, a.c2);
-            // the CTAs' lists, merged: an entry's place is its own place in its list and what is larger in each of the others
-            if (o.n_top > 0) {
-                unsigned long long* lists = reinterpret_cast<unsigned long long*>(buf);
-                int* lens = top.count;
-                const uint32_t at = smem_u32(top.top), at_n = smem_u32(&top.n_top);
-                if (threadIdx.x < a.n_cta) {
-                    const uint32_t there = cluster_map(at_n, threadIdx.x);
-                    int n;
-                    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(n) : "r"(there) : "memory");
-                    lens[threadIdx.x] = n;
-                }
-                __syncthreads();
-                for (int i = threadIdx.x; i < a.n_cta * kMaxTop; i += kRowThreads) {
-                    const int c = i / kMaxTop, j = i % kMaxTop;
-                    if (j < lens[c]) lists[i] = cluster_ld_u64(cluster_map(at, (uint32_t)c) + (uint32_t)j * 8);
-                }
-                __syncthreads();
-                int total = 0;
-                for (int c = 0; c < a.n_cta; c++) total += lens[c];
-                n_top = total < o.n_top ? total : o.n_top;
-                for (int i = threadIdx.x; i < a.n_cta * kMaxTop; i += kRowThreads) {
-                    const int c = i / kMaxTop, j = i % kMaxTop;
-                    if (j >= lens[c]) continue;
-                    const unsigned long long w = lists[i];
-                    int place = j;
-                    for (int d = 0; d < a.n_cta; d++) {
-                        if (d == c) continue;
-                        int lo = 0, hi = lens[d];                           // entries of list d that are larger than w
-                        while (lo < hi) {
-                            const int mid = (lo + hi) >> 1;
-                            if (lists[d * kMaxTop + mid] > w) lo = mid + 1; else hi = mid;
-                        }
-                        place += lo;
-                    }
-                    if (place < o.n_top) top.cand[place] = w;
-                }
-                best = top.cand;
-                __syncthreads();
-            }
+    const RowSums mine = thread_sums<T, true>(buf, s.groups, a.c2);
+    const uint32_t my_key = mine.m > kNegInf ? key_of(mine.m) : 0u;
+    uint32_t least;
+    RowSums sum = slice_sums<true>(mine, my_key, a.c2, sh, least);
+    const uint32_t most = sum.m > kNegInf ? key_of(sum.m) : 0u;
+    if (least > most) least = most;                              // (no thread has an entry)
+    if (a.n_cta == 1) {
+        const RowAnswer ans(sum, a.t);
+        if (o.n_top > 0) {
+            const int n = slice_top<T>(buf, s, o.n_top, my_key, least, most, top, [&](int place, unsigned long long w) { ans.put_top(o, r, place, w); });
+            for (int j = n + threadIdx.x; j < o.n_top; j += kRowThreads) ans.put_none(o, r, j);
         }
-        cluster_arrive();                                                    // nobody's shared memory is read any more
-        cluster_wait();
+        if (scalar) ans.put(o, r, a.vocab, token, z_token, sum);
+        if (sh.failed) let_copies_land();
+        return;
     }
+    if (o.n_top > 0) {
+        const int n = slice_top<T>(buf, s, o.n_top, my_key, least, most, top, [&](int place, unsigned long long w) { top.top[place] = w; });
+        if (threadIdx.x == 0) top.n_top = n;
+    }
+    if (threadIdx.x == 0) sh.sums = sum;
+    cluster_arrive();
+    cluster_wait();
     if (rank == 0) {
-        const float zm = sum.m == kNegInf ? 0.0f : sum.m;
-        const float log_s = sum.s == 0.0f ? 0.0f : logf(sum.s);
-        const bool nan = sum.s != sum.s;
-        if (threadIdx.x == 0) {
-            float lp = 0.0f;
-            if (token >= a.vocab) lp = NAN;
-            else if (token >= 0) lp = nan ? NAN : (z_token - zm) / a.t - log_s;
-            o.logprob[r] = lp;
-            o.entropy[r] = sum.s == 0.0f ? 0.0f : log_s - kLn2 * (sum.s1 / sum.s);
-        }
-        if (threadIdx.x < o.n_top) {
-            const int j = threadIdx.x;
-            const bool there = j < n_top && !nan;
-            const unsigned long long w = there ? best[j] : 0ull;
-            o.top_ids[r * o.n_top + j] = there ? (int)(0xffffffffu - (uint32_t)w) : -1;
-            o.top_logprobs[r * o.n_top + j] = there ? (of_key((uint32_t)(w >> 32)) - zm) / a.t - log_s : (nan ? NAN : kNegInf);
+        sum = join(sh, a.n_cta, a.c2);
+        const RowAnswer ans(sum, a.t);
+        if (scalar) ans.put(o, r, a.vocab, token, z_token, sum);
+        // the CTAs' lists, merged: an entry's place is its own place in its list and what is larger in each of the others
+        if (o.n_top > 0) {
+            unsigned long long* lists = reinterpret_cast<unsigned long long*>(buf);
+            int* lens = top.count;
+            const uint32_t at = smem_u32(top.top), at_n = smem_u32(&top.n_top);
+            if (threadIdx.x < a.n_cta) lens[threadIdx.x] = cluster_ld_s32(cluster_map(at_n, threadIdx.x));
+            __syncthreads();
+            for (int i = threadIdx.x; i < a.n_cta * kMaxTop; i += kRowThreads) {
+                const int c = i / kMaxTop, j = i % kMaxTop;
+                if (j < lens[c]) lists[i] = cluster_ld_u64(cluster_map(at, (uint32_t)c) + (uint32_t)j * 8);
+            }
+            __syncthreads();
+            int total = 0;
+            for (int c = 0; c < a.n_cta; c++) total += lens[c];
+            for (int i = threadIdx.x; i < a.n_cta * kMaxTop; i += kRowThreads) {
+                const int c = i / kMaxTop, j = i % kMaxTop;
+                if (j >= lens[c]) continue;
+                const unsigned long long w = lists[i];
+                int place = j;
+                for (int d = 0; d < a.n_cta; d++) {
+                    if (d == c) continue;
+                    int lo = 0, hi = lens[d];                           // entries of list d that are larger than w
+                    while (lo < hi) {
+                        const int mid = (lo + hi) >> 1;
+                        if (lists[d * kMaxTop + mid] > w) lo = mid + 1; else hi = mid;
+                    }
+                    place += lo;
+                }
+                if (place < o.n_top) ans.put_top(o, r, place, w);
+            }
+            for (int j = total + threadIdx.x; j < o.n_top; j += kRowThreads) ans.put_none(o, r, j);
         }
     }
+    cluster_arrive();                                                    // nobody's shared memory is read any more
+    cluster_wait();
     if (sh.failed) let_copies_land();
 }
 
@@ -521,7 +583,7 @@ __device__ __forceinline__ void teacher_softmax(TeacherShared& sh, int k, float 
 
 // GIVEN: the gradient alone, from the (m, log S) that an earlier call kept; slices then need nothing from one another.
 template <class T, bool GIVEN>
-__global__ void __launch_bounds__(kRowThreads, 2) distill_kernel(const RowArgs a, const DistillArgs o)
+__global__ void __launch_bounds__(kRowThreads, 4) distill_kernel(const RowArgs a, const DistillArgs o)
 {
     extern __shared__ __align__(16) uint4 buf[];
     __shared__ RowShared sh;
@@ -560,12 +622,11 @@ __global__ void __launch_bounds__(kRowThreads, 2) distill_kernel(const RowArgs a
         log_s = st.y;
         __syncthreads();
     } else {
-        float mine;
-        const float m = slice_max<T>(buf, s.groups, sh, mine);
-        sum = slice_sums<T, false>(buf, s.groups, m, a.c2, sh);
+        const RowSums mine = thread_sums<T, false>(buf, s.groups, a.c2);
+        uint32_t least;
+        sum = slice_sums<false>(mine, mine.m > kNegInf ? key_of(mine.m) : 0u, a.c2, sh, least);
         if (a.n_cta > 1) {
             if (threadIdx.x == 0) sh.sums = sum;
-            __syncthreads();
             cluster_arrive();
             cluster_wait();
             sum = join(sh, a.n_cta, a.c2);

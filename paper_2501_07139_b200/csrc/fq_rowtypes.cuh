@@ -22,10 +22,14 @@ template <> struct Group<float> {
     {
         return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
     }
-    static __device__ __forceinline__ float max_of(const uint4& v)
+    // running maximum (NaN is not seen)
+    using Max = float;
+    static __device__ __forceinline__ Max lowest() { return -INFINITY; }
+    static __device__ __forceinline__ void take_max(Max& m, const uint4& v)
     {
-        return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+        m = fmaxf(fmaxf(m, fmaxf(__uint_as_float(v.x), __uint_as_float(v.y))), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
     }
+    static __device__ __forceinline__ float of_max(Max m) { return m; }
     static __device__ __forceinline__ float to_f(float v) { return v; }
     static __device__ __forceinline__ float from_f(float v) { return v; }
 };
@@ -47,12 +51,14 @@ template <> struct Group<__nv_bfloat16> {
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
-    static __device__ __forceinline__ float max_of(const uint4& v)
+    using Max = __nv_bfloat162;
+    static __device__ __forceinline__ Max lowest() { return __float2bfloat162_rn(-INFINITY); }
+    static __device__ __forceinline__ void take_max(Max& m, const uint4& v)
     {
         const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
-        const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
-        return fmaxf(__low2float(m), __high2float(m));
+        m = __hmax2(m, __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
     }
+    static __device__ __forceinline__ float of_max(Max m) { return fmaxf(__low2float(m), __high2float(m)); }
     static __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
     static __device__ __forceinline__ __nv_bfloat16 from_f(float v) { return __float2bfloat16_rn(v); }
 };
@@ -74,12 +80,14 @@ template <> struct Group<__half> {
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
-    static __device__ __forceinline__ float max_of(const uint4& v)
+    using Max = __half2;
+    static __device__ __forceinline__ Max lowest() { return __float2half2_rn(-INFINITY); }
+    static __device__ __forceinline__ void take_max(Max& m, const uint4& v)
     {
         const __half2* h = reinterpret_cast<const __half2*>(&v);
-        const __half2 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
-        return fmaxf(__low2float(m), __high2float(m));
+        m = __hmax2(m, __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
     }
+    static __device__ __forceinline__ float of_max(Max m) { return fmaxf(__low2float(m), __high2float(m)); }
     static __device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
     static __device__ __forceinline__ __half from_f(float v) { return __float2half_rn(v); }
 };

@@ -2,9 +2,9 @@
 
 Tolerances, with u = 2^-24 (half a step of fp32) and d = (z - m) / T:
   exp(d)     the difference, the scaling and its constant: 3 u |d|; the exponential itself 2^-22 = 4 u
-  S          those of its terms, weighted: 4 u + 3 u E where E = sum exp(d)|d| / S <= log V; additions: a thread adds at most V / 1024 + 4 numbers in
-             a row (two sums in each of 512 threads), the others are added in 5 + 16 + 8 steps
-  log S      the relative error of S, and one rounding of the result:              e = u (4 + 3 E + V / 1024 + 33 + 1 + log V)
+  S          those of its terms, weighted: 4 u + 3 u E where E = sum exp(d)|d| / S <= log V; additions: a thread adds at most V / 512 + 4 numbers in
+             a row (two sums in each of 256 threads), the others are added in 5 + 8 + 8 steps, each after a factor of 4 u
+  log S      the relative error of S, and one rounding of the result:              e = u (4 + 3 E + V / 512 + 36 + 1 + log V)
   logprob    e + 3 u |d| + u |result|
   entropy    log S and sum exp(d) d / S, whose terms are off by another u each and whose sum is too:   e + E (2 e + 2 u) + u |result|
   p of K     the same with K for V;  loss = sum p (lp - lq): sum p (e_lp + e_lq) + (the relative error of p) |lp - lq|, K additions
@@ -81,7 +81,7 @@ def distribution(z, t):
 
 
 def log_error(e, v):
-    return 1.01 * U * (4 + 3 * e + v / 1024 + 34 + math.log(v))
+    return 1.01 * U * (4 + 3 * e + v / 512 + 37 + math.log(v))
 
 
 def below(got, ref, tol, what):
