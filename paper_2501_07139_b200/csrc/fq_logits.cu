@@ -25,7 +25,7 @@ constexpr int kRowThreads = 256;
 constexpr int kRowWarps = kRowThreads / 32;
 constexpr int kMaxTop = FQ_MAX_TOP;
 constexpr int kCandidates = 512;
-constexpr int kBins = 256;
+constexpr int kBinBits = 7, kBins = 1 << kBinBits;
 constexpr int kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNegInf = -INFINITY;
@@ -295,8 +295,8 @@ __device__ __forceinline__ int block_count(int mine, int& word)
     return word;
 }
 __device__ __forceinline__ unsigned long long entry_word(uint32_t key, int index) { return (unsigned long long)key << 32 | (0xffffffffu - (uint32_t)index); }
-// Where a bin lies: those of a lane (eight in a row, from the top) in different banks from the other lanes'.
-__device__ __forceinline__ int bin_at(int bin) { return (bin & 7) * 32 + (bin >> 3); }
+// Where a bin lies: those of a lane (some in a row, from the top) in different banks from the other lanes'.
+__device__ __forceinline__ int bin_at(int bin) { return bin % (kBins / 32) * 32 + bin / (kBins / 32); }
 __device__ __forceinline__ void add_candidate(TopShared& sh, uint32_t key, int index)
 {
     const int at = atomicAdd(&sh.n, 1);
@@ -339,21 +339,21 @@ __device__ __noinline__ void exact_candidates(const uint4* buf, const Slice& s, 
 
 // Calls place(rank, word) for the k largest entries, once each, and returns how many there are (fewer than k if the slice has no more).
 //   The threads' own maxima bound the k-th largest entry from below, k of them being entries.  A histogram of them over
-//   [least, most] gives a bound within 1/256 of that range; what reaches it, usually a few more entries than k, is collected by the
-//   warps whose threads' maxima do, and ordered by counting, eight lanes to a candidate.
+//   [least, most] gives a bound within 1/128 of that range; what reaches it, usually a few more entries than k, is collected by the
+//   warps whose threads' maxima do, and ordered by counting.
 template <class T, class Fn>
 __device__ __forceinline__ int slice_top(const uint4* buf, const Slice& s, int k, uint32_t my_key, uint32_t least, uint32_t most, TopShared& sh, Fn&& place)
 {
-    constexpr int N = Group<T>::N;
+    constexpr int N = Group<T>::N, B = kBins / 32;
     const int lane = threadIdx.x & 31;
-    const int span = 32 - __clz((int)(most - least)), shift = span > 8 ? span - 8 : 0;
+    const int span = 32 - __clz((int)(most - least)), shift = span > kBinBits ? span - kBinBits : 0;
     if (my_key) atomicAdd(&sh.bins[bin_at((int)((my_key - least) >> shift))], 1);
     __syncthreads();
-    // bins from the top, eight to a lane
-    int sum = 0, in_bin[kBins / 32];
+    // bins from the top, B to a lane
+    int sum = 0, in_bin[B];
 #pragma unroll
-    for (int i = 0; i < kBins / 32; i++) {
-        in_bin[i] = sh.bins[bin_at(kBins - 1 - (lane * (kBins / 32) + i))];
+    for (int i = 0; i < B; i++) {
+        in_bin[i] = sh.bins[bin_at(kBins - 1 - (lane * B + i))];
         sum += in_bin[i];
     }
     int upto = sum;
@@ -363,27 +363,42 @@ __device__ __forceinline__ int slice_top(const uint4* buf, const Slice& s, int k
         if (lane >= o) upto += v;
     }
     const unsigned enough = __ballot_sync(0xffffffffu, upto >= k);
-    uint32_t bound = 1;                                                // fewer than k threads have an entry: all entries are candidates
+    uint32_t bound = 0x00800000u;                                      // (the lowest finite value: fewer than k threads have an entry)
     if (enough) {
         const int who = __ffs((int)enough) - 1;
         int before = upto - sum, bin = 0;
 #pragma unroll
-        for (int i = 0; i < kBins / 32; i++) {
-            if (before < k) bin = kBins - 1 - (lane * (kBins / 32) + i);
+        for (int i = 0; i < B; i++) {
+            if (before < k) bin = kBins - 1 - (lane * B + i);
             before += in_bin[i];
         }
         bound = least + ((uint32_t)__shfl_sync(0xffffffffu, bin, who) << shift);
     }
-    // a warp goes through the entries of each of its threads that has a candidate, all lanes together
-    const T* el = reinterpret_cast<const T*>(buf);
-    const int rounds = (s.groups + kRowThreads - 1) / kRowThreads;
-    for (unsigned have = __ballot_sync(0xffffffffu, my_key >= bound); have; have &= have - 1) {
-        const int first_group = (threadIdx.x & ~31) + __ffs((int)have) - 1;
-        for (int i = lane; i < rounds * N; i += 32) {
-            const int group = first_group + (i / N) * kRowThreads, e = group * N + i % N;
-            if (group >= s.groups) continue;
-            const float v = Group<T>::to_f(el[e]);
-            if (v > kNegInf && key_of(v) >= bound) add_candidate(sh, key_of(v), s.first + e - s.shift);
+    const float reach = of_key(bound);                                 // (compared as numbers, not met by -inf or NaN)
+    // the groups of two of the warp's threads at a time, 16 lanes to a thread
+    const int rounds = (s.groups + kRowThreads - 1) / kRowThreads, base = threadIdx.x & ~31;
+    unsigned have = __ballot_sync(0xffffffffu, my_key >= bound);
+    while (have) {
+        const int t0 = __ffs((int)have) - 1;
+        have &= have - 1;
+        const int t1 = have ? __ffs((int)have) - 1 : -1;
+        have &= have - 1;                                              // (0 & ... stays 0)
+        const int owner = lane < 16 ? t0 : t1;
+        for (int r = lane & 15; r < rounds; r += 16) {
+            const int group = base + owner + r * kRowThreads;
+            if (owner < 0 || group >= s.groups) continue;
+            const uint4 v = buf[group];
+            typename Group<T>::Max m = Group<T>::lowest();
+            Group<T>::take_max(m, v);
+            if (Group<T>::of_max(m) >= reach) {
+                float2 f[N / 2];
+                Group<T>::unpack(v, f);
+#pragma unroll
+                for (int e = 0; e < N; e++) {
+                    const float z = e & 1 ? f[e / 2].y : f[e / 2].x;
+                    if (z >= reach) add_candidate(sh, key_of(z), s.first + group * N + e - s.shift);
+                }
+            }
         }
     }
     __syncthreads();
@@ -392,14 +407,12 @@ __device__ __forceinline__ int slice_top(const uint4* buf, const Slice& s, int k
         exact_candidates<T>(buf, s, k, sh);
         n = sh.n;
     }
-    for (int c0 = 0; c0 < n; c0 += kRowThreads / 8) {
-        const int c = c0 + (threadIdx.x >> 3);
-        const unsigned long long w = c < n ? sh.cand[c] : ~0ull;
+    for (int c = threadIdx.x; c < n; c += kRowThreads) {
+        const unsigned long long w = sh.cand[c];
         int rank = 0;
-        for (int j = threadIdx.x & 7; j < n; j += 8) rank += sh.cand[j] > w;
-#pragma unroll
-        for (int o = 1; o < 8; o <<= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
-        if ((threadIdx.x & 7) == 0 && c < n && rank < k) place(rank, w);
+#pragma unroll 8
+        for (int j = 0; j < n; j++) rank += sh.cand[j] > w;
+        if (rank < k) place(rank, w);
     }
     return n < k ? n : k;
 }
