@@ -222,15 +222,22 @@ __device__ __forceinline__ RowSums slice_sums(const RowSums& mine, uint32_t my_k
     const uint32_t low = __reduce_min_sync(0xffffffffu, my_key ? my_key : 0xffffffffu);
     if ((threadIdx.x & 31) == 0) sh.warp[threadIdx.x >> 5] = make_float4(w.m, w.s, w.s1, __uint_as_float(low));
     __syncthreads();
-    RowSums r{kNegInf, 0.0f, 0.0f};
-    least = 0xffffffffu;
+    // every warp adds the warps' up, one to a lane
+    const int lane = threadIdx.x & (kRowWarps - 1);
+    const float4 v = sh.warp[lane];
+    RowSums r{v.x, 0.0f, 0.0f};
+    least = __float_as_uint(v.w);
 #pragma unroll
-    for (int i = 0; i < kRowWarps; i++) {
-        r.m = fmaxf(r.m, sh.warp[i].x);
-        least = min(least, __float_as_uint(sh.warp[i].w));
+    for (int o = 1; o < kRowWarps; o <<= 1) {
+        r.m = fmaxf(r.m, __shfl_xor_sync(0xffffffffu, r.m, o));
+        least = min(least, __shfl_xor_sync(0xffffffffu, least, o));
     }
+    add_part(r, RowSums{v.x, v.y, v.z}, c2);
 #pragma unroll
-    for (int i = 0; i < kRowWarps; i++) add_part(r, RowSums{sh.warp[i].x, sh.warp[i].y, sh.warp[i].z}, c2);
+    for (int o = 1; o < kRowWarps; o <<= 1) {
+        r.s += __shfl_xor_sync(0xffffffffu, r.s, o);
+        if (ENTROPY) r.s1 += __shfl_xor_sync(0xffffffffu, r.s1, o);
+    }
     return r;
 }
 
@@ -267,8 +274,13 @@ __device__ __forceinline__ void await_slice(RowShared& sh, const RowArgs& a)
 struct TopShared {
     unsigned long long cand[kCandidates];     // (key, ~index): larger is earlier
     unsigned long long top[kMaxTop];
+    uint32_t key[kRowThreads];                // the threads' maxima
     int bins[kBins];                          // zeroed before
-    int n, n_top;                             // n: zeroed before
+    int n_groups, n_cand;                     // zeroed before
+    int n_threads, n_top;
+    float reach;
+    unsigned short group[kCandidates];
+    unsigned char thread[kRowThreads];
     int count[64];
 };
 
@@ -297,14 +309,8 @@ __device__ __forceinline__ int block_count(int mine, int& word)
 __device__ __forceinline__ unsigned long long entry_word(uint32_t key, int index) { return (unsigned long long)key << 32 | (0xffffffffu - (uint32_t)index); }
 // Where a bin lies: those of a lane (some in a row, from the top) in different banks from the other lanes'.
 __device__ __forceinline__ int bin_at(int bin) { return bin % (kBins / 32) * 32 + bin / (kBins / 32); }
-__device__ __forceinline__ void add_candidate(TopShared& sh, uint32_t key, int index)
-{
-    const int at = atomicAdd(&sh.n, 1);
-    if (at < kCandidates) sh.cand[at] = entry_word(key, index);
-}
-
 // Too many entries reach the bound (a row of equal logits): the k-th largest key and, among its bearers, the last index that belongs
-// to the k are found by halving, a pass over the slice each.  Leaves exactly k candidates.
+// to the k are found by halving, a pass over the slice each.  Leaves exactly k candidates, in one list.
 template <class T>
 __device__ __noinline__ void exact_candidates(const uint4* buf, const Slice& s, int k, TopShared& sh)
 {
@@ -328,84 +334,102 @@ __device__ __noinline__ void exact_candidates(const uint4* buf, const Slice& s, 
         each_entry<T>(buf, s, [&](float v, int index) { c += key_of(v) == kth && index < q; });
         if (block_count(c, sh.count[33 + b]) < k - above) last = q;
     }
-    if (threadIdx.x == 0) sh.n = 0;
+    if (threadIdx.x == 0) sh.n_cand = 0;
     __syncthreads();
     each_entry<T>(buf, s, [&](float v, int index) {
         const uint32_t key = key_of(v);
-        if (key > kth || (key == kth && index <= last)) add_candidate(sh, key, index);
+        if (key > kth || (key == kth && index <= last)) {
+            const int at = atomicAdd(&sh.n_cand, 1);
+            if (at < kCandidates) sh.cand[at] = entry_word(key, index);
+        }
     });
     __syncthreads();
 }
 
 // Calls place(rank, word) for the k largest entries, once each, and returns how many there are (fewer than k if the slice has no more).
 //   The threads' own maxima bound the k-th largest entry from below, k of them being entries.  A histogram of them over
-//   [least, most] gives a bound within 1/128 of that range; what reaches it, usually a few more entries than k, is collected by the
-//   warps whose threads' maxima do, and ordered by counting.
+//   [least, most] gives a bound within 1/128 of that range; what reaches it, usually a few more entries than k, is found in three steps
+//   that each deal the little there is to do to all threads: the threads whose maximum does, the groups of theirs that hold an
+//   entry that does, the entries.  Then they are ordered by counting.  (4094 x 32000 bf16, k = 32: a warp that goes through its own threads' groups
+//   spends 6500 instructions of the CTA's warps on all this, where the sums take 8700.)
 template <class T, class Fn>
 __device__ __forceinline__ int slice_top(const uint4* buf, const Slice& s, int k, uint32_t my_key, uint32_t least, uint32_t most, TopShared& sh, Fn&& place)
 {
     constexpr int N = Group<T>::N, B = kBins / 32;
     const int lane = threadIdx.x & 31;
+    sh.key[threadIdx.x] = my_key;
     const int span = 32 - __clz((int)(most - least)), shift = span > kBinBits ? span - kBinBits : 0;
     if (my_key) atomicAdd(&sh.bins[bin_at((int)((my_key - least) >> shift))], 1);
     __syncthreads();
-    // bins from the top, B to a lane
-    int sum = 0, in_bin[B];
-#pragma unroll
-    for (int i = 0; i < B; i++) {
-        in_bin[i] = sh.bins[bin_at(kBins - 1 - (lane * B + i))];
-        sum += in_bin[i];
-    }
-    int upto = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += v;
-    }
-    const unsigned enough = __ballot_sync(0xffffffffu, upto >= k);
-    uint32_t bound = 0x00800000u;                                      // (the lowest finite value: fewer than k threads have an entry)
-    if (enough) {
-        const int who = __ffs((int)enough) - 1;
-        int before = upto - sum, bin = 0;
+    if (threadIdx.x < 32) {
+        // bins from the top, B to a lane
+        int sum = 0, in_bin[B];
 #pragma unroll
         for (int i = 0; i < B; i++) {
-            if (before < k) bin = kBins - 1 - (lane * B + i);
-            before += in_bin[i];
+            in_bin[i] = sh.bins[bin_at(kBins - 1 - (lane * B + i))];
+            sum += in_bin[i];
         }
-        bound = least + ((uint32_t)__shfl_sync(0xffffffffu, bin, who) << shift);
-    }
-    const float reach = of_key(bound);                                 // (compared as numbers, not met by -inf or NaN)
-    // the groups of two of the warp's threads at a time, 16 lanes to a thread
-    const int rounds = (s.groups + kRowThreads - 1) / kRowThreads, base = threadIdx.x & ~31;
-    unsigned have = __ballot_sync(0xffffffffu, my_key >= bound);
-    while (have) {
-        const int t0 = __ffs((int)have) - 1;
-        have &= have - 1;
-        const int t1 = have ? __ffs((int)have) - 1 : -1;
-        have &= have - 1;                                              // (0 & ... stays 0)
-        const int owner = lane < 16 ? t0 : t1;
-        for (int r = lane & 15; r < rounds; r += 16) {
-            const int group = base + owner + r * kRowThreads;
-            if (owner < 0 || group >= s.groups) continue;
-            const uint4 v = buf[group];
-            typename Group<T>::Max m = Group<T>::lowest();
-            Group<T>::take_max(m, v);
-            if (Group<T>::of_max(m) >= reach) {
-                float2 f[N / 2];
-                Group<T>::unpack(v, f);
+        int upto = sum;
 #pragma unroll
-                for (int e = 0; e < N; e++) {
-                    const float z = e & 1 ? f[e / 2].y : f[e / 2].x;
-                    if (z >= reach) add_candidate(sh, key_of(z), s.first + group * N + e - s.shift);
-                }
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const unsigned enough = __ballot_sync(0xffffffffu, upto >= k);
+        uint32_t bound = 0x00800000u;                                  // (the lowest finite value: fewer than k threads have an entry)
+        if (enough) {
+            const int who = __ffs((int)enough) - 1;
+            int before = upto - sum, bin = 0;
+#pragma unroll
+            for (int i = 0; i < B; i++) {
+                if (before < k) bin = kBins - 1 - (lane * B + i);
+                before += in_bin[i];
             }
+            bound = least + ((uint32_t)__shfl_sync(0xffffffffu, bin, who) << shift);
+        }
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kRowWarps; i++) {
+            const bool yes = sh.key[i * 32 + lane] >= bound;
+            const unsigned all = __ballot_sync(0xffffffffu, yes);
+            if (yes) sh.thread[n + __popc(all & ((1u << lane) - 1))] = (unsigned char)(i * 32 + lane);
+            n += __popc(all);
+        }
+        if (lane == 0) {
+            sh.n_threads = n;
+            sh.reach = of_key(bound);
         }
     }
     __syncthreads();
-    int n = sh.n;
-    if (n > kCandidates) {
+    const float reach = sh.reach;                                      // (compared as a number, not met by -inf or NaN)
+    const int rounds = (s.groups + kRowThreads - 1) / kRowThreads, bits = 32 - __clz(rounds - 1);
+    for (int i = threadIdx.x; i < sh.n_threads << bits; i += kRowThreads) {
+        const int group = sh.thread[i >> bits] + (i & ((1 << bits) - 1)) * kRowThreads;
+        if (group >= s.groups) continue;
+        typename Group<T>::Max m = Group<T>::lowest();
+        Group<T>::take_max(m, buf[group]);
+        if (Group<T>::of_max(m) >= reach) {
+            const int at = atomicAdd(&sh.n_groups, 1);
+            if (at < kCandidates) sh.group[at] = (unsigned short)group;
+        }
+    }
+    __syncthreads();
+    const int n_groups = sh.n_groups;
+    const T* el = reinterpret_cast<const T*>(buf);
+    if (n_groups <= kCandidates)
+        for (int i = threadIdx.x; i < n_groups * N; i += kRowThreads) {
+            const int e = sh.group[i / N] * N + i % N;
+            const float v = Group<T>::to_f(el[e]);
+            if (v >= reach) {
+                const int at = atomicAdd(&sh.n_cand, 1);
+                if (at < kCandidates) sh.cand[at] = entry_word(key_of(v), s.first + e - s.shift);
+            }
+        }
+    __syncthreads();
+    int n = sh.n_cand;
+    if (n > kCandidates || n_groups > kCandidates) {
         exact_candidates<T>(buf, s, k, sh);
-        n = sh.n;
+        n = sh.n_cand;
     }
     for (int c = threadIdx.x; c < n; c += kRowThreads) {
         const unsigned long long w = sh.cand[c];
@@ -466,7 +490,8 @@ __global__ void __launch_bounds__(kRowThreads, 4) token_logprobs_kernel(const Ro
     for (int i = threadIdx.x; i < kBins; i += kRowThreads) top.bins[i] = 0;
     if (threadIdx.x == kRowThreads - 1) {
         sh.failed = 0;
-        top.n = 0;
+        top.n_groups = 0;
+        top.n_cand = 0;
     }
     fetch_slice<T>(row, s, buf, smem_u32(&sh.bar));
     __syncthreads();
