@@ -270,79 +270,271 @@ __device__ __forceinline__ void await_slice(RowShared& sh, const RowArgs& a)
     }
 }
 
+// ------------------------------------------------------------------------------- a slice that only passes through
+// Where the entries are needed once, or a few of them again, they go from global memory into registers: without a slice in shared
+// memory more CTAs fit on an SM, and those that search their rows' largest entries are hidden behind those that read.
+
+template <class T>
+struct Stream {
+    const T* src;                // element 0: the 16-byte group in which the slice begins
+    Slice s;
+    int lo, hi;                  // whole groups [lo, hi); of the others there are at most two, one at either end
+    __device__ __forceinline__ Stream(const T* row, const Slice& slice) : src(row + slice.first - slice.shift), s(slice)
+    {
+        whole_groups<T>(slice, lo, hi);
+        lo /= Group<T>::N;
+        hi /= Group<T>::N;
+    }
+    __device__ __forceinline__ uint4 whole(int group) const
+    {
+        uint4 v;
+        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(src + (long long)group * Group<T>::N) : "memory");
+        return v;
+    }
+    // Group `group` if it is one of those at the ends, -inf for what is not the slice's.
+    __device__ __noinline__ uint4 end(int group) const
+    {
+        constexpr int N = Group<T>::N;
+        uint4 v;
+        T* el = reinterpret_cast<T*>(&v);
+        for (int i = 0; i < N; i++) {
+            const int e = group * N + i;
+            el[i] = e >= s.shift && e < s.shift + s.n ? src[e] : Group<T>::from_f(kNegInf);
+        }
+        return v;
+    }
+    __device__ __forceinline__ bool is_whole(int group) const { return group >= lo && group < hi; }
+    __device__ __forceinline__ uint4 any(int group) const { return is_whole(group) ? whole(group) : end(group); }
+};
+
+// Running sums of a thread.
+template <class T, bool ENTROPY>
+struct Running {
+    float m = kNegInf;
+    float2 s = {0.0f, 0.0f}, s1 = {0.0f, 0.0f};
+
+    template <int G>
+    __device__ __forceinline__ void take(const uint4 (&v)[G], float c2)
+    {
+        typename Group<T>::Max best = Group<T>::lowest();
+#pragma unroll
+        for (int g = 0; g < G; g++) Group<T>::take_max(best, v[g]);
+        const float higher = fmaxf(m, Group<T>::of_max(best));
+        if (higher > m) {                                        // the sums so far are put on the new maximum
+            const float t = (m - higher) * c2, f = ex2(t);       // (m = -inf: factor 0; the sums are 0 or NaN)
+            if (ENTROPY) {
+                if (f > 0.0f) s1 = fma2(s, make_float2(t, t), s1);
+                s1 = mul2(s1, make_float2(f, f));
+            }
+            s = mul2(s, make_float2(f, f));
+            m = higher;
+        }
+        const float mm = m == kNegInf ? 0.0f : m;
+        // exp(d) d of a masked entry would be 0 * -inf.  Entries of two to a register are kept above a floor whose exponential is 0
+        // all the same, at half the cost of doing so with the scaled differences.
+        const float floor2 = (Group<T>::kFloor - mm) * c2;
+        if (ENTROPY && Group<T>::N == 8 && floor2 < -160.0f && floor2 > -1e37f) {
+#pragma unroll
+            for (int g = 0; g < G; g++) add<false>(Group<T>::above_floor(v[g]), mm, c2);
+        } else {
+#pragma unroll
+            for (int g = 0; g < G; g++) add<ENTROPY>(v[g], mm, c2);
+        }
+    }
+    template <bool CLAMP>
+    __device__ __forceinline__ void add(const uint4& v, float mm, float c2)
+    {
+        float2 f[Group<T>::N / 2];
+        Group<T>::unpack(v, f);
+#pragma unroll
+        for (int p = 0; p < Group<T>::N / 2; p++) {
+            float2 t = scaled2(f[p], mm, c2);
+            if (CLAMP) {                                         // (exp(-160 ln 2) is 0 in 32 bits)
+                t.x = max_nan(t.x, -160.0f);
+                t.y = max_nan(t.y, -160.0f);
+            }
+            const float2 e = make_float2(ex2(t.x), ex2(t.y));
+            s = add2(s, e);
+            if (ENTROPY) s1 = fma2(e, t, s1);
+        }
+    }
+    __device__ __forceinline__ RowSums sums() const { return RowSums{m, s.x + s.y, ENTROPY ? s1.x + s1.y : 0.0f}; }
+};
+
+// Sums of this thread's groups lo + thread, + 256 ...; those at the ends are the first threads' of two warps.
+template <class T, bool ENTROPY>
+__device__ __forceinline__ RowSums stream_sums(const Stream<T>& x, float c2)
+{
+    constexpr int U = 4;
+    Running<T, ENTROPY> run;
+    int i = x.lo + threadIdx.x;
+    if (i + (U - 1) * kRowThreads < x.hi) {
+        uint4 v[U];
+#pragma unroll
+        for (int g = 0; g < U; g++) v[g] = x.whole(i + g * kRowThreads);
+        for (;;) {
+            i += U * kRowThreads;
+            const bool more = i + (U - 1) * kRowThreads < x.hi;
+            uint4 w[U];
+            if (more)
+#pragma unroll
+                for (int g = 0; g < U; g++) w[g] = x.whole(i + g * kRowThreads);
+            run.take(v, c2);
+            if (!more) break;
+#pragma unroll
+            for (int g = 0; g < U; g++) v[g] = w[g];
+        }
+    }
+    uint4 v[U];
+#pragma unroll
+    for (int g = 0; g < U; g++) {
+        v[g] = Group<T>::fill();
+        if (i + g * kRowThreads < x.hi) v[g] = x.whole(i + g * kRowThreads);
+    }
+    if (i + 2 * kRowThreads < x.hi) {
+        run.take(v, c2);
+    } else if (i < x.hi) {
+        const uint4 half[2] = {v[0], v[1]};
+        run.take(half, c2);
+    }
+    const int end = threadIdx.x == 0 && x.s.groups > 0 && !x.is_whole(0) ? 0 : threadIdx.x == 32 && x.hi > 0 && x.hi < x.s.groups ? x.hi : -1;
+    if (end >= 0) {
+        const uint4 one[1] = {x.end(end)};
+        run.take(one, c2);
+    }
+    return run.sums();
+}
+
 // ------------------------------------------------------------------------------- the largest entries of a slice
-struct TopShared {
+struct __align__(16) TopShared {
+    uint4 data[kCandidates];                  // groups that hold a candidate
     unsigned long long cand[kCandidates];     // (key, ~index): larger is earlier
     unsigned long long top[kMaxTop];
     uint32_t key[kRowThreads];                // the threads' maxima
-    int bins[kBins];                          // zeroed before
+    int bins[256];                            // zeroed before
     int n_groups, n_cand;                     // zeroed before
     int n_threads, n_top;
     float reach;
-    unsigned short group[kCandidates];
+    int group[kCandidates];
     unsigned char thread[kRowThreads];
-    int count[64];
+    int warp[kRowWarps];
+    int list_len[kMaxCluster];
 };
 
-template <class T, class Fn>
-__device__ __forceinline__ void each_entry(const uint4* buf, const Slice& s, Fn&& fn)
-{
-    constexpr int N = Group<T>::N;
-#pragma unroll 1
-    for (int i = threadIdx.x; i < s.groups; i += kRowThreads) {
-        float2 f[N / 2];
-        Group<T>::unpack(buf[i], f);
-#pragma unroll
-        for (int e = 0; e < N; e++) {
-            const float v = e & 1 ? f[e / 2].y : f[e / 2].x;
-            if (v > kNegInf) fn(v, s.first + i * N + e - s.shift);        // not -inf, not NaN
-        }
-    }
-}
-__device__ __forceinline__ int block_count(int mine, int& word)
-{
-    const int c = __reduce_add_sync(0xffffffffu, mine);
-    if ((threadIdx.x & 31) == 0 && c) atomicAdd(&word, c);
-    __syncthreads();
-    return word;
-}
 __device__ __forceinline__ unsigned long long entry_word(uint32_t key, int index) { return (unsigned long long)key << 32 | (0xffffffffu - (uint32_t)index); }
 // Where a bin lies: those of a lane (some in a row, from the top) in different banks from the other lanes'.
 __device__ __forceinline__ int bin_at(int bin) { return bin % (kBins / 32) * 32 + bin / (kBins / 32); }
-// Too many entries reach the bound (a row of equal logits): the k-th largest key and, among its bearers, the last index that belongs
-// to the k are found by halving, a pass over the slice each.  Leaves exactly k candidates, in one list.
-template <class T>
-__device__ __noinline__ void exact_candidates(const uint4* buf, const Slice& s, int k, TopShared& sh)
+
+// Of bins 0 .. 32 B - 1 (at(bin) says where they lie) the highest one so that it and those above it hold k, or -1; `above` gets what
+// those above it hold.  A whole warp.
+template <int B, class At>
+__device__ __forceinline__ int bin_of_kth(const int* bins, int k, At&& at, int& above)
 {
-    for (int i = threadIdx.x; i < 64; i += kRowThreads) sh.count[i] = 0;
-    __syncthreads();
+    const int lane = threadIdx.x & 31;
+    int sum = 0, in_bin[B];                                            // from the top, B to a lane
+#pragma unroll
+    for (int i = 0; i < B; i++) {
+        in_bin[i] = bins[at(32 * B - 1 - (lane * B + i))];
+        sum += in_bin[i];
+    }
+    int upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+    }
+    const unsigned enough = __ballot_sync(0xffffffffu, upto >= k);
+    if (!enough) return -1;
+    int before = upto - sum, bin = 0, over = 0;
+#pragma unroll
+    for (int i = 0; i < B; i++) {
+        if (before < k) { bin = 32 * B - 1 - (lane * B + i); over = before; }
+        before += in_bin[i];
+    }
+    const int who = __ffs((int)enough) - 1;
+    above = __shfl_sync(0xffffffffu, over, who);
+    return __shfl_sync(0xffffffffu, bin, who);
+}
+
+// Too many entries reach the bound (a row of equal logits): the k-th largest key is found digit by digit, a pass over the slice each,
+// then its first bearers in order of their indices.  Leaves exactly k candidates.  Needs as many finite entries as k.
+template <class T>
+__device__ __noinline__ void exact_candidates(const Stream<T>& x, int k, TopShared& sh)
+{
+    constexpr int N = Group<T>::N;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t kth = 0;
-    for (int b = 31; b >= 0; b--) {
-        const uint32_t q = kth | 1u << b;
-        int c = 0;
-        each_entry<T>(buf, s, [&](float v, int) { c += key_of(v) >= q; });
-        if (block_count(c, sh.count[b]) >= k) kth = q;
+    int need = k;                                                      // of the entries whose upper digits are those of kth
+    for (int d = 24; d >= 0; d -= 8) {
+        __syncthreads();
+        sh.bins[threadIdx.x] = 0;
+        __syncthreads();
+        int digit = 0, run = 0;                                        // alike entries in a row are counted before they are added
+        for (int i = threadIdx.x; i < x.s.groups; i += kRowThreads) {
+            const uint4 v = x.any(i);
+            for (int e = 0; e < N; e++) {
+                const float z = Group<T>::to_f(reinterpret_cast<const T*>(&v)[e]);
+                const uint32_t key = key_of(z);
+                if (!(z > kNegInf) || (d < 24 && (key ^ kth) >> (d + 8))) continue;
+                const int now = (int)(key >> d & 255u);
+                if (now != digit && run) { atomicAdd(&sh.bins[digit], run); run = 0; }
+                digit = now;
+                run++;
+            }
+        }
+        if (run) atomicAdd(&sh.bins[digit], run);
+        __syncthreads();
+        int above = 0;
+        const int bin = bin_of_kth<8>(sh.bins, need, [](int b) { return b; }, above);      // (every warp)
+        kth |= (uint32_t)(bin < 0 ? 0 : bin) << d;
+        need -= above;
     }
-    int c = 0;
-    each_entry<T>(buf, s, [&](float v, int) { c += key_of(v) > kth; });
-    const int above = block_count(c, sh.count[32]);                    // fewer than k
-    int last = 0;                                                      // the bearers below this index are too few, that at it completes the k
-    for (int b = 30; b >= 0; b--) {
-        if ((1 << b) > s.first + s.n) continue;
-        const int q = last | 1 << b;
-        c = 0;
-        each_entry<T>(buf, s, [&](float v, int index) { c += key_of(v) == kth && index < q; });
-        if (block_count(c, sh.count[33 + b]) < k - above) last = q;
-    }
+    __syncthreads();
     if (threadIdx.x == 0) sh.n_cand = 0;
     __syncthreads();
-    each_entry<T>(buf, s, [&](float v, int index) {
-        const uint32_t key = key_of(v);
-        if (key > kth || (key == kth && index <= last)) {
-            const int at = atomicAdd(&sh.n_cand, 1);
-            if (at < kCandidates) sh.cand[at] = entry_word(key, index);
+    // those above it, fewer than k, in any order; its bearers, in order, until there are enough
+    int taken = 0;
+    for (int i0 = 0; i0 < x.s.groups; i0 += kRowThreads) {
+        const int i = i0 + threadIdx.x;
+        unsigned bearers = 0;
+        uint4 v = Group<T>::fill();
+        if (i < x.s.groups) {
+            v = x.any(i);
+            for (int e = 0; e < N; e++) {
+                const float z = Group<T>::to_f(reinterpret_cast<const T*>(&v)[e]);
+                if (!(z > kNegInf)) continue;
+                const uint32_t key = key_of(z);
+                if (key == kth) bearers |= 1u << e;
+                if (key > kth) {
+                    const int at = atomicAdd(&sh.n_cand, 1);
+                    if (at < kCandidates) sh.cand[at] = entry_word(key, x.s.first + i * N + e - x.s.shift);
+                }
+            }
         }
-    });
+        if (taken >= need) continue;                                   // (the same for all threads)
+        int upto = __popc(bearers);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int n = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += n;
+        }
+        if (lane == 31) sh.warp[warp] = upto;
+        __syncthreads();
+        int before = taken, all = 0;
+        for (int w = 0; w < kRowWarps; w++) {
+            if (w < warp) before += sh.warp[w];
+            all += sh.warp[w];
+        }
+        before += upto - __popc(bearers);
+        for (; bearers; bearers &= bearers - 1, before++)
+            if (before < need) {
+                const int at = atomicAdd(&sh.n_cand, 1);
+                if (at < kCandidates) sh.cand[at] = entry_word(kth, x.s.first + i * N + __ffs((int)bearers) - 1 - x.s.shift);
+            }
+        taken += all;
+        __syncthreads();
+    }
     __syncthreads();
 }
 
@@ -350,43 +542,23 @@ __device__ __noinline__ void exact_candidates(const uint4* buf, const Slice& s, 
 //   The threads' own maxima bound the k-th largest entry from below, k of them being entries.  A histogram of them over
 //   [least, most] gives a bound within 1/128 of that range; what reaches it, usually a few more entries than k, is found in three steps
 //   that each deal the little there is to do to all threads: the threads whose maximum does, the groups of theirs that hold an
-//   entry that does, the entries.  Then they are ordered by counting.  (4094 x 32000 bf16, k = 32: a warp that goes through its own threads' groups
-//   spends 6500 instructions of the CTA's warps on all this, where the sums take 8700.)
+//   entry that does (read once more, from the L2 as a rule), the entries.  Then they are ordered by counting.  (4094 x 32000 bf16,
+//   k = 32: a warp that goes through its own threads' groups spends 6500 instructions of the CTA's warps on all this, where the sums
+//   take 8700; like this it is 2600.)
 template <class T, class Fn>
-__device__ __forceinline__ int slice_top(const uint4* buf, const Slice& s, int k, uint32_t my_key, uint32_t least, uint32_t most, TopShared& sh, Fn&& place)
+__device__ __forceinline__ int slice_top(const Stream<T>& x, int k, uint32_t my_key, uint32_t least, uint32_t most, TopShared& sh, Fn&& place)
 {
-    constexpr int N = Group<T>::N, B = kBins / 32;
+    constexpr int N = Group<T>::N;
     const int lane = threadIdx.x & 31;
     sh.key[threadIdx.x] = my_key;
     const int span = 32 - __clz((int)(most - least)), shift = span > kBinBits ? span - kBinBits : 0;
     if (my_key) atomicAdd(&sh.bins[bin_at((int)((my_key - least) >> shift))], 1);
     __syncthreads();
     if (threadIdx.x < 32) {
-        // bins from the top, B to a lane
-        int sum = 0, in_bin[B];
-#pragma unroll
-        for (int i = 0; i < B; i++) {
-            in_bin[i] = sh.bins[bin_at(kBins - 1 - (lane * B + i))];
-            sum += in_bin[i];
-        }
-        int upto = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += v;
-        }
-        const unsigned enough = __ballot_sync(0xffffffffu, upto >= k);
-        uint32_t bound = 0x00800000u;                                  // (the lowest finite value: fewer than k threads have an entry)
-        if (enough) {
-            const int who = __ffs((int)enough) - 1;
-            int before = upto - sum, bin = 0;
-#pragma unroll
-            for (int i = 0; i < B; i++) {
-                if (before < k) bin = kBins - 1 - (lane * B + i);
-                before += in_bin[i];
-            }
-            bound = least + ((uint32_t)__shfl_sync(0xffffffffu, bin, who) << shift);
-        }
+        int above;
+        const int bin = bin_of_kth<kBins / 32>(sh.bins, k, [](int b) { return bin_at(b); }, above);
+        // (fewer than k threads have an entry: the lowest finite value)
+        const uint32_t bound = bin < 0 ? 0x00800000u : least + ((uint32_t)bin << shift);
         int n = 0;
 #pragma unroll
         for (int i = 0; i < kRowWarps; i++) {
@@ -402,33 +574,35 @@ __device__ __forceinline__ int slice_top(const uint4* buf, const Slice& s, int k
     }
     __syncthreads();
     const float reach = sh.reach;                                      // (compared as a number, not met by -inf or NaN)
-    const int rounds = (s.groups + kRowThreads - 1) / kRowThreads, bits = 32 - __clz(rounds - 1);
-    for (int i = threadIdx.x; i < sh.n_threads << bits; i += kRowThreads) {
-        const int group = sh.thread[i >> bits] + (i & ((1 << bits) - 1)) * kRowThreads;
-        if (group >= s.groups) continue;
+    const int rounds = (x.hi - x.lo + kRowThreads - 1) / kRowThreads, bits = rounds > 1 ? 32 - __clz(rounds - 1) : 0;
+    const int items = sh.n_threads << bits;
+    for (int i = threadIdx.x; i < items + 2; i += kRowThreads) {
+        // the groups of those threads, and the two at the ends
+        const int group = i < items ? x.lo + sh.thread[i >> bits] + (i & ((1 << bits) - 1)) * kRowThreads : i == items ? 0 : x.s.groups - 1;
+        if (i < items ? group >= x.hi : x.s.groups == 0 || x.is_whole(group) || (i > items && group == 0)) continue;
+        const uint4 v = i < items ? x.whole(group) : x.end(group);
         typename Group<T>::Max m = Group<T>::lowest();
-        Group<T>::take_max(m, buf[group]);
+        Group<T>::take_max(m, v);
         if (Group<T>::of_max(m) >= reach) {
             const int at = atomicAdd(&sh.n_groups, 1);
-            if (at < kCandidates) sh.group[at] = (unsigned short)group;
+            if (at < kCandidates) { sh.group[at] = group; sh.data[at] = v; }
         }
     }
     __syncthreads();
     const int n_groups = sh.n_groups;
-    const T* el = reinterpret_cast<const T*>(buf);
+    const T* el = reinterpret_cast<const T*>(sh.data);
     if (n_groups <= kCandidates)
         for (int i = threadIdx.x; i < n_groups * N; i += kRowThreads) {
-            const int e = sh.group[i / N] * N + i % N;
-            const float v = Group<T>::to_f(el[e]);
+            const float v = Group<T>::to_f(el[i]);
             if (v >= reach) {
                 const int at = atomicAdd(&sh.n_cand, 1);
-                if (at < kCandidates) sh.cand[at] = entry_word(key_of(v), s.first + e - s.shift);
+                if (at < kCandidates) sh.cand[at] = entry_word(key_of(v), x.s.first + sh.group[i / N] * N + i % N - x.s.shift);
             }
         }
     __syncthreads();
     int n = sh.n_cand;
     if (n > kCandidates || n_groups > kCandidates) {
-        exact_candidates<T>(buf, s, k, sh);
+        exact_candidates<T>(x, k, sh);
         n = sh.n_cand;
     }
     for (int c = threadIdx.x; c < n; c += kRowThreads) {
@@ -480,31 +654,19 @@ struct RowAnswer {
 template <class T>
 __global__ void __launch_bounds__(kRowThreads, 4) token_logprobs_kernel(const RowArgs a, const LogprobArgs o)
 {
-    extern __shared__ __align__(16) uint4 buf[];
     __shared__ RowShared sh;
     __shared__ TopShared top;
     const int rank = a.n_cta > 1 ? (int)cluster_cta() : 0;
     const long long r = blockIdx.x / a.n_cta;
     const T* row = static_cast<const T*>(a.z) + r * a.ld;
-    const Slice s = slice_of<T>(a, row, rank);
-    for (int i = threadIdx.x; i < kBins; i += kRowThreads) top.bins[i] = 0;
-    if (threadIdx.x == kRowThreads - 1) {
-        sh.failed = 0;
-        top.n_groups = 0;
-        top.n_cand = 0;
-    }
-    fetch_slice<T>(row, s, buf, smem_u32(&sh.bar));
-    __syncthreads();
-    // the last warp fetches the token's logit while the slice is on its way
+    const Stream<T> x(row, slice_of<T>(a, row, rank));
+    // the last warp asks for the token, and for its logit at the end
     const bool scalar = rank == 0 && threadIdx.x == kRowThreads - 32;
-    long long token = -1;
-    float z_token = 0.0f;
-    if (scalar) {
-        token = load_id(o.tokens, o.wide, r);
-        if (token >= 0 && token < a.vocab) z_token = Group<T>::to_f(row[token]);
-    }
-    await_slice(sh, a);
-    const RowSums mine = thread_sums<T, true>(buf, s.groups, a.c2);
+    const long long token = scalar ? load_id(o.tokens, o.wide, r) : -1;
+    for (int i = threadIdx.x; i < kBins; i += kRowThreads) top.bins[i] = 0;
+    if (threadIdx.x == kRowThreads - 1) top.n_groups = top.n_cand = 0;
+    const RowSums mine = stream_sums<T, true>(x, a.c2);
+    const float z_token = token >= 0 && token < a.vocab ? Group<T>::to_f(row[token]) : 0.0f;
     const uint32_t my_key = mine.m > kNegInf ? key_of(mine.m) : 0u;
     uint32_t least;
     RowSums sum = slice_sums<true>(mine, my_key, a.c2, sh, least);
@@ -512,16 +674,15 @@ __global__ void __launch_bounds__(kRowThreads, 4) token_logprobs_kernel(const Ro
     if (least > most) least = most;                              // (no thread has an entry)
     if (a.n_cta == 1) {
         const RowAnswer ans(sum, a.t);
+        if (scalar) ans.put(o, r, a.vocab, token, z_token, sum);
         if (o.n_top > 0) {
-            const int n = slice_top<T>(buf, s, o.n_top, my_key, least, most, top, [&](int place, unsigned long long w) { ans.put_top(o, r, place, w); });
+            const int n = slice_top<T>(x, o.n_top, my_key, least, most, top, [&](int place, unsigned long long w) { ans.put_top(o, r, place, w); });
             for (int j = n + threadIdx.x; j < o.n_top; j += kRowThreads) ans.put_none(o, r, j);
         }
-        if (scalar) ans.put(o, r, a.vocab, token, z_token, sum);
-        if (sh.failed) let_copies_land();
         return;
     }
     if (o.n_top > 0) {
-        const int n = slice_top<T>(buf, s, o.n_top, my_key, least, most, top, [&](int place, unsigned long long w) { top.top[place] = w; });
+        const int n = slice_top<T>(x, o.n_top, my_key, least, most, top, [&](int place, unsigned long long w) { top.top[place] = w; });
         if (threadIdx.x == 0) top.n_top = n;
     }
     if (threadIdx.x == 0) sh.sums = sum;
@@ -533,8 +694,9 @@ __global__ void __launch_bounds__(kRowThreads, 4) token_logprobs_kernel(const Ro
         if (scalar) ans.put(o, r, a.vocab, token, z_token, sum);
         // the CTAs' lists, merged: an entry's place is its own place in its list and what is larger in each of the others
         if (o.n_top > 0) {
-            unsigned long long* lists = reinterpret_cast<unsigned long long*>(buf);
-            int* lens = top.count;
+            unsigned long long* lists = reinterpret_cast<unsigned long long*>(top.data);
+            static_assert(sizeof top.data >= sizeof(unsigned long long) * kMaxCluster * kMaxTop, "room for the lists");
+            int* lens = top.list_len;
             const uint32_t at = smem_u32(top.top), at_n = smem_u32(&top.n_top);
             if (threadIdx.x < a.n_cta) lens[threadIdx.x] = cluster_ld_s32(cluster_map(at_n, threadIdx.x));
             __syncthreads();
@@ -566,7 +728,6 @@ __global__ void __launch_bounds__(kRowThreads, 4) token_logprobs_kernel(const Ro
     }
     cluster_arrive();                                                    // nobody's shared memory is read any more
     cluster_wait();
-    if (sh.failed) let_copies_land();
 }
 
 // ------------------------------------------------------------------------------- distillation
@@ -617,6 +778,67 @@ __device__ __forceinline__ void teacher_softmax(TeacherShared& sh, int k, float 
             sh.lp[lane + 32 * i] = (u[i] - mm) / t - log_s;
         }
     if (lane == 0) sh.any = s != 0.0f;                                       // (NaN: true)
+}
+
+// sum p (log p - log q), in every lane of warp 0.  All threads; slot j is thread j's.
+__device__ __forceinline__ float distill_loss(TeacherShared& te, int k, const RowSums& sum, float log_s, float z_id, float t)
+{
+    const float zm = sum.m == kNegInf ? 0.0f : sum.m;
+    float term = 0.0f;
+    if (threadIdx.x < k) {
+        const float p = te.p[threadIdx.x];
+        // p times a distance that 32 bits do not hold may well be one that they do
+        if (!(p == 0.0f)) term = p * (te.lp[threadIdx.x] + log_s) - p * (z_id - zm) / t;
+    }
+    if (threadIdx.x < kMaxTop) {
+        term = warp_sum(term);
+        if ((threadIdx.x & 31) == 0) te.part[threadIdx.x >> 5] = term;
+    }
+    __syncthreads();
+    float loss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kMaxTop / 32; i++) loss += te.part[i];
+    return loss;
+}
+
+// The value alone: the logits pass through once.
+template <class T>
+__global__ void __launch_bounds__(kRowThreads, 4) distill_loss_kernel(const RowArgs a, const DistillArgs o)
+{
+    __shared__ RowShared sh;
+    __shared__ TeacherShared te;
+    const int rank = a.n_cta > 1 ? (int)cluster_cta() : 0;
+    const long long r = blockIdx.x / a.n_cta;
+    const T* row = static_cast<const T*>(a.z) + r * a.ld;
+    long long id = -1;
+    float z_id = kNegInf;
+    if (rank == 0 && threadIdx.x < o.k) {
+        id = load_id(o.ids, o.wide, r * o.k + threadIdx.x);
+        const float u = o.teacher[r * o.k + threadIdx.x];
+        if (id >= 0 && id < a.vocab) z_id = Group<T>::to_f(row[id]);
+        te.lp[threadIdx.x] = id >= 0 ? u : kNegInf;
+    }
+    const RowSums mine = stream_sums<T, false>(Stream<T>(row, slice_of<T>(a, row, rank)), a.c2);
+    const bool bad = __syncthreads_or(id >= a.vocab);
+    if (rank == 0 && threadIdx.x < 32) teacher_softmax(te, o.k, a.c2, a.t);
+    uint32_t least;
+    RowSums sum = slice_sums<false>(mine, mine.m > kNegInf ? key_of(mine.m) : 0u, a.c2, sh, least);
+    if (a.n_cta > 1) {
+        if (threadIdx.x == 0) sh.sums = sum;
+        cluster_arrive();
+        cluster_wait();
+        if (rank == 0) sum = join(sh, a.n_cta, a.c2);
+        cluster_arrive();                                        // nobody's sums are read any more
+    }
+    if (rank == 0) {
+        const float log_s = sum.s == 0.0f ? 0.0f : logf(sum.s);
+        const float loss = distill_loss(te, o.k, sum, log_s, z_id, a.t);
+        if (threadIdx.x == 0) {
+            o.loss[r] = bad ? NAN : loss;
+            o.stats[r] = make_float2(sum.m, sum.s != sum.s ? NAN : log_s);
+        }
+    }
+    if (a.n_cta > 1) cluster_wait();
 }
 
 // GIVEN: the gradient alone, from the (m, log S) that an earlier call kept; slices then need nothing from one another.
@@ -673,78 +895,64 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_kernel(const RowArgs a
     }
     const float zm = sum.m == kNegInf ? 0.0f : sum.m;
     if (!GIVEN && rank == 0) {
-        float term = 0.0f;
-        if (threadIdx.x < o.k) {
-            const float p = te.p[threadIdx.x];
-            // p (log p - log q); p times a distance that 32 bits do not hold may well be one that they do
-            if (!(p == 0.0f)) term = p * (te.lp[threadIdx.x] + log_s) - p * (z_id - zm) / a.t;
-        }
-        if (threadIdx.x < kMaxTop) {
-            term = warp_sum(term);
-            if ((threadIdx.x & 31) == 0) te.part[threadIdx.x >> 5] = term;
-        }
-        __syncthreads();
+        const float loss = distill_loss(te, o.k, sum, log_s, z_id, a.t);
         if (threadIdx.x == 0) {
-            float loss = 0.0f;
-            for (int i = 0; i < kMaxTop / 32; i++) loss += te.part[i];
             o.loss[r] = te.bad ? NAN : loss;
             o.stats[r] = make_float2(sum.m, sum.s != sum.s ? NAN : log_s);
         }
     }
-    if (o.grad) {
-        // g (q_i - p_i) / T, formed where the logits are.  A row without a teacher, or whose upstream gradient is 0, gets zeros
-        // whatever it holds.
-        const float g = o.grad_loss[r];
-        const bool zero = g == 0.0f || (!te.any && !te.bad);
-        const float w = te.bad ? NAN : g / a.t;
-        const float off = log_s * kLog2e;                        // q = 2^(t - off)
-        T* out_row = static_cast<T*>(o.grad) + r * o.ldg;
-        T* el = reinterpret_cast<T*>(buf);
-        for (int i = threadIdx.x; i < s.groups; i += kRowThreads) {
-            float2 f[N / 2];
-            Group<T>::unpack(buf[i], f);
+    // g (q_i - p_i) / T, formed where the logits are.  A row without a teacher, or whose upstream gradient is 0, gets zeros
+    // whatever it holds.
+    const float g = o.grad_loss[r];
+    const bool zero = g == 0.0f || (!te.any && !te.bad);
+    const float w = te.bad ? NAN : g / a.t;
+    const float off = log_s * kLog2e;                        // q = 2^(t - off)
+    T* out_row = static_cast<T*>(o.grad) + r * o.ldg;
+    T* el = reinterpret_cast<T*>(buf);
+    for (int i = threadIdx.x; i < s.groups; i += kRowThreads) {
+        float2 f[N / 2];
+        Group<T>::unpack(buf[i], f);
 #pragma unroll
-            for (int p = 0; p < N / 2; p++) {
-                const float2 t = add2(scaled2(f[p], zm, a.c2), make_float2(-off, -off));
-                const float2 q = mul2(make_float2(ex2(t.x), ex2(t.y)), make_float2(w, w));
-                f[p] = zero ? make_float2(0.0f, 0.0f) : q;
-            }
-            buf[i] = Group<T>::pack(f);
+        for (int p = 0; p < N / 2; p++) {
+            const float2 t = add2(scaled2(f[p], zm, a.c2), make_float2(-off, -off));
+            const float2 q = mul2(make_float2(ex2(t.x), ex2(t.y)), make_float2(w, w));
+            f[p] = zero ? make_float2(0.0f, 0.0f) : q;
         }
-        __syncthreads();
-        if (threadIdx.x < o.k && !zero && id >= s.first && id < s.first + s.n) {
-            float p = 0.0f;
-            bool first = true;
-            for (int j = 0; j < o.k; j++)
-                if (te.id[j] == id) {
-                    if (j < (int)threadIdx.x) first = false;
-                    p += te.p[j];
-                }
-            const float t = (z_id - zm) * a.c2 - off;
-            if (first) el[s.shift + (int)(id - s.first)] = Group<T>::from_f((ex2(t) - p) * w);
-        }
-        const bool alike = ((reinterpret_cast<uintptr_t>(out_row) ^ reinterpret_cast<uintptr_t>(row)) & 15) == 0;
-        T* dst = out_row + s.first - s.shift;                    // element 0 of the buffer
-        int lo, hi;
-        whole_groups<T>(s, lo, hi);
-        if (alike) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncthreads();
-        const int end = s.shift + s.n;
-        if (alike) {
-            if (threadIdx.x == 0 && hi > lo) {
-                asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
-                             ::"l"(dst + lo), "r"(smem_u32(el + lo)), "r"((hi - lo) * (int)sizeof(T)) : "memory");
-                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        buf[i] = Group<T>::pack(f);
+    }
+    __syncthreads();
+    if (threadIdx.x < o.k && !zero && id >= s.first && id < s.first + s.n) {
+        float p = 0.0f;
+        bool first = true;
+        for (int j = 0; j < o.k; j++)
+            if (te.id[j] == id) {
+                if (j < (int)threadIdx.x) first = false;
+                p += te.p[j];
             }
-            const int t = threadIdx.x - 32;
-            if (t >= 0 && t < 2 * N) {
-                const int e = t < N ? s.shift + t : hi + (t - N);
-                if (t < N ? e < lo && e < end : e < end) dst[e] = el[e];
-            }
-        } else {
-            for (int e = s.shift + threadIdx.x; e < end; e += kRowThreads) dst[e] = el[e];
+        const float t = (z_id - zm) * a.c2 - off;
+        if (first) el[s.shift + (int)(id - s.first)] = Group<T>::from_f((ex2(t) - p) * w);
+    }
+    const bool alike = ((reinterpret_cast<uintptr_t>(out_row) ^ reinterpret_cast<uintptr_t>(row)) & 15) == 0;
+    T* dst = out_row + s.first - s.shift;                    // element 0 of the buffer
+    int lo, hi;
+    whole_groups<T>(s, lo, hi);
+    if (alike) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    const int end = s.shift + s.n;
+    if (alike) {
+        if (threadIdx.x == 0 && hi > lo) {
+            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
+                         ::"l"(dst + lo), "r"(smem_u32(el + lo)), "r"((hi - lo) * (int)sizeof(T)) : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
         }
+        const int t = threadIdx.x - 32;
+        if (t >= 0 && t < 2 * N) {
+            const int e = t < N ? s.shift + t : hi + (t - N);
+            if (t < N ? e < lo && e < end : e < end) dst[e] = el[e];
+        }
+    } else {
+        for (int e = s.shift + threadIdx.x; e < end; e += kRowThreads) dst[e] = el[e];
     }
     if (!GIVEN && a.n_cta > 1) {                                 // nobody's sums are read any more
         cluster_arrive();
@@ -770,6 +978,19 @@ Cut cut_rows(int rows, int vocab, int size, int sm_count)
     c.smem = (size_t)c.slice * size + 32;
     const size_t lists = c.n_cta > 1 ? (size_t)c.n_cta * kMaxTop * 8 : 0;
     if (c.smem < lists) c.smem = lists;
+    return c;
+}
+
+// Rows that pass through are cut only where they are few: four CTAs on every SM read as fast as more do, down to slices of 8 KB.
+Cut cut_streams(int rows, int vocab, int size, int sm_count)
+{
+    constexpr int kLeastBytes = 8 * 1024;
+    const int n = 16 / size;
+    const auto per = [&](int ctas) { return ((vocab + ctas - 1) / ctas + n - 1) / n * n; };
+    Cut c{};
+    c.n_cta = 1;
+    while (c.n_cta < kMaxCluster && (long long)rows * c.n_cta * 2 <= 4 * sm_count && per(2 * c.n_cta) * size >= kLeastBytes) c.n_cta *= 2;
+    c.slice = per(c.n_cta);
     return c;
 }
 
@@ -818,6 +1039,13 @@ int logprobs_typed(const Ctx* ctx, int rows, const Cut& c, const RowArgs& a, con
     return launch_rows(token_logprobs_kernel<T>, ready, ctx, rows, c, true, st, a, o);
 }
 
+template <class T>
+int loss_typed(const Ctx* ctx, int rows, const Cut& c, const RowArgs& a, const DistillArgs& o, cudaStream_t st)
+{
+    static std::atomic<bool> ready[64];
+    return launch_rows(distill_loss_kernel<T>, ready, ctx, rows, c, true, st, a, o);
+}
+
 template <class T, bool GIVEN>
 int distill_typed(const Ctx* ctx, int rows, const Cut& c, const RowArgs& a, const DistillArgs& o, cudaStream_t st)
 {
@@ -831,6 +1059,13 @@ int distill_any(const fq_ctx* ctx, int dtype, int rows, int vocab, long long ld,
 {
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
+    if (!o.grad) {
+        const Cut c = cut_streams(rows, vocab, type_size(dtype), ctx->sm_count);
+        const RowArgs a = row_args(ctx, logits, vocab, ld, temperature, c);
+        if (dtype == FQ_DT_F32) return loss_typed<float>(ctx, rows, c, a, o, st);
+        if (dtype == FQ_DT_F16) return loss_typed<__half>(ctx, rows, c, a, o, st);
+        return loss_typed<__nv_bfloat16>(ctx, rows, c, a, o, st);
+    }
     const Cut c = cut_rows(rows, vocab, type_size(dtype), ctx->sm_count);
     const RowArgs a = row_args(ctx, logits, vocab, ld, temperature, c);
     if (dtype == FQ_DT_F32) return distill_typed<float, GIVEN>(ctx, rows, c, a, o, st);
@@ -856,7 +1091,7 @@ int fq_token_logprobs(fq_ctx* ctx, const void* logits_dev, int dtype, int rows, 
         return FQ_ERR_ALIGN;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
-    const Cut c = cut_rows(rows, vocab, type_size(dtype), ctx->sm_count);
+    const Cut c = cut_streams(rows, vocab, type_size(dtype), ctx->sm_count);
     const RowArgs a = row_args(ctx, logits_dev, vocab, ld, temperature, c);
     const LogprobArgs o{tokens_dev, id_bytes == 8, logprob_dev, entropy_dev, n_top, top_ids_dev, top_logprobs_dev};
     const cudaStream_t st = (cudaStream_t)stream;

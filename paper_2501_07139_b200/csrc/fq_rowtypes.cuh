@@ -30,6 +30,9 @@ template <> struct Group<float> {
         m = fmaxf(fmaxf(m, fmaxf(__uint_as_float(v.x), __uint_as_float(v.y))), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
     }
     static __device__ __forceinline__ float of_max(Max m) { return m; }
+    static __device__ __forceinline__ uint4 fill() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }      // -inf
+    static constexpr float kFloor = -1e30f;
+    static __device__ __forceinline__ uint4 above_floor(const uint4& v) { return v; }                                             // (not used)
     static __device__ __forceinline__ float to_f(float v) { return v; }
     static __device__ __forceinline__ float from_f(float v) { return v; }
 };
@@ -59,6 +62,17 @@ template <> struct Group<__nv_bfloat16> {
         m = __hmax2(m, __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
     }
     static __device__ __forceinline__ float of_max(Max m) { return fmaxf(__low2float(m), __high2float(m)); }
+    static __device__ __forceinline__ uint4 fill() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }      // -inf
+    // a value whose exponential is 0 wherever that of -inf is, as long as the largest is far enough above it
+    static constexpr float kFloor = -1e30f;
+    static __device__ __forceinline__ uint4 above_floor(uint4 v)                                                  // (NaN stays)
+    {
+        __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
+        const __nv_bfloat162 low = __float2bfloat162_rn(kFloor);
+#pragma unroll
+        for (int i = 0; i < 4; i++) h[i] = __hmax2_nan(h[i], low);
+        return v;
+    }
     static __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
     static __device__ __forceinline__ __nv_bfloat16 from_f(float v) { return __float2bfloat16_rn(v); }
 };
@@ -88,6 +102,17 @@ template <> struct Group<__half> {
         m = __hmax2(m, __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
     }
     static __device__ __forceinline__ float of_max(Max m) { return fmaxf(__low2float(m), __high2float(m)); }
+    static __device__ __forceinline__ uint4 fill() { return make_uint4(0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u); }      // -inf
+    // a value whose exponential is 0 wherever that of -inf is, as long as the largest is far enough above it
+    static constexpr float kFloor = -65504.0f;
+    static __device__ __forceinline__ uint4 above_floor(uint4 v)                                                  // (NaN stays)
+    {
+        __half2* h = reinterpret_cast<__half2*>(&v);
+        const __half2 low = __float2half2_rn(kFloor);
+#pragma unroll
+        for (int i = 0; i < 4; i++) h[i] = __hmax2_nan(h[i], low);
+        return v;
+    }
     static __device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
     static __device__ __forceinline__ __half from_f(float v) { return __float2half_rn(v); }
 };

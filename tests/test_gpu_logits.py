@@ -335,11 +335,12 @@ def test_streams_and_graphs(fq):
 
 def test_a_wait_that_runs_out_is_reported(fq):
     """With a limit that no copy keeps the call gives up, says so, and later ones are right."""
-    z = rows_of("normal", 300, 60000, torch.float32, 1)
-    tokens = tokens_of(300, 60000, 1)
+    rows, vocab = 300, 60000
+    z = rows_of("normal", rows, vocab, torch.float32, 1)
+    ids, teacher, g = slots_of(rows, vocab, 8, 1)
     fq.fq_set_wait_limit_ns(1)
-    fq.fq_token_logprobs(z, tokens, 5)
+    fq.fq_distill_topk(z, ids, teacher, 1.0, g)
     assert fq.fq_status() == -8
     fq.fq_set_wait_limit_ns(0)
-    check_logprobs(fq, z, tokens, 5, 1.0)
+    check_distill(fq, z, ids, teacher, 1.0, g)
     assert fq.fq_status() == 0
