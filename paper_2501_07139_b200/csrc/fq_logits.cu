@@ -25,6 +25,9 @@ constexpr int kRowThreads = 256;
 constexpr int kRowWarps = kRowThreads / 32;
 constexpr int kMaxTop = FQ_MAX_TOP;
 constexpr int kCandidates = 512;
+constexpr int kBatchBits = 2, kBatch = 1 << kBatchBits;       // 16-byte groups that a thread reads at a time
+constexpr int kSlots = 8;                 // pieces of a thread's groups whose largest entries are kept apart
+constexpr int kFewTop = 64;               // up to here 128 threads have maxima enough to bound the alternatives closely
 constexpr int kBinBits = 7, kBins = 1 << kBinBits;
 constexpr int kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -210,7 +213,7 @@ __device__ __forceinline__ void add_part(RowSums& r, const RowSums& part, float 
 }
 
 // Sums of the slice, in every thread; `least` is the smallest of the threads' keys (of those that have an entry).
-template <bool ENTROPY>
+template <int THREADS, bool ENTROPY>
 __device__ __forceinline__ RowSums slice_sums(const RowSums& mine, uint32_t my_key, float c2, RowShared& sh, uint32_t& least)
 {
     // (a thread without entries, or whose entries are all NaN, has m = -inf; its sum, 0 or NaN, counts as it is)
@@ -223,18 +226,18 @@ __device__ __forceinline__ RowSums slice_sums(const RowSums& mine, uint32_t my_k
     if ((threadIdx.x & 31) == 0) sh.warp[threadIdx.x >> 5] = make_float4(w.m, w.s, w.s1, __uint_as_float(low));
     __syncthreads();
     // every warp adds the warps' up, one to a lane
-    const int lane = threadIdx.x & (kRowWarps - 1);
+    const int lane = threadIdx.x & ((THREADS / 32) - 1);
     const float4 v = sh.warp[lane];
     RowSums r{v.x, 0.0f, 0.0f};
     least = __float_as_uint(v.w);
 #pragma unroll
-    for (int o = 1; o < kRowWarps; o <<= 1) {
+    for (int o = 1; o < (THREADS / 32); o <<= 1) {
         r.m = fmaxf(r.m, __shfl_xor_sync(0xffffffffu, r.m, o));
         least = min(least, __shfl_xor_sync(0xffffffffu, least, o));
     }
     add_part(r, RowSums{v.x, v.y, v.z}, c2);
 #pragma unroll
-    for (int o = 1; o < kRowWarps; o <<= 1) {
+    for (int o = 1; o < (THREADS / 32); o <<= 1) {
         r.s += __shfl_xor_sync(0xffffffffu, r.s, o);
         if (ENTROPY) r.s1 += __shfl_xor_sync(0xffffffffu, r.s1, o);
     }
@@ -275,6 +278,14 @@ __device__ __forceinline__ void await_slice(RowShared& sh, const RowArgs& a)
 // memory more CTAs fit on an SM, and those that search their rows' largest entries are hidden behind those that read.
 
 template <class T>
+__device__ __forceinline__ uint4 load_group(const T* p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+
+template <class T>
 struct Stream {
     const T* src;                // element 0: the 16-byte group in which the slice begins
     Slice s;
@@ -285,13 +296,7 @@ struct Stream {
         lo /= Group<T>::N;
         hi /= Group<T>::N;
     }
-    __device__ __forceinline__ uint4 whole(int group) const
-    {
-        uint4 v;
-        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                     : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(src + (long long)group * Group<T>::N) : "memory");
-        return v;
-    }
+    __device__ __forceinline__ uint4 whole(int group) const { return load_group(src + (long long)group * Group<T>::N); }
     // Group `group` if it is one of those at the ends, -inf for what is not the slice's.
     __device__ __noinline__ uint4 end(int group) const
     {
@@ -314,13 +319,14 @@ struct Running {
     float m = kNegInf;
     float2 s = {0.0f, 0.0f}, s1 = {0.0f, 0.0f};
 
+    // Returns the largest of these entries.
     template <int G>
-    __device__ __forceinline__ void take(const uint4 (&v)[G], float c2)
+    __device__ __forceinline__ float take(const uint4 (&v)[G], float c2)
     {
         typename Group<T>::Max best = Group<T>::lowest();
 #pragma unroll
         for (int g = 0; g < G; g++) Group<T>::take_max(best, v[g]);
-        const float higher = fmaxf(m, Group<T>::of_max(best));
+        const float here = Group<T>::of_max(best), higher = fmaxf(m, here);
         if (higher > m) {                                        // the sums so far are put on the new maximum
             const float t = (m - higher) * c2, f = ex2(t);       // (m = -inf: factor 0; the sums are 0 or NaN)
             if (ENTROPY) {
@@ -341,6 +347,7 @@ struct Running {
 #pragma unroll
             for (int g = 0; g < G; g++) add<ENTROPY>(v[g], mm, c2);
         }
+        return here;
     }
     template <bool CLAMP>
     __device__ __forceinline__ void add(const uint4& v, float mm, float c2)
@@ -362,41 +369,40 @@ struct Running {
     __device__ __forceinline__ RowSums sums() const { return RowSums{m, s.x + s.y, ENTROPY ? s1.x + s1.y : 0.0f}; }
 };
 
-// Sums of this thread's groups lo + thread, + 256 ...; those at the ends are the first threads' of two warps.
-template <class T, bool ENTROPY>
-__device__ __forceinline__ RowSums stream_sums(const Stream<T>& x, float c2)
+// Sums of this thread's groups lo + thread, + THREADS ..., kBatch of them at a time; those at the ends are the first threads' of two
+// warps.  largest (or NULL): [kSlots][THREADS], -inf before; gets the largest entry of the thread's batches b, b + kSlots, ... in [b].
+template <class T, int THREADS, bool ENTROPY>
+__device__ __forceinline__ RowSums stream_sums(const Stream<T>& x, float c2, float* largest)
 {
-    constexpr int U = 4;
+    constexpr int U = kBatch;
     Running<T, ENTROPY> run;
-    int i = x.lo + threadIdx.x;
-    if (i + (U - 1) * kRowThreads < x.hi) {
+    const T* at = x.src + (long long)(x.lo + (int)threadIdx.x) * Group<T>::N;
+    int left = x.hi - x.lo - (int)threadIdx.x;                   // > g THREADS: there is a group g rounds on
+    int slot = threadIdx.x;
+    const auto keep = [&](float here) {
+        if (!largest) return;
+        largest[slot] = fmaxf(largest[slot], here);
+        slot = slot + THREADS < kSlots * THREADS ? slot + THREADS : (int)threadIdx.x;
+    };
+    for (; left > (U - 1) * THREADS; left -= U * THREADS, at += U * THREADS * Group<T>::N) {
         uint4 v[U];
 #pragma unroll
-        for (int g = 0; g < U; g++) v[g] = x.whole(i + g * kRowThreads);
-        for (;;) {
-            i += U * kRowThreads;
-            const bool more = i + (U - 1) * kRowThreads < x.hi;
-            uint4 w[U];
-            if (more)
-#pragma unroll
-                for (int g = 0; g < U; g++) w[g] = x.whole(i + g * kRowThreads);
-            run.take(v, c2);
-            if (!more) break;
-#pragma unroll
-            for (int g = 0; g < U; g++) v[g] = w[g];
-        }
+        for (int g = 0; g < U; g++) v[g] = load_group(at + g * THREADS * Group<T>::N);
+        keep(run.take(v, c2));
     }
-    uint4 v[U];
+    uint4 v[U - 1];
 #pragma unroll
-    for (int g = 0; g < U; g++) {
+    for (int g = 0; g < U - 1; g++) {
         v[g] = Group<T>::fill();
-        if (i + g * kRowThreads < x.hi) v[g] = x.whole(i + g * kRowThreads);
+        if (left > g * THREADS) v[g] = load_group(at + g * THREADS * Group<T>::N);
     }
-    if (i + 2 * kRowThreads < x.hi) {
-        run.take(v, c2);
-    } else if (i < x.hi) {
-        const uint4 half[2] = {v[0], v[1]};
-        run.take(half, c2);
+    if (left > (U / 2) * THREADS) {
+        keep(run.take(v, c2));
+    } else if (left > 0) {
+        uint4 half[U / 2];
+#pragma unroll
+        for (int g = 0; g < U / 2; g++) half[g] = v[g];
+        keep(run.take(half, c2));
     }
     const int end = threadIdx.x == 0 && x.s.groups > 0 && !x.is_whole(0) ? 0 : threadIdx.x == 32 && x.hi > 0 && x.hi < x.s.groups ? x.hi : -1;
     if (end >= 0) {
@@ -407,18 +413,22 @@ __device__ __forceinline__ RowSums stream_sums(const Stream<T>& x, float c2)
 }
 
 // ------------------------------------------------------------------------------- the largest entries of a slice
-struct __align__(16) TopShared {
-    uint4 data[kCandidates];                  // groups that hold a candidate
+template <int THREADS>
+struct TopShared {
     unsigned long long cand[kCandidates];     // (key, ~index): larger is earlier
     unsigned long long top[kMaxTop];
-    uint32_t key[kRowThreads];                // the threads' maxima
-    int bins[256];                            // zeroed before
-    int n_groups, n_cand;                     // zeroed before
-    int n_threads, n_top;
+    union {
+        struct {
+            float largest[kSlots * THREADS];          // of some batches of a thread each; -inf before
+            unsigned short piece[kSlots * THREADS];   // those that may hold a candidate
+        };
+        unsigned long long lists[kMaxCluster * kMaxTop];      // of all CTAs, in the first one
+    };
+    int bins[256];                            // the first kBins zeroed before
+    int n_pieces, n_cand;                     // zeroed before
+    int n_top;
     float reach;
-    int group[kCandidates];
-    unsigned char thread[kRowThreads];
-    int warp[kRowWarps];
+    int warp[THREADS / 32];
     int list_len[kMaxCluster];
 };
 
@@ -459,8 +469,8 @@ __device__ __forceinline__ int bin_of_kth(const int* bins, int k, At&& at, int& 
 
 // Too many entries reach the bound (a row of equal logits): the k-th largest key is found digit by digit, a pass over the slice each,
 // then its first bearers in order of their indices.  Leaves exactly k candidates.  Needs as many finite entries as k.
-template <class T>
-__device__ __noinline__ void exact_candidates(const Stream<T>& x, int k, TopShared& sh)
+template <class T, int THREADS>
+__device__ __noinline__ void exact_candidates(const Stream<T>& x, int k, TopShared<THREADS>& sh)
 {
     constexpr int N = Group<T>::N;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -468,10 +478,10 @@ __device__ __noinline__ void exact_candidates(const Stream<T>& x, int k, TopShar
     int need = k;                                                      // of the entries whose upper digits are those of kth
     for (int d = 24; d >= 0; d -= 8) {
         __syncthreads();
-        sh.bins[threadIdx.x] = 0;
+        for (int i = threadIdx.x; i < 256; i += THREADS) sh.bins[i] = 0;
         __syncthreads();
         int digit = 0, run = 0;                                        // alike entries in a row are counted before they are added
-        for (int i = threadIdx.x; i < x.s.groups; i += kRowThreads) {
+        for (int i = threadIdx.x; i < x.s.groups; i += THREADS) {
             const uint4 v = x.any(i);
             for (int e = 0; e < N; e++) {
                 const float z = Group<T>::to_f(reinterpret_cast<const T*>(&v)[e]);
@@ -495,7 +505,7 @@ __device__ __noinline__ void exact_candidates(const Stream<T>& x, int k, TopShar
     __syncthreads();
     // those above it, fewer than k, in any order; its bearers, in order, until there are enough
     int taken = 0;
-    for (int i0 = 0; i0 < x.s.groups; i0 += kRowThreads) {
+    for (int i0 = 0; i0 < x.s.groups; i0 += THREADS) {
         const int i = i0 + threadIdx.x;
         unsigned bearers = 0;
         uint4 v = Group<T>::fill();
@@ -522,7 +532,7 @@ __device__ __noinline__ void exact_candidates(const Stream<T>& x, int k, TopShar
         if (lane == 31) sh.warp[warp] = upto;
         __syncthreads();
         int before = taken, all = 0;
-        for (int w = 0; w < kRowWarps; w++) {
+        for (int w = 0; w < THREADS / 32; w++) {
             if (w < warp) before += sh.warp[w];
             all += sh.warp[w];
         }
@@ -540,17 +550,13 @@ __device__ __noinline__ void exact_candidates(const Stream<T>& x, int k, TopShar
 
 // Calls place(rank, word) for the k largest entries, once each, and returns how many there are (fewer than k if the slice has no more).
 //   The threads' own maxima bound the k-th largest entry from below, k of them being entries.  A histogram of them over
-//   [least, most] gives a bound within 1/128 of that range; what reaches it, usually a few more entries than k, is found in three steps
-//   that each deal the little there is to do to all threads: the threads whose maximum does, the groups of theirs that hold an
-//   entry that does (read once more, from the L2 as a rule), the entries.  Then they are ordered by counting.  (4094 x 32000 bf16,
-//   k = 32: a warp that goes through its own threads' groups spends 6500 instructions of the CTA's warps on all this, where the sums
-//   take 8700; like this it is 2600.)
-template <class T, class Fn>
-__device__ __forceinline__ int slice_top(const Stream<T>& x, int k, uint32_t my_key, uint32_t least, uint32_t most, TopShared& sh, Fn&& place)
+//   [least, most] gives a bound within 1/128 of that range; what reaches it, usually a few more entries than k, is found in two steps
+//   that each deal the little there is to do to all threads: the batches whose maximum does, then the entries of their groups (read
+//   once more, from the L2 as a rule).  Then they are ordered by counting.
+template <class T, int THREADS, class Fn>
+__device__ __forceinline__ int slice_top(const Stream<T>& x, int k, uint32_t my_key, uint32_t least, uint32_t most, TopShared<THREADS>& sh, Fn&& place)
 {
     constexpr int N = Group<T>::N;
-    const int lane = threadIdx.x & 31;
-    sh.key[threadIdx.x] = my_key;
     const int span = 32 - __clz((int)(most - least)), shift = span > kBinBits ? span - kBinBits : 0;
     if (my_key) atomicAdd(&sh.bins[bin_at((int)((my_key - least) >> shift))], 1);
     __syncthreads();
@@ -558,54 +564,48 @@ __device__ __forceinline__ int slice_top(const Stream<T>& x, int k, uint32_t my_
         int above;
         const int bin = bin_of_kth<kBins / 32>(sh.bins, k, [](int b) { return bin_at(b); }, above);
         // (fewer than k threads have an entry: the lowest finite value)
-        const uint32_t bound = bin < 0 ? 0x00800000u : least + ((uint32_t)bin << shift);
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < kRowWarps; i++) {
-            const bool yes = sh.key[i * 32 + lane] >= bound;
-            const unsigned all = __ballot_sync(0xffffffffu, yes);
-            if (yes) sh.thread[n + __popc(all & ((1u << lane) - 1))] = (unsigned char)(i * 32 + lane);
-            n += __popc(all);
-        }
-        if (lane == 0) {
-            sh.n_threads = n;
-            sh.reach = of_key(bound);
-        }
+        if (threadIdx.x == 0) sh.reach = of_key(bin < 0 ? 0x00800000u : least + ((uint32_t)bin << shift));
     }
     __syncthreads();
     const float reach = sh.reach;                                      // (compared as a number, not met by -inf or NaN)
-    const int rounds = (x.hi - x.lo + kRowThreads - 1) / kRowThreads, bits = rounds > 1 ? 32 - __clz(rounds - 1) : 0;
-    const int items = sh.n_threads << bits;
-    for (int i = threadIdx.x; i < items + 2; i += kRowThreads) {
-        // the groups of those threads, and the two at the ends
-        const int group = i < items ? x.lo + sh.thread[i >> bits] + (i & ((1 << bits) - 1)) * kRowThreads : i == items ? 0 : x.s.groups - 1;
-        if (i < items ? group >= x.hi : x.s.groups == 0 || x.is_whole(group) || (i > items && group == 0)) continue;
+#pragma unroll
+    for (int i = 0; i < kSlots; i++)
+        if (sh.largest[i * THREADS + threadIdx.x] >= reach) sh.piece[atomicAdd(&sh.n_pieces, 1)] = (unsigned short)(i * THREADS + threadIdx.x);
+    __syncthreads();
+    // a piece is up to 2^bits groups: kBatch of every kSlots-th batch
+    const int rounds = (x.hi - x.lo + THREADS - 1) / THREADS, turns = (rounds + kSlots * kBatch - 1) / (kSlots * kBatch);
+    const int bits = kBatchBits + (turns > 1 ? 32 - __clz(turns - 1) : 0), items = sh.n_pieces << bits;
+    for (int i = threadIdx.x; i < items + 2; i += THREADS) {           // and the two groups at the ends
+        int group;
+        if (i < items) {
+            const int piece = sh.piece[i >> bits], part = i & ((1 << bits) - 1);
+            group = x.lo + piece % THREADS + ((part >> kBatchBits) * kSlots + piece / THREADS) * kBatch * THREADS + (part & (kBatch - 1)) * THREADS;
+            if (group >= x.hi) continue;
+        } else {
+            group = i == items ? 0 : x.s.groups - 1;
+            if (x.s.groups == 0 || x.is_whole(group) || (i > items && group == 0)) continue;
+        }
         const uint4 v = i < items ? x.whole(group) : x.end(group);
-        typename Group<T>::Max m = Group<T>::lowest();
-        Group<T>::take_max(m, v);
-        if (Group<T>::of_max(m) >= reach) {
-            const int at = atomicAdd(&sh.n_groups, 1);
-            if (at < kCandidates) { sh.group[at] = group; sh.data[at] = v; }
+        float2 f[N / 2];
+        Group<T>::unpack(v, f);
+        unsigned found = 0;
+#pragma unroll
+        for (int e = 0; e < N; e++) found |= (e & 1 ? f[e / 2].y : f[e / 2].x) >= reach ? 1u << e : 0u;
+        for (; found; found &= found - 1) {
+            const int e = __ffs((int)found) - 1, at = atomicAdd(&sh.n_cand, 1);
+            float z = f[0].x;
+#pragma unroll
+            for (int j = 1; j < N; j++) z = j == e ? (j & 1 ? f[j / 2].y : f[j / 2].x) : z;
+            if (at < kCandidates) sh.cand[at] = entry_word(key_of(z), x.s.first + group * N + e - x.s.shift);
         }
     }
-    __syncthreads();
-    const int n_groups = sh.n_groups;
-    const T* el = reinterpret_cast<const T*>(sh.data);
-    if (n_groups <= kCandidates)
-        for (int i = threadIdx.x; i < n_groups * N; i += kRowThreads) {
-            const float v = Group<T>::to_f(el[i]);
-            if (v >= reach) {
-                const int at = atomicAdd(&sh.n_cand, 1);
-                if (at < kCandidates) sh.cand[at] = entry_word(key_of(v), x.s.first + sh.group[i / N] * N + i % N - x.s.shift);
-            }
-        }
     __syncthreads();
     int n = sh.n_cand;
-    if (n > kCandidates || n_groups > kCandidates) {
-        exact_candidates<T>(x, k, sh);
+    if (n > kCandidates) {
+        exact_candidates<T, THREADS>(x, k, sh);
         n = sh.n_cand;
     }
-    for (int c = threadIdx.x; c < n; c += kRowThreads) {
+    for (int c = threadIdx.x; c < n; c += THREADS) {
         const unsigned long long w = sh.cand[c];
         int rank = 0;
 #pragma unroll 8
@@ -651,38 +651,41 @@ struct RowAnswer {
     }
 };
 
-template <class T>
-__global__ void __launch_bounds__(kRowThreads, 4) token_logprobs_kernel(const RowArgs a, const LogprobArgs o)
+template <class T, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel(const RowArgs a, const LogprobArgs o)
 {
     __shared__ RowShared sh;
-    __shared__ TopShared top;
+    __shared__ TopShared<THREADS> top;
     const int rank = a.n_cta > 1 ? (int)cluster_cta() : 0;
     const long long r = blockIdx.x / a.n_cta;
     const T* row = static_cast<const T*>(a.z) + r * a.ld;
     const Stream<T> x(row, slice_of<T>(a, row, rank));
     // the last warp asks for the token, and for its logit at the end
-    const bool scalar = rank == 0 && threadIdx.x == kRowThreads - 32;
+    const bool scalar = rank == 0 && threadIdx.x == THREADS - 32;
     const long long token = scalar ? load_id(o.tokens, o.wide, r) : -1;
-    for (int i = threadIdx.x; i < kBins; i += kRowThreads) top.bins[i] = 0;
-    if (threadIdx.x == kRowThreads - 1) top.n_groups = top.n_cand = 0;
-    const RowSums mine = stream_sums<T, true>(x, a.c2);
+    for (int i = threadIdx.x; i < kBins; i += THREADS) top.bins[i] = 0;
+    if (threadIdx.x == THREADS - 1) top.n_pieces = top.n_cand = 0;
+    if (o.n_top > 0)
+#pragma unroll
+        for (int i = 0; i < kSlots; i++) top.largest[i * THREADS + threadIdx.x] = kNegInf;
+    const RowSums mine = stream_sums<T, THREADS, true>(x, a.c2, o.n_top > 0 ? top.largest : nullptr);
     const float z_token = token >= 0 && token < a.vocab ? Group<T>::to_f(row[token]) : 0.0f;
     const uint32_t my_key = mine.m > kNegInf ? key_of(mine.m) : 0u;
     uint32_t least;
-    RowSums sum = slice_sums<true>(mine, my_key, a.c2, sh, least);
+    RowSums sum = slice_sums<THREADS, true>(mine, my_key, a.c2, sh, least);
     const uint32_t most = sum.m > kNegInf ? key_of(sum.m) : 0u;
     if (least > most) least = most;                              // (no thread has an entry)
     if (a.n_cta == 1) {
         const RowAnswer ans(sum, a.t);
         if (scalar) ans.put(o, r, a.vocab, token, z_token, sum);
         if (o.n_top > 0) {
-            const int n = slice_top<T>(x, o.n_top, my_key, least, most, top, [&](int place, unsigned long long w) { ans.put_top(o, r, place, w); });
-            for (int j = n + threadIdx.x; j < o.n_top; j += kRowThreads) ans.put_none(o, r, j);
+            const int n = slice_top<T, THREADS>(x, o.n_top, my_key, least, most, top, [&](int place, unsigned long long w) { ans.put_top(o, r, place, w); });
+            for (int j = n + threadIdx.x; j < o.n_top; j += THREADS) ans.put_none(o, r, j);
         }
         return;
     }
     if (o.n_top > 0) {
-        const int n = slice_top<T>(x, o.n_top, my_key, least, most, top, [&](int place, unsigned long long w) { top.top[place] = w; });
+        const int n = slice_top<T, THREADS>(x, o.n_top, my_key, least, most, top, [&](int place, unsigned long long w) { top.top[place] = w; });
         if (threadIdx.x == 0) top.n_top = n;
     }
     if (threadIdx.x == 0) sh.sums = sum;
@@ -694,20 +697,19 @@ __global__ void __launch_bounds__(kRowThreads, 4) token_logprobs_kernel(const Ro
         if (scalar) ans.put(o, r, a.vocab, token, z_token, sum);
         // the CTAs' lists, merged: an entry's place is its own place in its list and what is larger in each of the others
         if (o.n_top > 0) {
-            unsigned long long* lists = reinterpret_cast<unsigned long long*>(top.data);
-            static_assert(sizeof top.data >= sizeof(unsigned long long) * kMaxCluster * kMaxTop, "room for the lists");
+            unsigned long long* lists = top.lists;
             int* lens = top.list_len;
             const uint32_t at = smem_u32(top.top), at_n = smem_u32(&top.n_top);
             if (threadIdx.x < a.n_cta) lens[threadIdx.x] = cluster_ld_s32(cluster_map(at_n, threadIdx.x));
             __syncthreads();
-            for (int i = threadIdx.x; i < a.n_cta * kMaxTop; i += kRowThreads) {
+            for (int i = threadIdx.x; i < a.n_cta * kMaxTop; i += THREADS) {
                 const int c = i / kMaxTop, j = i % kMaxTop;
                 if (j < lens[c]) lists[i] = cluster_ld_u64(cluster_map(at, (uint32_t)c) + (uint32_t)j * 8);
             }
             __syncthreads();
             int total = 0;
             for (int c = 0; c < a.n_cta; c++) total += lens[c];
-            for (int i = threadIdx.x; i < a.n_cta * kMaxTop; i += kRowThreads) {
+            for (int i = threadIdx.x; i < a.n_cta * kMaxTop; i += THREADS) {
                 const int c = i / kMaxTop, j = i % kMaxTop;
                 if (j >= lens[c]) continue;
                 const unsigned long long w = lists[i];
@@ -723,7 +725,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) token_logprobs_kernel(const Ro
                 }
                 if (place < o.n_top) ans.put_top(o, r, place, w);
             }
-            for (int j = total + threadIdx.x; j < o.n_top; j += kRowThreads) ans.put_none(o, r, j);
+            for (int j = total + threadIdx.x; j < o.n_top; j += THREADS) ans.put_none(o, r, j);
         }
     }
     cluster_arrive();                                                    // nobody's shared memory is read any more
@@ -802,8 +804,8 @@ __device__ __forceinline__ float distill_loss(TeacherShared& te, int k, const Ro
 }
 
 // The value alone: the logits pass through once.
-template <class T>
-__global__ void __launch_bounds__(kRowThreads, 4) distill_loss_kernel(const RowArgs a, const DistillArgs o)
+template <class T, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_loss_kernel(const RowArgs a, const DistillArgs o)
 {
     __shared__ RowShared sh;
     __shared__ TeacherShared te;
@@ -818,11 +820,11 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_loss_kernel(const RowA
         if (id >= 0 && id < a.vocab) z_id = Group<T>::to_f(row[id]);
         te.lp[threadIdx.x] = id >= 0 ? u : kNegInf;
     }
-    const RowSums mine = stream_sums<T, false>(Stream<T>(row, slice_of<T>(a, row, rank)), a.c2);
+    const RowSums mine = stream_sums<T, THREADS, false>(Stream<T>(row, slice_of<T>(a, row, rank)), a.c2, nullptr);
     const bool bad = __syncthreads_or(id >= a.vocab);
     if (rank == 0 && threadIdx.x < 32) teacher_softmax(te, o.k, a.c2, a.t);
     uint32_t least;
-    RowSums sum = slice_sums<false>(mine, mine.m > kNegInf ? key_of(mine.m) : 0u, a.c2, sh, least);
+    RowSums sum = slice_sums<THREADS, false>(mine, mine.m > kNegInf ? key_of(mine.m) : 0u, a.c2, sh, least);
     if (a.n_cta > 1) {
         if (threadIdx.x == 0) sh.sums = sum;
         cluster_arrive();
@@ -884,7 +886,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_kernel(const RowArgs a
     } else {
         const RowSums mine = thread_sums<T, false>(buf, s.groups, a.c2);
         uint32_t least;
-        sum = slice_sums<false>(mine, mine.m > kNegInf ? key_of(mine.m) : 0u, a.c2, sh, least);
+        sum = slice_sums<kRowThreads, false>(mine, mine.m > kNegInf ? key_of(mine.m) : 0u, a.c2, sh, least);
         if (a.n_cta > 1) {
             if (threadIdx.x == 0) sh.sums = sum;
             cluster_arrive();
@@ -981,21 +983,21 @@ Cut cut_rows(int rows, int vocab, int size, int sm_count)
     return c;
 }
 
-// Rows that pass through are cut only where they are few: four CTAs on every SM read as fast as more do, down to slices of 8 KB.
-Cut cut_streams(int rows, int vocab, int size, int sm_count)
+// Rows that pass through are cut only where they are few: until the SMs have all the CTAs that they hold, down to slices of 8 KB.
+Cut cut_streams(int rows, int vocab, int size, int sm_count, int threads)
 {
     constexpr int kLeastBytes = 8 * 1024;
     const int n = 16 / size;
     const auto per = [&](int ctas) { return ((vocab + ctas - 1) / ctas + n - 1) / n * n; };
     Cut c{};
     c.n_cta = 1;
-    while (c.n_cta < kMaxCluster && (long long)rows * c.n_cta * 2 <= 4 * sm_count && per(2 * c.n_cta) * size >= kLeastBytes) c.n_cta *= 2;
+    while (c.n_cta < kMaxCluster && (long long)rows * c.n_cta * 2 <= 1024 / threads * sm_count && per(2 * c.n_cta) * size >= kLeastBytes) c.n_cta *= 2;
     c.slice = per(c.n_cta);
     return c;
 }
 
 template <class... Args>
-int launch_rows(void (*kernel)(Args...), std::atomic<bool>* ready, const Ctx* ctx, int rows, const Cut& c, bool cluster, cudaStream_t st,
+int launch_rows(void (*kernel)(Args...), int threads, std::atomic<bool>* ready, const Ctx* ctx, int rows, const Cut& c, bool cluster, cudaStream_t st,
                 Args... args)
 {
     if (ctx->device >= 64) return FQ_ERR_ARG;
@@ -1007,7 +1009,7 @@ int launch_rows(void (*kernel)(Args...), std::atomic<bool>* ready, const Ctx* ct
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = (unsigned)c.n_cta; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)rows * (unsigned)c.n_cta); cfg.blockDim = dim3(kRowThreads); cfg.dynamicSmemBytes = c.smem;
+    cfg.gridDim = dim3((unsigned)rows * (unsigned)c.n_cta); cfg.blockDim = dim3((unsigned)threads); cfg.dynamicSmemBytes = c.smem;
     cfg.stream = st;
     if (cluster && c.n_cta > 1) { cfg.attrs = &attr; cfg.numAttrs = 1; }
     return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
@@ -1035,22 +1037,23 @@ RowArgs row_args(const Ctx* ctx, const void* logits, int vocab, long long ld, fl
 template <class T>
 int logprobs_typed(const Ctx* ctx, int rows, const Cut& c, const RowArgs& a, const LogprobArgs& o, cudaStream_t st)
 {
-    static std::atomic<bool> ready[64];
-    return launch_rows(token_logprobs_kernel<T>, ready, ctx, rows, c, true, st, a, o);
+    static std::atomic<bool> ready[2][64];
+    return o.n_top <= kFewTop ? launch_rows(token_logprobs_kernel<T, 128>, 128, ready[0], ctx, rows, c, true, st, a, o)
+                              : launch_rows(token_logprobs_kernel<T, 256>, 256, ready[1], ctx, rows, c, true, st, a, o);
 }
 
 template <class T>
 int loss_typed(const Ctx* ctx, int rows, const Cut& c, const RowArgs& a, const DistillArgs& o, cudaStream_t st)
 {
     static std::atomic<bool> ready[64];
-    return launch_rows(distill_loss_kernel<T>, ready, ctx, rows, c, true, st, a, o);
+    return launch_rows(distill_loss_kernel<T, 128>, 128, ready, ctx, rows, c, true, st, a, o);
 }
 
 template <class T, bool GIVEN>
 int distill_typed(const Ctx* ctx, int rows, const Cut& c, const RowArgs& a, const DistillArgs& o, cudaStream_t st)
 {
     static std::atomic<bool> ready[64];
-    return launch_rows(distill_kernel<T, GIVEN>, ready, ctx, rows, c, !GIVEN, st, a, o);
+    return launch_rows(distill_kernel<T, GIVEN>, kRowThreads, ready, ctx, rows, c, !GIVEN, st, a, o);
 }
 
 template <bool GIVEN>
@@ -1060,7 +1063,7 @@ int distill_any(const fq_ctx* ctx, int dtype, int rows, int vocab, long long ld,
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
     if (!o.grad) {
-        const Cut c = cut_streams(rows, vocab, type_size(dtype), ctx->sm_count);
+        const Cut c = cut_streams(rows, vocab, type_size(dtype), ctx->sm_count, 128);
         const RowArgs a = row_args(ctx, logits, vocab, ld, temperature, c);
         if (dtype == FQ_DT_F32) return loss_typed<float>(ctx, rows, c, a, o, st);
         if (dtype == FQ_DT_F16) return loss_typed<__half>(ctx, rows, c, a, o, st);
@@ -1091,7 +1094,7 @@ int fq_token_logprobs(fq_ctx* ctx, const void* logits_dev, int dtype, int rows, 
         return FQ_ERR_ALIGN;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
-    const Cut c = cut_streams(rows, vocab, type_size(dtype), ctx->sm_count);
+    const Cut c = cut_streams(rows, vocab, type_size(dtype), ctx->sm_count, n_top <= kFewTop ? 128 : 256);
     const RowArgs a = row_args(ctx, logits_dev, vocab, ld, temperature, c);
     const LogprobArgs o{tokens_dev, id_bytes == 8, logprob_dev, entropy_dev, n_top, top_ids_dev, top_logprobs_dev};
     const cudaStream_t st = (cudaStream_t)stream;
