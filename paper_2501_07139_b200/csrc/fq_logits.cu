@@ -964,17 +964,20 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_kernel(const RowArgs a
 }
 
 // ------------------------------------------------------------------------------- host side
-// How the rows are cut.  A slice of up to 68 KB leaves room for three CTAs on an SM, so that one computes while the copies of the
-// others are on their way.  With few rows a row is spread over more SMs, down to slices of 8 KB.
+// How rows that stay on chip are cut.  A slice of up to 68 KB leaves room for three CTAs on an SM, so that one computes while the copies
+// of the others are on their way.  Where the CTAs of a row need nothing from one another, slices of up to 36 KB, six to an SM, are better
+// (gradient alone, 4096 x 32000 bf16: 87 us against 93; with clusters of two, value and gradient: 146 us against 109).  With few
+// rows a row is spread over more SMs, down to slices of 8 KB.
 struct Cut { int n_cta, slice; size_t smem; };
-Cut cut_rows(int rows, int vocab, int size, int sm_count)
+Cut cut_rows(int rows, int vocab, int size, int sm_count, bool cluster)
 {
-    constexpr int kSliceBytes = 68 * 1024, kLeastBytes = 8 * 1024;
+    constexpr int kLeastBytes = 8 * 1024;
+    const int slice_bytes = (cluster ? 68 : 36) * 1024;
     const int n = 16 / size;
     Cut c{};
     const auto per = [&](int ctas) { return ((vocab + ctas - 1) / ctas + n - 1) / n * n; };
     c.n_cta = 1;
-    while (c.n_cta < kMaxCluster && per(c.n_cta) * size > kSliceBytes) c.n_cta *= 2;
+    while ((c.n_cta < kMaxCluster || !cluster) && per(c.n_cta) * size > slice_bytes) c.n_cta *= 2;
     while (c.n_cta < kMaxCluster && (long long)rows * c.n_cta * 2 <= sm_count && per(2 * c.n_cta) * size >= kLeastBytes) c.n_cta *= 2;
     c.slice = per(c.n_cta);
     c.smem = (size_t)c.slice * size + 32;
@@ -1069,7 +1072,7 @@ int distill_any(const fq_ctx* ctx, int dtype, int rows, int vocab, long long ld,
         if (dtype == FQ_DT_F16) return loss_typed<__half>(ctx, rows, c, a, o, st);
         return loss_typed<__nv_bfloat16>(ctx, rows, c, a, o, st);
     }
-    const Cut c = cut_rows(rows, vocab, type_size(dtype), ctx->sm_count);
+    const Cut c = cut_rows(rows, vocab, type_size(dtype), ctx->sm_count, !GIVEN);
     const RowArgs a = row_args(ctx, logits, vocab, ld, temperature, c);
     if (dtype == FQ_DT_F32) return distill_typed<float, GIVEN>(ctx, rows, c, a, o, st);
     if (dtype == FQ_DT_F16) return distill_typed<__half, GIVEN>(ctx, rows, c, a, o, st);
