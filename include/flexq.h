@@ -305,7 +305,8 @@ int fq_quantize_rows(fq_ctx* ctx, const void* x_dev, int dtype, int rows, int co
 /* Product of 8-bit codes with a scale for every token and every output channel:
  *   Y[m][n] = (fp32(sum_k xc[m][k] * wc[n][k]) * x_scales[m]) * w_scales[n]
  * The sum is exact (32-bit integers; k_in <= 131071); fp32 products, Y rounded once to y_dtype.
- *   x_codes_dev int8 [M][ldx >= k_in], w_codes_dev int8 [n_out][ldw >= k_in]: 16-byte aligned, ldx and ldw multiples of 16.
+ *   x_codes_dev int8 [M][ldx >= k_in], w_codes_dev int8 [n_out][ldw >= k_in]: 16-byte aligned, ldx and ldw multiples of 16.  What lies
+ *               between k_in and the next multiple of 16 may be read, whatever it is, and does not count.
  *   Y_dev       y_dtype [M][ldy >= n_out]: 16-byte aligned, rows a multiple of 16 bytes apart.
  * 1 <= M, n_out <= 2^20. */
 int fq_gemm_i8(fq_ctx* ctx, const int8_t* x_codes_dev, const float* x_scales_dev, int M, long long ldx, const int8_t* w_codes_dev,

@@ -8,7 +8,9 @@
 #include <cudaTypedefs.h>
 
 #include <atomic>
+#include <cstdlib>
 
+#include "fq_cluster.cuh"
 #include "fq_internal.cuh"
 #include "fq_ptx.cuh"
 #include "fq_rowtypes.cuh"
@@ -59,6 +61,24 @@ __device__ __forceinline__ void tmem_ld32(uint32_t (&v)[32], uint32_t addr)
           "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
         : "r"(addr) : "memory");
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void tmem_ld16(uint32_t (&v)[16], uint32_t addr)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(addr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 
 // 32 neighbouring outputs of a row: `n` of them exist, dst is 16-byte aligned.
@@ -237,7 +257,226 @@ gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     }
 }
 
+// ------------------------------------------------------------------------------- some tokens: weights in strips
+// Up to kStripTokens tokens: the weights are the larger operand by far, and the time is that of reading them.  Roles change places: a tile is 128
+// outputs (UMMA M) x all the tokens (UMMA N, a multiple of 16), and K is split over the CTAs of a cluster so that all SMs read at once.
+// The CTAs' sums, 32-bit integers whose order does not matter, meet in distributed shared memory: CTA r of the cluster adds up
+// and writes the tokens r, r + S, ...
+//
+// Behind the quantiser the kernel starts early and fetches weights while the tokens are still being quantised: the quantiser has waited for everything
+// before it, so that the weights are there; only the codes have to be waited for.
+constexpr int kStripTokens = 128;
+constexpr int kStripTmemCols = 128;
+constexpr int kStripStageW = 128 * kBK;                  // 16 KB
+constexpr int kStripMaxStages = 12;
+
+struct StripArgs {
+    I8Args a;
+    int nt;                      // tokens of a tile
+    int stages;
+    int splits;                  // CTAs of a cluster
+    int early;                   // the previous kernel writes the codes, and nothing else that is read here
+};
+
+constexpr int strip_bars_bytes() { return (2 * kStripMaxStages + 1) * 8 + 16; }
+
+template <class T>
+__global__ void __launch_bounds__(kThreads) gemm_i8_strip_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                                                                 const StripArgs q)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = q.splits > 1 ? (int)cluster_cta() : 0, tile = (int)blockIdx.x / q.splits, m0 = (int)blockIdx.y * q.nt;
+    const int stage_bytes = kStripStageW + q.nt * kBK;
+    uint8_t* tail = smem + q.stages * stage_bytes;
+    const uint32_t bars = g_smem_u32(tail), full0 = bars, empty0 = bars + 8 * kStripMaxStages, done = bars + 16 * kStripMaxStages;
+    volatile uint32_t* tmem_ptr = reinterpret_cast<volatile uint32_t*>(tail + (2 * kStripMaxStages + 1) * 8);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_ptr + 1);
+    const I8Args& a = q.a;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < q.stages; s++) {
+            mbar_init(full0 + 8 * s, 1);
+            mbar_init(empty0 + 8 * s, 1);
+        }
+        mbar_init(done, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {                     // this warp owns the TMEM allocation
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(g_smem_u32(const_cast<uint32_t*>(tmem_ptr))), "n"(kStripTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem_base = *tmem_ptr;
+
+    const int k_steps = (a.K + kBK - 1) / kBK;
+    const int k0 = (int)((long long)k_steps * rank / q.splits), k1 = (int)((long long)k_steps * (rank + 1) / q.splits);
+    if (!q.early) asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    if (warp == 0) {
+        // ================================================================== TMA producer
+        if (lane == 0) {
+            const auto stage_at = [&](int s) { return g_smem_u32(smem + s * stage_bytes); };
+            const int ahead = k1 - k0 < q.stages ? k1 - k0 : q.stages;
+            for (int s = 0; s < ahead; s++) {
+                mbar_expect_tx(full0 + 8 * s, (uint32_t)stage_bytes);
+                tma_load_2d(stage_at(s), &map_w, (k0 + s) * kBK, tile * 128, full0 + 8 * s);
+            }
+            if (q.early) asm volatile("griddepcontrol.wait;" ::: "memory");
+            for (int s = 0; s < ahead; s++) tma_load_2d(stage_at(s) + kStripStageW, &map_x, (k0 + s) * kBK, m0, full0 + 8 * s);
+            int stage = 0;
+            uint32_t wraps = 0;
+            bool ok = true;
+            for (int ks = k0 + ahead; ks < k1 && ok; ks++) {
+                ok = g_wait(empty0 + 8 * stage, wraps & 1u, abort_flag);
+                if (!ok) break;
+                mbar_expect_tx(full0 + 8 * stage, (uint32_t)stage_bytes);
+                tma_load_2d(stage_at(stage), &map_w, ks * kBK, tile * 128, full0 + 8 * stage);
+                tma_load_2d(stage_at(stage) + kStripStageW, &map_x, ks * kBK, m0, full0 + 8 * stage);
+                if (++stage == q.stages) { stage = 0; wraps++; }
+            }
+            if (!ok) { atomicCAS(a.status, 0, FQ_ERR_TIMEOUT); *abort_flag = 1; }
+        }
+    } else if (warp == 1) {
+        // ================================================================== MMA issuer
+        const uint32_t idesc = umma_idesc_i8(128, q.nt);
+        const uint64_t adesc0 = umma_desc_sw128(g_smem_u32(smem)), bdesc0 = umma_desc_sw128(g_smem_u32(smem) + kStripStageW);
+        int stage = 0;
+        uint32_t wraps = 0;
+        bool ok = true;
+        for (int ks = k0; ks < k1; ks++) {
+            ok = __all_sync(0xffffffffu, g_wait(full0 + 8 * stage, wraps & 1u, abort_flag));
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint64_t step = (uint64_t)((uint32_t)(stage * stage_bytes) >> 4);
+            const uint32_t more = ks > k0 ? 1u : 0u;
+            if (elect_one()) {
+#pragma unroll
+                for (int kk = 0; kk < kBK / 32; kk++)
+                    asm volatile(
+                        "{\n\t.reg .pred p;\n\t"
+                        "setp.ne.b32 p, %4, 0;\n\t"
+                        "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                        ::"r"(tmem_base), "l"(adesc0 + step + (uint64_t)(kk * 2)), "l"(bdesc0 + step + (uint64_t)(kk * 2)), "r"(idesc),
+                          "r"(kk > 0 ? 1u : more) : "memory");
+                umma_commit(empty0 + 8 * stage);
+            }
+            __syncwarp();
+            if (++stage == q.stages) { stage = 0; wraps++; }
+        }
+        if (ok && elect_one()) umma_commit(done);
+        __syncwarp();
+        if (!ok && lane == 0) { atomicCAS(a.status, 0, FQ_ERR_TIMEOUT); *abort_flag = 1; }
+    } else {
+        // ================================================================== epilogue (warps 2..5)
+        const int quarter = warp & 3, row = quarter * 32 + lane, n = tile * 128 + row;      // output
+        const bool ok = __all_sync(0xffffffffu, g_wait<64>(done, 0, abort_flag));
+        if (ok) {
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const float sw = n < a.N ? a.sw[n] : 0.0f;
+            if (q.early) asm volatile("griddepcontrol.wait;" ::: "memory");                 // the tokens' scales
+            int* part = reinterpret_cast<int*>(smem);                                        // [token][128]; every copy and every MMA is done
+#pragma unroll 1
+            for (int t0 = 0; t0 < q.nt; t0 += 16) {
+                uint32_t v[16];
+                tmem_ld16(v, tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)t0);
+#pragma unroll
+                for (int t = 0; t < 16; t++) {
+                    if (q.splits > 1) {
+                        part[(t0 + t) * 128 + row] = (int)v[t];
+                    } else if (n < a.N && m0 + t0 + t < a.M) {
+                        static_cast<T*>(a.y)[(long long)(m0 + t0 + t) * a.ldy + n] = Group<T>::from_f((float)(int)v[t] * a.sx[m0 + t0 + t] * sw);
+                    }
+                }
+            }
+        } else if (lane == 0) {
+            atomicCAS(a.status, 0, FQ_ERR_TIMEOUT);
+            *abort_flag = 1;
+        }
+    }
+    if (q.splits > 1) {
+        cluster_arrive();
+        cluster_wait();                  // all CTAs' sums are in their shared memory
+        if (warp >= 2) {
+            const int row = (warp & 3) * 32 + lane, n = tile * 128 + row;
+            const uint32_t at = g_smem_u32(smem) + (uint32_t)row * 4;
+            const float sw = n < a.N ? a.sw[n] : 0.0f;
+            const int end = a.M - m0 < q.nt ? a.M - m0 : q.nt;
+            for (int t = rank; t < end; t += q.splits) {
+                int sum = 0;
+#pragma unroll 8
+                for (int c = 0; c < q.splits; c++) sum += cluster_ld_s32(cluster_map(at, (uint32_t)c) + (uint32_t)t * 512);
+                if (n < a.N) static_cast<T*>(a.y)[(long long)(m0 + t) * a.ldy + n] = Group<T>::from_f((float)sum * a.sx[m0 + t] * sw);
+            }
+        }
+        cluster_arrive();
+        cluster_wait();                  // nobody's shared memory is read any more
+    }
+    // every path ends here.  After a wait that ran out, copies may still be on their way into shared memory.
+    __syncthreads();
+    if (*abort_flag) let_copies_land();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "n"(kStripTmemCols) : "memory");
+    }
+}
+
 // ------------------------------------------------------------------------------- host side
+struct StripPlan { int nt, blocks, splits, stages; size_t smem; };
+StripPlan strip_plan(const Ctx* ctx, int M, int N, int K)
+{
+    StripPlan p{};
+    p.blocks = (M + kStripTokens - 1) / kStripTokens;
+    p.nt = ((M + p.blocks - 1) / p.blocks + 15) / 16 * 16;
+    const int tiles = (N + 127) / 128 * p.blocks, k_steps = (K + kBK - 1) / kBK, stage = kStripStageW + p.nt * kBK;
+    p.splits = 1;
+    int most = 3 * ctx->sm_count, per = 2;
+    if (const char* e = getenv("I8MOST")) most = atoi(e);
+    if (const char* e = getenv("I8PER")) per = atoi(e);
+    while (p.splits < 8 && tiles * p.splits * 2 <= most && k_steps >= 4 * p.splits) p.splits *= 2;
+    const int room = (per == 1 ? 220 : per == 2 ? 110 : 72) * 1024 - 1024 - strip_bars_bytes();
+    p.stages = room / stage;
+    if (p.stages > kStripMaxStages) p.stages = kStripMaxStages;
+    p.smem = (size_t)p.stages * stage + strip_bars_bytes() + 1024;
+    return p;
+}
+
+template <class T>
+int launch_strip(const Ctx* ctx, const int8_t* xc, long long ldx, const int8_t* wc, long long ldw, const I8Args& a, bool early, cudaStream_t st)
+{
+    static std::atomic<bool> ready[64];
+    if (ctx->device >= 64) return FQ_ERR_ARG;
+    if (!ready[ctx->device].load(std::memory_order_acquire)) {
+        FQ_CUDA_OK(cudaFuncSetAttribute(gemm_i8_strip_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024));
+        ready[ctx->device].store(true, std::memory_order_release);
+    }
+    const StripPlan p = strip_plan(ctx, a.M, a.N, a.K);
+    CUtensorMap map_x, map_w;
+    int rc = make_map_i8(&map_x, xc, a.M, a.K, ldx, p.nt);
+    if (rc != FQ_OK) return rc;
+    rc = make_map_i8(&map_w, wc, a.N, a.K, ldw, 128);
+    if (rc != FQ_OK) return rc;
+    const StripArgs q{a, p.nt, p.stages, p.splits, early};
+    cudaLaunchAttribute attr[2]{};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)p.splits; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)((a.N + 127) / 128 * p.splits), (unsigned)p.blocks); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = p.smem;
+    cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = early ? 2 : 1;
+    FQ_CUDA_OK(cudaLaunchKernelEx(&cfg, gemm_i8_strip_kernel<T>, map_x, map_w, q));
+    return FQ_OK;
+}
+
 // Outputs per tile: the width for which the last wave leaves the least idle (the time of a wave goes with the width, plus
 // something for a tile's ends).
 int pair_tile_n(int M, int n_out, int pairs)
@@ -306,8 +545,16 @@ int check_codes(const int8_t* xc, const float* sx, int k_in, long long ldx)
     return FQ_OK;
 }
 
-int launch_any(const Ctx* ctx, const int8_t* xc, long long ldx, const int8_t* wc, long long ldw, int y_dtype, const I8Args& a, cudaStream_t st)
+int launch_any(const Ctx* ctx, const int8_t* xc, long long ldx, const int8_t* wc, long long ldw, int y_dtype, const I8Args& a, bool early,
+               cudaStream_t st)
 {
+    int lim = kStripTokens;
+    if (const char* e = getenv("I8LIM")) lim = atoi(e);
+    if (a.M <= lim) {
+        if (y_dtype == FQ_DT_F32) return launch_strip<float>(ctx, xc, ldx, wc, ldw, a, early, st);
+        if (y_dtype == FQ_DT_F16) return launch_strip<__half>(ctx, xc, ldx, wc, ldw, a, early, st);
+        return launch_strip<__nv_bfloat16>(ctx, xc, ldx, wc, ldw, a, early, st);
+    }
     if (y_dtype == FQ_DT_F32) return launch_pair<float>(ctx, xc, ldx, wc, ldw, a, st);
     if (y_dtype == FQ_DT_F16) return launch_pair<__half>(ctx, xc, ldx, wc, ldw, a, st);
     return launch_pair<__nv_bfloat16>(ctx, xc, ldx, wc, ldw, a, st);
@@ -328,8 +575,11 @@ int fq_gemm_i8(fq_ctx* ctx, const int8_t* x_codes_dev, const float* x_scales_dev
     if (rc != FQ_OK) return rc;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
+    if (gemv_i8_takes(M, k_in))
+        return launch_gemv_i8(ctx, x_codes_dev, -1, ldx, x_scales_dev, M, w_codes_dev, w_scales_dev, n_out, k_in, ldw, Y_dev, y_dtype, ldy,
+                              (cudaStream_t)stream);
     const I8Args a{x_scales_dev, w_scales_dev, Y_dev, M, n_out, k_in, ldy, 0, ctx->status_dev};
-    return launch_any(ctx, x_codes_dev, ldx, w_codes_dev, ldw, y_dtype, a, (cudaStream_t)stream);
+    return launch_any(ctx, x_codes_dev, ldx, w_codes_dev, ldw, y_dtype, a, false, (cudaStream_t)stream);
 }
 
 int fq_linear_i8(fq_ctx* ctx, const void* X_dev, int x_dtype, int M, long long ldx, const int8_t* w_codes_dev, const float* w_scales_dev,
@@ -346,10 +596,12 @@ int fq_linear_i8(fq_ctx* ctx, const void* X_dev, int x_dtype, int M, long long l
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
     const cudaStream_t st = (cudaStream_t)stream;
+    if (gemv_i8_takes(M, k_in))
+        return launch_gemv_i8(ctx, X_dev, x_dtype, ldx, nullptr, M, w_codes_dev, w_scales_dev, n_out, k_in, ldw, Y_dev, y_dtype, ldy, st);
     rc = launch_quantize_rows(X_dev, x_dtype, M, k_in, ldx, codes_dev, ldc, scales_dev, st);
     if (rc != FQ_OK) return rc;
     const I8Args a{scales_dev, w_scales_dev, Y_dev, M, n_out, k_in, ldy, 0, ctx->status_dev};
-    return launch_any(ctx, codes_dev, ldc, w_codes_dev, ldw, y_dtype, a, st);
+    return launch_any(ctx, codes_dev, ldc, w_codes_dev, ldw, y_dtype, a, true, st);
 }
 
 }  // extern "C"

@@ -131,6 +131,9 @@ __device__ __forceinline__ float warp_max_nan(float v)
     return v;
 }
 
+// The code of x in a row whose largest absolute value is a, from the quotient in 64 bits.
+static __device__ __noinline__ int exact_code(float x, float a) { return __double2int_rn(127.0 * (double)x / (double)a); }
+
 // Codes of a row whose largest absolute value is `a` (fq_quant_rows.cu says how).
 struct RowScale {
     float a, r, scale;
@@ -145,10 +148,10 @@ struct RowScale {
     }
     __device__ __forceinline__ int code(float x) const
     {
-        if (!fine) return a > 0.0f ? __double2int_rn(127.0 * (double)x / (double)a) : 0;
+        if (!fine) return a > 0.0f ? exact_code(x, a) : 0;
         if (r == 0.0f) return 0;                                 // (0 * inf is NaN)
         const float t = x * r, q = rintf(t);
-        if (fabsf(fabsf(t - q) - 0.5f) < 3.2e-5f) return __double2int_rn(127.0 * (double)x / (double)a);
+        if (fabsf(fabsf(t - q) - 0.5f) < 3.2e-5f) return exact_code(x, a);
         return (int)q;
     }
 };
