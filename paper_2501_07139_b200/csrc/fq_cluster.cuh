@@ -40,6 +40,12 @@ __device__ __forceinline__ int cluster_ld_s32(uint32_t addr)
     asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
     return v;
 }
+__device__ __forceinline__ int4 cluster_ld_s32x4(uint32_t addr)
+{
+    int4 v;
+    asm volatile("ld.shared::cluster.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
 __device__ __forceinline__ unsigned long long cluster_ld_u64(uint32_t addr)
 {
     unsigned long long v;

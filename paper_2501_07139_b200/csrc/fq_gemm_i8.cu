@@ -7,8 +7,8 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
+#include <algorithm>
 #include <atomic>
-#include <cstdlib>
 
 #include "fq_cluster.cuh"
 #include "fq_internal.cuh"
@@ -98,6 +98,24 @@ __device__ __forceinline__ void store_outputs(T* dst, const float (&f)[32], int 
 #pragma unroll
         for (int e = 0; e < 32; e++)
             if (e < n) dst[e] = Group<T>::from_f(f[e]);
+    }
+}
+
+// Four neighbouring outputs, dst aligned to four of them.
+template <class T>
+__device__ __forceinline__ void store_four(T* dst, const float (&f)[4], int n)
+{
+    if (n >= 4) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<float4*>(dst) = make_float4(f[0], f[1], f[2], f[3]);
+        } else {
+            T h[4] = {Group<T>::from_f(f[0]), Group<T>::from_f(f[1]), Group<T>::from_f(f[2]), Group<T>::from_f(f[3])};
+            *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(h);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            if (i < n) dst[i] = Group<T>::from_f(f[i]);
     }
 }
 
@@ -268,7 +286,7 @@ gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
 constexpr int kStripTokens = 128;
 constexpr int kStripTmemCols = 128;
 constexpr int kStripStageW = 128 * kBK;                  // 16 KB
-constexpr int kStripMaxStages = 12;
+constexpr int kStripMaxStages = 12, kMaxSplits = 8;
 
 struct StripArgs {
     I8Args a;
@@ -404,15 +422,26 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_strip_kernel(const __grid_co
         cluster_arrive();
         cluster_wait();                  // all CTAs' sums are in their shared memory
         if (warp >= 2) {
-            const int row = (warp & 3) * 32 + lane, n = tile * 128 + row;
-            const uint32_t at = g_smem_u32(smem) + (uint32_t)row * 4;
-            const float sw = n < a.N ? a.sw[n] : 0.0f;
-            const int end = a.M - m0 < q.nt ? a.M - m0 : q.nt;
-            for (int t = rank; t < end; t += q.splits) {
-                int sum = 0;
-#pragma unroll 8
-                for (int c = 0; c < q.splits; c++) sum += cluster_ld_s32(cluster_map(at, (uint32_t)c) + (uint32_t)t * 512);
-                if (n < a.N) static_cast<T*>(a.y)[(long long)(m0 + t) * a.ldy + n] = Group<T>::from_f((float)sum * a.sx[m0 + t] * sw);
+            // a warp takes a token, a lane four of its outputs
+            const int n = tile * 128 + 4 * lane, end = a.M - m0 < q.nt ? a.M - m0 : q.nt;
+            float sw[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) sw[i] = n + i < a.N ? a.sw[n + i] : 0.0f;
+            const uint32_t at = g_smem_u32(smem) + (uint32_t)lane * 16;
+            for (int t = rank + q.splits * (warp - 2); t < end; t += q.splits * 4) {
+                int4 v[kMaxSplits];
+#pragma unroll
+                for (int c = 0; c < kMaxSplits; c++) {
+                    v[c] = make_int4(0, 0, 0, 0);
+                    if (c < q.splits) v[c] = cluster_ld_s32x4(cluster_map(at, (uint32_t)c) + (uint32_t)t * 512);
+                }
+#pragma unroll
+                for (int c = 1; c < kMaxSplits; c++) {
+                    v[0].x += v[c].x; v[0].y += v[c].y; v[0].z += v[c].z; v[0].w += v[c].w;
+                }
+                const float sx = a.sx[m0 + t];
+                const float f[4] = {(float)v[0].x * sx * sw[0], (float)v[0].y * sx * sw[1], (float)v[0].z * sx * sw[2], (float)v[0].w * sx * sw[3]};
+                store_four(static_cast<T*>(a.y) + (long long)(m0 + t) * a.ldy + n, f, a.N - n);
             }
         }
         cluster_arrive();
@@ -430,6 +459,7 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_strip_kernel(const __grid_co
 }
 
 // ------------------------------------------------------------------------------- host side
+// K is split until there are two to three CTAs for every SM, which then share its memory: one waits, adds up or writes while others read.
 struct StripPlan { int nt, blocks, splits, stages; size_t smem; };
 StripPlan strip_plan(const Ctx* ctx, int M, int N, int K)
 {
@@ -438,15 +468,20 @@ StripPlan strip_plan(const Ctx* ctx, int M, int N, int K)
     p.nt = ((M + p.blocks - 1) / p.blocks + 15) / 16 * 16;
     const int tiles = (N + 127) / 128 * p.blocks, k_steps = (K + kBK - 1) / kBK, stage = kStripStageW + p.nt * kBK;
     p.splits = 1;
-    int most = 3 * ctx->sm_count, per = 2;
-    if (const char* e = getenv("I8MOST")) most = atoi(e);
-    if (const char* e = getenv("I8PER")) per = atoi(e);
-    while (p.splits < 8 && tiles * p.splits * 2 <= most && k_steps >= 4 * p.splits) p.splits *= 2;
+    while (p.splits < kMaxSplits && tiles * p.splits * 2 <= 3 * ctx->sm_count && k_steps >= 4 * p.splits) p.splits *= 2;
+    const int per = std::min(3, (tiles * p.splits + ctx->sm_count - 1) / ctx->sm_count);
     const int room = (per == 1 ? 220 : per == 2 ? 110 : 72) * 1024 - 1024 - strip_bars_bytes();
     p.stages = room / stage;
     if (p.stages > kStripMaxStages) p.stages = kStripMaxStages;
     p.smem = (size_t)p.stages * stage + strip_bars_bytes() + 1024;
     return p;
+}
+
+// Strips up to 128 tokens, and up to 256 where the pairs' tiles, one row of them, would leave many SMs idle (256 tokens, 4096 x 11008: 21 us
+// against 27 us; 11008 x 4096: 26 us against 19 us).
+bool takes_strips(const Ctx* ctx, int M, int N)
+{
+    return M <= kStripTokens || (M <= 2 * kStripTokens && (N + 127) / 128 * 10 <= ctx->sm_count / 2 * 6);
 }
 
 template <class T>
@@ -548,9 +583,7 @@ int check_codes(const int8_t* xc, const float* sx, int k_in, long long ldx)
 int launch_any(const Ctx* ctx, const int8_t* xc, long long ldx, const int8_t* wc, long long ldw, int y_dtype, const I8Args& a, bool early,
                cudaStream_t st)
 {
-    int lim = kStripTokens;
-    if (const char* e = getenv("I8LIM")) lim = atoi(e);
-    if (a.M <= lim) {
+    if (takes_strips(ctx, a.M, a.N)) {
         if (y_dtype == FQ_DT_F32) return launch_strip<float>(ctx, xc, ldx, wc, ldw, a, early, st);
         if (y_dtype == FQ_DT_F16) return launch_strip<__half>(ctx, xc, ldx, wc, ldw, a, early, st);
         return launch_strip<__nv_bfloat16>(ctx, xc, ldx, wc, ldw, a, early, st);
@@ -576,7 +609,7 @@ int fq_gemm_i8(fq_ctx* ctx, const int8_t* x_codes_dev, const float* x_scales_dev
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
     if (gemv_i8_takes(M, k_in))
-        return launch_gemv_i8(ctx, x_codes_dev, -1, ldx, x_scales_dev, M, w_codes_dev, w_scales_dev, n_out, k_in, ldw, Y_dev, y_dtype, ldy,
+        return launch_gemv_i8(ctx, x_codes_dev, -1, ldx, x_scales_dev, M, w_codes_dev, w_scales_dev, n_out, k_in, ldw, Y_dev, y_dtype, ldy, false,
                               (cudaStream_t)stream);
     const I8Args a{x_scales_dev, w_scales_dev, Y_dev, M, n_out, k_in, ldy, 0, ctx->status_dev};
     return launch_any(ctx, x_codes_dev, ldx, w_codes_dev, ldw, y_dtype, a, false, (cudaStream_t)stream);
@@ -596,10 +629,12 @@ int fq_linear_i8(fq_ctx* ctx, const void* X_dev, int x_dtype, int M, long long l
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
     const cudaStream_t st = (cudaStream_t)stream;
-    if (gemv_i8_takes(M, k_in))
-        return launch_gemv_i8(ctx, X_dev, x_dtype, ldx, nullptr, M, w_codes_dev, w_scales_dev, n_out, k_in, ldw, Y_dev, y_dtype, ldy, st);
-    rc = launch_quantize_rows(X_dev, x_dtype, M, k_in, ldx, codes_dev, ldc, scales_dev, st);
+    if (gemv_i8_takes(M, k_in) && gemv_i8_quantises(M, k_in))
+        return launch_gemv_i8(ctx, X_dev, x_dtype, ldx, nullptr, M, w_codes_dev, w_scales_dev, n_out, k_in, ldw, Y_dev, y_dtype, ldy, false, st);
+    rc = launch_quantize_rows(X_dev, x_dtype, M, k_in, ldx, codes_dev, ldc, scales_dev, ctx->sm_count, st);
     if (rc != FQ_OK) return rc;
+    if (gemv_i8_takes(M, k_in))
+        return launch_gemv_i8(ctx, codes_dev, -1, ldc, scales_dev, M, w_codes_dev, w_scales_dev, n_out, k_in, ldw, Y_dev, y_dtype, ldy, true, st);
     const I8Args a{scales_dev, w_scales_dev, Y_dev, M, n_out, k_in, ldy, 0, ctx->status_dev};
     return launch_any(ctx, codes_dev, ldc, w_codes_dev, ldw, y_dtype, a, true, st);
 }

@@ -210,12 +210,14 @@ struct CtaWork {
 
 // 8-bit layers
 int launch_quantize_rows(const void* x, int dtype, int rows, int cols, long long ldx, int8_t* codes, long long ldc, float* scales,
-                         cudaStream_t st);
+                         int sm_count, cudaStream_t st);
 
 // a few tokens, given as activations (x_dtype: FQ_DT_*) or as codes with their scales (x_dtype -1)
+//   early: the kernel before writes the codes and their scales, and nothing else that is read here
 bool gemv_i8_takes(int M, int k_in);
+bool gemv_i8_quantises(int M, int k_in);       // as activations
 int launch_gemv_i8(const Ctx* ctx, const void* x, int x_dtype, long long ldx, const float* sx, int M, const int8_t* w, const float* sw, int n_out,
-                   int k_in, long long ldw, void* y, int y_dtype, long long ldy, cudaStream_t st);
+                   int k_in, long long ldw, void* y, int y_dtype, long long ldy, bool early, cudaStream_t st);
 
 int launch_gemm(Ctx* ctx, const void* store, int blob_stride, const FieldList& fl, int zero_adjust, int n_out, int k_in,
                 const uint16_t* X, int M, int ldx, uint16_t* Y, int ldy, void* w_scratch, cudaStream_t st);

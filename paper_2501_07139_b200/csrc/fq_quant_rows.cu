@@ -1,9 +1,8 @@
 // Symmetric 8-bit quantiser of matrix rows:  a = max |x|,  scale = a / 127,  code = rint(127 x / a), ties to even.
 //
 // A code is that of the exact quotient: in fp32 alone a value next to the border between two codes could fall on either side, and
-// 127 x / a does meet borders (x = a / 2 is 63.5).  t = x * fp32(127 / a) is off by at most 127 * 2^-23; only where t is
-// closer than that to a border, one value in some ten thousand, the quotient is taken in 64 bits, where operands of 24 bits keep
-// every quotient that is not on the border off it.
+// 127 x / a does meet borders (x = a / 2 is 63.5; among 4096 bf16 values some seven are).  x times a little inexact 127 / a is off by at most
+// 3.1e-5; where it is closer than 5e-5 to a border, the side is settled by the exact sign of 127 x - border a.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -13,7 +12,6 @@
 namespace fq {
 namespace {
 
-constexpr int kQuantThreads = 256;
 
 struct QuantArgs {
     const void* x;
@@ -24,107 +22,123 @@ struct QuantArgs {
     float* scales;
 };
 
+// (`red` is free again after the CTA's next barrier.)
+template <int THREADS>
 __device__ __forceinline__ float block_max(float m, float* red)
 {
+    constexpr int W = THREADS / 32;
     m = warp_max_nan(m);
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = m;
     __syncthreads();
-    m = red[0];
+    m = red[threadIdx.x & (W - 1)];
 #pragma unroll
-    for (int w = 1; w < kQuantThreads / 32; w++) m = max_nan(m, red[w]);
+    for (int o = 1; o < W; o <<= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
     return m;
 }
 
 // Rows of any length and alignment: read twice, the second time from the caches.
-template <class T>
-__global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const QuantArgs a)
+template <class T, int THREADS>
+__global__ void __launch_bounds__(THREADS) quantize_rows_kernel(const QuantArgs a)
 {
-    __shared__ float red[kQuantThreads / 32];
+    __shared__ float red[THREADS / 32];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");    // (whoever reads the codes waits for the end of this kernel)
     const long long r = blockIdx.x;
     const T* x = static_cast<const T*>(a.x) + r * a.ldx;
     float m = 0.0f;
-    for (int c = threadIdx.x; c < a.cols; c += kQuantThreads) m = max_nan(m, fabsf(Group<T>::to_f(x[c])));
-    const RowScale s(block_max(m, red));
+    for (int c = threadIdx.x; c < a.cols; c += THREADS) m = max_nan(m, fabsf(Group<T>::to_f(x[c])));
+    m = block_max<THREADS>(m, red);
+    const RowScale s(m);
     int8_t* q = a.codes + r * a.ldc;
-    for (int c = threadIdx.x; c < a.cols; c += kQuantThreads) q[c] = (int8_t)s.code(Group<T>::to_f(x[c]));
-    if (threadIdx.x == 0) a.scales[r] = s.scale;
+    for (int c = threadIdx.x; c < a.cols; c += THREADS) q[c] = s.one(Group<T>::to_f(x[c]));
+    if (threadIdx.x == 0) a.scales[r] = RowScale::scale(m);
 }
 
 // Rows that stay in registers, U pieces of 8 values to a thread: pieces are 16-byte aligned on both sides, and there is a whole number of them.
-template <class T, int U>
-__global__ void __launch_bounds__(kQuantThreads) quantize_rows_kept_kernel(const QuantArgs a)
+// A CTA goes from row to row, the next one on its way while one is worked on.  (8192 x 4096 bf16: 39 us with a CTA for every row.)
+template <class T, int THREADS, int U>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) quantize_rows_kept_kernel(const QuantArgs a)
 {
-    __shared__ float red[kQuantThreads / 32];
+    __shared__ float red[2][THREADS / 32];
     constexpr int G = 8 / Group<T>::N;                   // 16-byte groups of a piece
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const long long r = blockIdx.x;
-    const T* x = static_cast<const T*>(a.x) + r * a.ldx;
     const int pieces = a.cols / 8;
-    uint4 v[U][G];
+    const auto load = [&](uint4 (&v)[U][G], int r) {
+        const T* x = static_cast<const T*>(a.x) + (long long)r * a.ldx;
 #pragma unroll
-    for (int u = 0; u < U; u++)
+        for (int u = 0; u < U; u++)
 #pragma unroll
-        for (int g = 0; g < G; g++) {
-            v[u][g] = make_uint4(0u, 0u, 0u, 0u);
-            const int p = u * kQuantThreads + threadIdx.x;
-            if (p < pieces) v[u][g] = *reinterpret_cast<const uint4*>(x + p * 8 + g * Group<T>::N);
-        }
-    float m = 0.0f;
-#pragma unroll
-    for (int u = 0; u < U; u++)
-#pragma unroll
-        for (int g = 0; g < G; g++) {
-            float2 f[Group<T>::N / 2];
-            Group<T>::unpack(v[u][g], f);
-#pragma unroll
-            for (int i = 0; i < Group<T>::N / 2; i++) m = max_nan(m, max_nan(fabsf(f[i].x), fabsf(f[i].y)));
-        }
-    const RowScale s(block_max(m, red));
-    int8_t* q = a.codes + r * a.ldc;
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-        const int p = u * kQuantThreads + threadIdx.x;
-        if (p >= pieces) break;
-        uint32_t w[2];
-#pragma unroll
-        for (int g = 0; g < G; g++) {
-            float2 f[Group<T>::N / 2];
-            Group<T>::unpack(v[u][g], f);
-#pragma unroll
-            for (int i = 0; i < Group<T>::N / 4; i++) {
-                const uint32_t c0 = (uint32_t)s.code(f[2 * i].x) & 255u, c1 = (uint32_t)s.code(f[2 * i].y) & 255u;
-                const uint32_t c2 = (uint32_t)s.code(f[2 * i + 1].x) & 255u, c3 = (uint32_t)s.code(f[2 * i + 1].y) & 255u;
-                w[g * (Group<T>::N / 4) + i] = c0 | c1 << 8 | c2 << 16 | c3 << 24;
+            for (int g = 0; g < G; g++) {
+                v[u][g] = make_uint4(0u, 0u, 0u, 0u);
+                const int p = u * THREADS + threadIdx.x;
+                if (p < pieces && r < a.rows) v[u][g] = *reinterpret_cast<const uint4*>(x + p * 8 + g * Group<T>::N);
             }
+    };
+    uint4 v[U][G];
+    load(v, (int)blockIdx.x);
+    int turn = 0;
+    for (int r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
+        uint4 next[U][G];
+        load(next, r + (int)gridDim.x);
+        typename Group<T>::Max most = Group<T>::nothing();
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int g = 0; g < G; g++) Group<T>::take_abs(most, v[u][g]);
+        const float m = block_max<THREADS>(Group<T>::of_abs(most), red[turn]);
+        const RowScale s(m);
+        int8_t* q = a.codes + (long long)r * a.ldc;
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int p = u * THREADS + threadIdx.x;
+            uint32_t w[2];
+#pragma unroll
+            for (int g = 0; g < G; g++) {
+                float2 f[Group<T>::N / 2];
+                Group<T>::unpack(v[u][g], f);
+#pragma unroll
+                for (int i = 0; i < Group<T>::N / 4; i++)
+                    w[g * (Group<T>::N / 4) + i] = s.four(f[2 * i], f[2 * i + 1]);
+            }
+            if (p < pieces) *reinterpret_cast<uint2*>(q + p * 8) = make_uint2(w[0], w[1]);
         }
-        *reinterpret_cast<uint2*>(q + p * 8) = make_uint2(w[0], w[1]);
+        if (threadIdx.x == 0) a.scales[r] = RowScale::scale(m);
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int g = 0; g < G; g++) v[u][g] = next[u][g];
     }
-    if (threadIdx.x == 0) a.scales[r] = s.scale;
 }
 
-template <class T>
-void launch_typed(const QuantArgs& a, cudaStream_t st)
+template <class T, int THREADS>
+int launch_threads(const QuantArgs& a, int sm_count, cudaStream_t st)
 {
-    const int per_thread = (a.cols / 8 + kQuantThreads - 1) / kQuantThreads;
+    const int per_thread = (a.cols / 8 + THREADS - 1) / THREADS, grid = a.rows < sm_count * (1024 / THREADS) ? a.rows : sm_count * (1024 / THREADS);
     const bool pieces = a.cols % 8 == 0 && aligned(a.x, 16) && a.ldx * sizeof(T) % 16 == 0 && aligned(a.codes, 8) && a.ldc % 8 == 0;
-    if (pieces && per_thread <= 1) quantize_rows_kept_kernel<T, 1><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a);
-    else if (pieces && per_thread <= 2) quantize_rows_kept_kernel<T, 2><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a);
-    else if (pieces && per_thread <= 4) quantize_rows_kept_kernel<T, 4><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a);
-    else if (pieces && per_thread <= 8) quantize_rows_kept_kernel<T, 8><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a);
-    else quantize_rows_kernel<T><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a);
+    if (pieces && per_thread <= 1) quantize_rows_kept_kernel<T, THREADS, 1><<<(unsigned)grid, THREADS, 0, st>>>(a);
+    else if (pieces && per_thread <= 2) quantize_rows_kept_kernel<T, THREADS, 2><<<(unsigned)grid, THREADS, 0, st>>>(a);
+    else quantize_rows_kernel<T, THREADS><<<(unsigned)a.rows, THREADS, 0, st>>>(a);
+    return cudaGetLastError() == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
+}
+
+// A thread has one or two pieces of a row: few rows get more threads each, many of them only as many as it takes.
+template <class T>
+int launch_typed(const QuantArgs& a, int sm_count, cudaStream_t st)
+{
+    if (a.cols > 8192 || (a.cols > 2048 && a.rows <= sm_count)) return launch_threads<T, 1024>(a, sm_count, st);
+    if (a.cols > 4096) return launch_threads<T, 512>(a, sm_count, st);
+    if (a.cols > 2048) return launch_threads<T, 256>(a, sm_count, st);
+    return launch_threads<T, 128>(a, sm_count, st);
 }
 
 }  // namespace
 
 int launch_quantize_rows(const void* x, int dtype, int rows, int cols, long long ldx, int8_t* codes, long long ldc, float* scales,
-                         cudaStream_t st)
+                         int sm_count, cudaStream_t st)
 {
     const QuantArgs a{x, ldx, rows, cols, codes, ldc, scales};
-    if (dtype == FQ_DT_F32) launch_typed<float>(a, st);
-    else if (dtype == FQ_DT_F16) launch_typed<__half>(a, st);
-    else launch_typed<__nv_bfloat16>(a, st);
-    return cudaGetLastError() == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
+    if (dtype == FQ_DT_F32) return launch_typed<float>(a, sm_count, st);
+    if (dtype == FQ_DT_F16) return launch_typed<__half>(a, sm_count, st);
+    return launch_typed<__nv_bfloat16>(a, sm_count, st);
 }
 
 }  // namespace fq
@@ -140,5 +154,5 @@ extern "C" int fq_quantize_rows(fq_ctx* ctx, const void* x_dev, int dtype, int r
     if (!aligned(x_dev, (size_t)size) || !aligned(scales_dev, 4)) return FQ_ERR_ALIGN;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
-    return launch_quantize_rows(x_dev, dtype, rows, cols, ldx, codes_dev, ldc, scales_dev, (cudaStream_t)stream);
+    return launch_quantize_rows(x_dev, dtype, rows, cols, ldx, codes_dev, ldc, scales_dev, ctx->sm_count, (cudaStream_t)stream);
 }
