@@ -19,6 +19,7 @@ FQ_DT_BF16 = 1
 FQ_DT_F32 = 2
 FQ_MAX_TOP = 128
 FQ_MAX_VOCAB = 393216
+_I8, _F32, _I32, _IDS = (torch.int8,), (torch.float32,), (torch.int32,), (torch.int32, torch.int64)
 _TYPES = {torch.float16: FQ_DT_F16, torch.bfloat16: FQ_DT_BF16, torch.float32: FQ_DT_F32}
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -157,11 +158,6 @@ def _stream_on(device: torch.device) -> int:
     if _raw_stream and torch.cuda.is_initialized():
         return _raw_stream(device.index)
     return torch.cuda.current_stream(device).cuda_stream
-
-
-def _pitch(t: torch.Tensor, rows: int, cols: int) -> int:
-    """Elements from one row to the next (of one row: any that the library takes)."""
-    return t.stride(0) if rows > 1 else -(-cols // 16) * 16
 
 
 def _check(rc: int, where: str) -> int:
@@ -397,139 +393,136 @@ class FlexQ:
 
     # -- 8-bit layers ------------------------------------------------------------------------
     def _matrix(self, t: torch.Tensor, name: str, types) -> tuple:
-        if t.dim() != 2 or t.dtype not in types or t.device != self.device or (t.stride(1) != 1 and t.shape[1] > 1):
+        """(rows, columns, elements from one row to the next; of one row, any that the library takes)"""
+        shape, st = t.shape, t.stride()
+        if len(shape) != 2 or t.dtype not in types or t.device != self.device or (st[1] != 1 and shape[1] > 1):
             raise ValueError(f"{name}: a matrix of {', '.join(str(d) for d in types)} on {self.device} with dense rows is needed, not "
-                             f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
-        return t.shape
+                             f"{t.dtype} {tuple(shape)} with strides {st} on {t.device}")
+        rows, cols = shape
+        return rows, cols, st[0] if rows > 1 else -(-cols // 16) * 16
 
-    def _vector(self, t: torch.Tensor, name: str, types, n: int) -> torch.Tensor:
-        if t.dim() != 1 or t.shape[0] != n or t.dtype not in types or t.device != self.device or not t.is_contiguous():
-            raise ValueError(f"{name}: {n} dense values of {', '.join(str(d) for d in types)} on {self.device} are needed, not "
+    def _dense(self, t: torch.Tensor, name: str, types, shape: tuple) -> torch.Tensor:
+        if t.shape != shape or t.dtype not in types or t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"{name}: dense {shape} values of {', '.join(str(d) for d in types)} on {self.device} are needed, not "
                              f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
         return t
 
-    def _dense(self, t: torch.Tensor, name: str, types, shape) -> torch.Tensor:
-        if tuple(t.shape) != shape or t.dtype not in types or t.device != self.device or not t.is_contiguous():
-            raise ValueError(f"{name}: a dense {shape} matrix of {', '.join(str(d) for d in types)} on {self.device} is needed, not "
-                             f"{t.dtype} {tuple(t.shape)} on {t.device}")
-        return t
-
-    def _new_codes(self, rows: int, cols: int) -> torch.Tensor:
-        return torch.empty((rows, -(-cols // 16) * 16), dtype=torch.int8, device=self.device)[:, :cols]
+    def _codes_and_scales(self, codes, scales, rows, cols):
+        """Given or new ones: codes, their pitch, scales.  New codes get a row pitch that fq_gemm_i8 takes (a multiple of 16)."""
+        if codes is None:
+            pitch = -(-cols // 16) * 16
+            codes = torch.empty((rows, pitch), dtype=torch.int8, device=self.device)
+            if pitch != cols:
+                codes = codes[:, :cols]
+        else:
+            r, c, pitch = self._matrix(codes, "codes", _I8)
+            if r != rows or c != cols:
+                raise ValueError(f"codes: {rows} x {cols} are needed, not {r} x {c}")
+        if scales is None:
+            scales = torch.empty(rows, dtype=torch.float32, device=self.device)
+        else:
+            self._dense(scales, "scales", _F32, (rows,))
+        return codes, pitch, scales
 
     def fq_quantize_rows(self, x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None):
         """Rows of x (tokens, or the channels of a weight matrix) -> (int8 codes, fp32 scale per row).  New codes get a row pitch
         that fq_gemm_i8 takes (a multiple of 16)."""
-        rows, cols = self._matrix(x, "x", _TYPES)
-        if codes is None:
-            codes = self._new_codes(rows, cols)
-        elif self._matrix(codes, "codes", (torch.int8,)) != x.shape:
-            raise ValueError("codes: another shape than x")
-        if scales is None:
-            scales = torch.empty(rows, dtype=torch.float32, device=self.device)
-        self._vector(scales, "scales", (torch.float32,), rows)
-        _check(lib().fq_quantize_rows(self._h, x.data_ptr(), _TYPES[x.dtype], rows, cols, _pitch(x, rows, cols), codes.data_ptr(),
-                                      _pitch(codes, rows, cols), scales.data_ptr(), _stream_on(self.device)), "fq_quantize_rows")
+        rows, cols, ldx = self._matrix(x, "x", _TYPES)
+        codes, ldc, scales = self._codes_and_scales(codes, scales, rows, cols)
+        _check(lib().fq_quantize_rows(self._h, x.data_ptr(), _TYPES[x.dtype], rows, cols, ldx, codes.data_ptr(), ldc, scales.data_ptr(),
+                                      _stream_on(self.device)), "fq_quantize_rows")
         return codes, scales
 
     def _weights(self, w_codes, w_scales, y, m, k):
-        n, kw = self._matrix(w_codes, "w_codes", (torch.int8,))
-        self._vector(w_scales, "w_scales", (torch.float32,), n)
-        if kw != k or tuple(self._matrix(y, "y", _TYPES)) != (m, n):
-            raise ValueError(f"shapes do not fit: {m} rows of {k}, weights {n} x {kw}, outputs {tuple(y.shape)}")
-        return n
+        n, kw, ldw = self._matrix(w_codes, "w_codes", _I8)
+        self._dense(w_scales, "w_scales", _F32, (n,))
+        my, ny, ldy = self._matrix(y, "y", _TYPES)
+        if kw != k or my != m or ny != n:
+            raise ValueError(f"shapes do not fit: {m} rows of {k}, weights {n} x {kw}, outputs {my} x {ny}")
+        return n, ldw, ldy
 
     def fq_gemm_i8(self, x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, y: torch.Tensor):
         """y[m][n] = x_scales[m] * w_scales[n] * sum_k x_codes[m][k] * w_codes[n][k]; y fp16, bf16 or fp32."""
-        m, k = self._matrix(x_codes, "x_codes", (torch.int8,))
-        self._vector(x_scales, "x_scales", (torch.float32,), m)
-        n = self._weights(w_codes, w_scales, y, m, k)
-        _check(lib().fq_gemm_i8(self._h, x_codes.data_ptr(), x_scales.data_ptr(), m, _pitch(x_codes, m, k), w_codes.data_ptr(),
-                                w_scales.data_ptr(), n, k, _pitch(w_codes, n, k), y.data_ptr(), _TYPES[y.dtype], _pitch(y, m, n),
-                                _stream_on(self.device)), "fq_gemm_i8")
+        m, k, ldx = self._matrix(x_codes, "x_codes", _I8)
+        self._dense(x_scales, "x_scales", _F32, (m,))
+        n, ldw, ldy = self._weights(w_codes, w_scales, y, m, k)
+        _check(lib().fq_gemm_i8(self._h, x_codes.data_ptr(), x_scales.data_ptr(), m, ldx, w_codes.data_ptr(), w_scales.data_ptr(), n, k, ldw,
+                                y.data_ptr(), _TYPES[y.dtype], ldy, _stream_on(self.device)), "fq_gemm_i8")
         return y
 
     def fq_linear_i8(self, x: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, y: torch.Tensor,
                      codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None):
         """fq_quantize_rows of x, then fq_gemm_i8, in one call.  `codes` and `scales` are scratch; new where they are not given."""
-        m, k = self._matrix(x, "x", _TYPES)
-        n = self._weights(w_codes, w_scales, y, m, k)
-        if codes is None:
-            codes = self._new_codes(m, k)
-        elif self._matrix(codes, "codes", (torch.int8,)) != x.shape:
-            raise ValueError("codes: another shape than x")
-        if scales is None:
-            scales = torch.empty(m, dtype=torch.float32, device=self.device)
-        self._vector(scales, "scales", (torch.float32,), m)
-        _check(lib().fq_linear_i8(self._h, x.data_ptr(), _TYPES[x.dtype], m, _pitch(x, m, k), w_codes.data_ptr(), w_scales.data_ptr(), n, k,
-                                  _pitch(w_codes, n, k), codes.data_ptr(), _pitch(codes, m, k), scales.data_ptr(), y.data_ptr(),
-                                  _TYPES[y.dtype], _pitch(y, m, n), _stream_on(self.device)), "fq_linear_i8")
+        m, k, ldx = self._matrix(x, "x", _TYPES)
+        n, ldw, ldy = self._weights(w_codes, w_scales, y, m, k)
+        codes, ldc, scales = self._codes_and_scales(codes, scales, m, k)
+        _check(lib().fq_linear_i8(self._h, x.data_ptr(), _TYPES[x.dtype], m, ldx, w_codes.data_ptr(), w_scales.data_ptr(), n, k, ldw,
+                                  codes.data_ptr(), ldc, scales.data_ptr(), y.data_ptr(), _TYPES[y.dtype], ldy, _stream_on(self.device)),
+               "fq_linear_i8")
         return y
 
     # -- what a model answers ------------------------------------------------------------------
     def fq_token_logprobs(self, logits: torch.Tensor, tokens: torch.Tensor, n_top: int = 0, temperature: float = 1.0, out=None):
         """Rows of logits and one token each -> (log probability fp32 [rows], entropy fp32 [rows], ids int32 [rows][n_top] of the most
         likely tokens, their log probabilities fp32 [rows][n_top]).  `out`: the four tensors to write to."""
-        rows, vocab = self._matrix(logits, "logits", _TYPES)
-        self._vector(tokens, "tokens", (torch.int32, torch.int64), rows)
+        rows, vocab, ld = self._matrix(logits, "logits", _TYPES)
+        self._dense(tokens, "tokens", _IDS, (rows,))
         if n_top < 0:
             raise ValueError("n_top is negative")
-        if out is None:
-            both = torch.empty((2, rows), dtype=torch.float32, device=self.device)
-            logprob, entropy = both[0], both[1]
-            ids = torch.empty((rows, n_top), dtype=torch.int32, device=self.device)
-            tops = torch.empty((rows, n_top), dtype=torch.float32, device=self.device)
+        if out is None:                                  # one allocation for all four
+            logprob, entropy, tops, ids = torch.empty(rows * (2 + 2 * n_top), dtype=torch.float32, device=self.device).split(
+                (rows, rows, rows * n_top, rows * n_top))
+            tops, ids = tops.view(rows, n_top), ids.view(torch.int32).view(rows, n_top)
         else:
             logprob, entropy, ids, tops = out
-            self._vector(logprob, "logprob", (torch.float32,), rows)
-            self._vector(entropy, "entropy", (torch.float32,), rows)
-            self._dense(ids, "ids", (torch.int32,), (rows, n_top))
-            self._dense(tops, "tops", (torch.float32,), (rows, n_top))
-        _check(lib().fq_token_logprobs(self._h, logits.data_ptr(), _TYPES[logits.dtype], rows, vocab, _pitch(logits, rows, vocab),
-                                       tokens.data_ptr(), tokens.element_size(), temperature, logprob.data_ptr(), entropy.data_ptr(), n_top,
-                                       ids.data_ptr(), tops.data_ptr(), _stream_on(self.device)), "fq_token_logprobs")
+            self._dense(logprob, "logprob", _F32, (rows,))
+            self._dense(entropy, "entropy", _F32, (rows,))
+            self._dense(ids, "ids", _I32, (rows, n_top))
+            self._dense(tops, "tops", _F32, (rows, n_top))
+        _check(lib().fq_token_logprobs(self._h, logits.data_ptr(), _TYPES[logits.dtype], rows, vocab, ld, tokens.data_ptr(),
+                                       tokens.element_size(), temperature, logprob.data_ptr(), entropy.data_ptr(), n_top, ids.data_ptr(),
+                                       tops.data_ptr(), _stream_on(self.device)), "fq_token_logprobs")
         return logprob, entropy, ids, tops
 
     def _slots(self, logits, ids, teacher, grad_loss, grad):
-        rows, vocab = self._matrix(logits, "logits", _TYPES)
+        rows, vocab, ld = self._matrix(logits, "logits", _TYPES)
         n_top = ids.shape[1] if ids.dim() == 2 else 0
-        self._dense(ids, "ids", (torch.int32, torch.int64), (rows, n_top))
-        self._dense(teacher, "teacher", (torch.float32,), (rows, n_top))
+        self._dense(ids, "ids", _IDS, (rows, n_top))
+        self._dense(teacher, "teacher", _F32, (rows, n_top))
         if grad_loss is not None:
-            self._vector(grad_loss, "grad_loss", (torch.float32,), rows)
-        if grad is not None and (self._matrix(grad, "grad", (logits.dtype,)) != logits.shape):
-            raise ValueError("grad: another shape than logits")
-        return rows, vocab, n_top
+            self._dense(grad_loss, "grad_loss", _F32, (rows,))
+            if grad is None:
+                grad = torch.empty((rows, vocab), dtype=logits.dtype, device=self.device)
+        elif grad is not None:
+            raise ValueError("grad without grad_loss")
+        ldg = 0
+        if grad is not None:
+            r, c, ldg = self._matrix(grad, "grad", (logits.dtype,))
+            if r != rows or c != vocab:
+                raise ValueError(f"grad: {rows} x {vocab} are needed, not {r} x {c}")
+        return rows, vocab, ld, n_top, grad, ldg
 
     def fq_distill_topk(self, logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, temperature: float = 1.0,
                         grad_loss: Optional[torch.Tensor] = None, grad: Optional[torch.Tensor] = None):
         """KL of every row's distribution from its teacher's top logits -> (loss fp32 [rows], lse fp32 [rows][2], gradient or None).
         ids int32 / int64 [rows][n] (negative: an empty slot) and teacher fp32 [rows][n] are the teacher's tokens and logits, or log
-        probabilities.  With `grad_loss` (fp32 [rows], upstream) the gradient with respect to the logits comes from the same pass, into
+        probabilities.  With `grad_loss` (fp32 [rows], upstream) the gradient with respect to the logits comes from the same call, into
         `grad` if that is given (it may be `logits`); without, fq_distill_topk_grad gives it later from `lse`."""
-        rows, vocab, n_top = self._slots(logits, ids, teacher, grad_loss, grad)
-        if grad_loss is None and grad is not None:
-            raise ValueError("grad without grad_loss")
-        if grad_loss is not None and grad is None:
-            grad = torch.empty((rows, vocab), dtype=logits.dtype, device=self.device)
-        loss = torch.empty(rows, dtype=torch.float32, device=self.device)
-        lse = torch.empty((rows, 2), dtype=torch.float32, device=self.device)
-        _check(lib().fq_distill_topk(self._h, logits.data_ptr(), _TYPES[logits.dtype], rows, vocab, _pitch(logits, rows, vocab), ids.data_ptr(),
-                                     ids.element_size(), teacher.data_ptr(), n_top, temperature,
-                                     None if grad_loss is None else grad_loss.data_ptr(), loss.data_ptr(), lse.data_ptr(),
-                                     None if grad is None else grad.data_ptr(), 0 if grad is None else _pitch(grad, rows, vocab),
+        rows, vocab, ld, n_top, grad, ldg = self._slots(logits, ids, teacher, grad_loss, grad)
+        lse, loss = torch.empty(3 * rows, dtype=torch.float32, device=self.device).split((2 * rows, rows))
+        lse = lse.view(rows, 2)
+        _check(lib().fq_distill_topk(self._h, logits.data_ptr(), _TYPES[logits.dtype], rows, vocab, ld, ids.data_ptr(), ids.element_size(),
+                                     teacher.data_ptr(), n_top, temperature, None if grad_loss is None else grad_loss.data_ptr(),
+                                     loss.data_ptr(), lse.data_ptr(), None if grad is None else grad.data_ptr(), ldg,
                                      _stream_on(self.device)), "fq_distill_topk")
         return loss, lse, grad
 
     def fq_distill_topk_grad(self, logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, lse: torch.Tensor, grad_loss: torch.Tensor,
                              temperature: float = 1.0, grad: Optional[torch.Tensor] = None):
         """The gradient of fq_distill_topk's losses, weighted with `grad_loss`, from the `lse` that it returned."""
-        rows, vocab, n_top = self._slots(logits, ids, teacher, grad_loss, grad)
-        self._dense(lse, "lse", (torch.float32,), (rows, 2))
-        if grad is None:
-            grad = torch.empty((rows, vocab), dtype=logits.dtype, device=self.device)
-        _check(lib().fq_distill_topk_grad(self._h, logits.data_ptr(), _TYPES[logits.dtype], rows, vocab, _pitch(logits, rows, vocab),
-                                          ids.data_ptr(), ids.element_size(), teacher.data_ptr(), n_top, temperature, grad_loss.data_ptr(),
-                                          lse.data_ptr(), grad.data_ptr(), _pitch(grad, rows, vocab), _stream_on(self.device)),
-               "fq_distill_topk_grad")
+        rows, vocab, ld, n_top, grad, ldg = self._slots(logits, ids, teacher, grad_loss, grad)
+        self._dense(lse, "lse", _F32, (rows, 2))
+        _check(lib().fq_distill_topk_grad(self._h, logits.data_ptr(), _TYPES[logits.dtype], rows, vocab, ld, ids.data_ptr(), ids.element_size(),
+                                          teacher.data_ptr(), n_top, temperature, grad_loss.data_ptr(), lse.data_ptr(), grad.data_ptr(), ldg,
+                                          _stream_on(self.device)), "fq_distill_topk_grad")
         return grad
