@@ -10,6 +10,7 @@
 // Slices keep the alignment that the row has in global memory, whatever it is: the 16-byte groups inside the slice are copied, the
 // elements before the first and behind the last group are loaded one by one, and the rest of those two groups is filled with -inf,
 // which no maximum and no sum sees: every pass runs over whole groups without masks.
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 
@@ -22,7 +23,6 @@ namespace fq {
 namespace {
 
 constexpr int kRowThreads = 256;
-constexpr int kRowWarps = kRowThreads / 32;
 constexpr int kMaxTop = FQ_MAX_TOP;
 constexpr int kCandidates = 512;
 constexpr int kBatchBits = 2, kBatch = 1 << kBatchBits;       // 16-byte groups that a thread reads at a time
@@ -139,7 +139,7 @@ struct RowSums { float m, s, s1; };       // maximum, sum of exp(d), sum of exp(
 struct RowShared {
     unsigned long long bar;
     RowSums sums;                         // of this CTA's slice, read by the others
-    float4 warp[kRowWarps];               // the warps' sums, and the least of their threads' keys
+    float4 warp[16];                      // the warps' sums, and the least of their threads' keys
     int failed;
 };
 
@@ -396,10 +396,8 @@ struct TopShared {
     };
     int bins[256];                            // the first kBins zeroed before
     int n_pieces, n_cand;                     // zeroed before
-    int n_top;
     float reach;
     int warp[THREADS / 32];
-    int list_len[kMaxCluster];
 };
 
 __device__ __forceinline__ unsigned long long entry_word(uint32_t key, int index) { return (unsigned long long)key << 32 | (0xffffffffu - (uint32_t)index); }
@@ -596,6 +594,18 @@ struct LogprobArgs {
     float* top_logprobs;
 };
 
+template <int THREADS>
+__device__ __forceinline__ int block_sum(int mine, int* words)
+{
+    const int w = __reduce_add_sync(0xffffffffu, mine);
+    if ((threadIdx.x & 31) == 0) words[threadIdx.x >> 5] = w;
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int i = 0; i < THREADS / 32; i++) all += words[i];
+    return all;
+}
+
 // What a row's sums make of its entries.
 struct RowAnswer {
     float zm, log_s, t;
@@ -654,9 +664,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
         }
         return;
     }
-    if (o.n_top > 0) {
-        const int n = slice_top<T, THREADS>(x, o.n_top, my_key, least, most, top, [&](int place, unsigned long long w) { top.top[place] = w; });
-        if (threadIdx.x == 0) top.n_top = n;
+    const int k = o.n_top;
+    if (k > 0) {                                                 // (0 where there are fewer: smaller than any entry's word)
+        const int n = slice_top<T, THREADS>(x, k, my_key, least, most, top, [&](int place, unsigned long long w) { top.top[place] = w; });
+        for (int j = n + threadIdx.x; j < k; j += THREADS) top.top[j] = 0ull;
     }
     if (threadIdx.x == 0) sh.sums = sum;
     cluster_arrive();
@@ -666,36 +677,32 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
         const RowAnswer ans(sum, a.t);
         if (scalar) ans.put(o, r, a.vocab, token, z_token, sum);
         // the CTAs' lists, merged: an entry's place is its own place in its list and what is larger in each of the others
-        if (o.n_top > 0) {
-            unsigned long long* lists = top.lists;
-            int* lens = top.list_len;
-            const uint32_t at = smem_u32(top.top), at_n = smem_u32(&top.n_top);
-            if (threadIdx.x < a.n_cta) lens[threadIdx.x] = cluster_ld_s32(cluster_map(at_n, threadIdx.x));
+        if (k > 0) {
+            const uint32_t at = smem_u32(top.top);
+            for (int i = threadIdx.x; i < a.n_cta * k; i += THREADS) top.lists[i] = cluster_ld_u64(cluster_map(at, (uint32_t)(i / k)) + (uint32_t)(i % k) * 8);
             __syncthreads();
-            for (int i = threadIdx.x; i < a.n_cta * kMaxTop; i += THREADS) {
-                const int c = i / kMaxTop, j = i % kMaxTop;
-                if (j < lens[c]) lists[i] = cluster_ld_u64(cluster_map(at, (uint32_t)c) + (uint32_t)j * 8);
-            }
-            __syncthreads();
-            int total = 0;
-            for (int c = 0; c < a.n_cta; c++) total += lens[c];
-            for (int i = threadIdx.x; i < a.n_cta * kMaxTop; i += THREADS) {
-                const int c = i / kMaxTop, j = i % kMaxTop;
-                if (j >= lens[c]) continue;
-                const unsigned long long w = lists[i];
-                int place = j;
-                for (int d = 0; d < a.n_cta; d++) {
-                    if (d == c) continue;
-                    int lo = 0, hi = lens[d];                           // entries of list d that are larger than w
-                    while (lo < hi) {
-                        const int mid = (lo + hi) >> 1;
-                        if (lists[d * kMaxTop + mid] > w) lo = mid + 1; else hi = mid;
+            int mine_of = 0;
+            for (int i = threadIdx.x; i < a.n_cta * k; i += THREADS) {
+                const unsigned long long w = top.lists[i];
+                if (w == 0) continue;
+                mine_of++;
+                int larger[kMaxCluster] = {};                    // of every list, found bit by bit, all lists side by side
+#pragma unroll
+                for (int step = kMaxTop; step > 0; step >>= 1) {
+                    if (step > k) continue;
+#pragma unroll
+                    for (int d = 0; d < kMaxCluster; d++) {
+                        const int to = larger[d] + step;
+                        if (d < a.n_cta && to <= k && top.lists[d * k + to - 1] > w) larger[d] = to;
                     }
-                    place += lo;
                 }
-                if (place < o.n_top) ans.put_top(o, r, place, w);
+                int place = 0;                                   // (of its own list that is its place there)
+#pragma unroll
+                for (int d = 0; d < kMaxCluster; d++) place += larger[d];
+                if (place < k) ans.put_top(o, r, place, w);
             }
-            for (int j = total + threadIdx.x; j < o.n_top; j += THREADS) ans.put_none(o, r, j);
+            const int total = block_sum<THREADS>(mine_of, top.warp);
+            for (int j = total + threadIdx.x; j < k; j += THREADS) ans.put_none(o, r, j);
         }
     }
     cluster_arrive();                                                    // nobody's shared memory is read any more
@@ -719,7 +726,9 @@ struct TeacherShared {
     long long id[kMaxTop];
     float p[kMaxTop], lp[kMaxTop];        // probability, its logarithm (first: the logits)
     float part[kMaxTop / 32];
-    int any, bad;
+    float value[kMaxTop];                 // gradient at the slot's token
+    int at[kMaxTop];                      // where that is in the buffer, or -1
+    int any;
 };
 
 // The teacher's distribution over its slots (threads 0..31 after the slots are written).
@@ -821,37 +830,33 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_kernel(const RowArgs a
     __shared__ RowShared sh;
     __shared__ TeacherShared te;
     constexpr int N = Group<T>::N;
-    const int rank = (int)(blockIdx.x % a.n_cta);
+    const int rank = (int)(blockIdx.x % a.n_cta), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const long long r = blockIdx.x / a.n_cta;
     const T* row = static_cast<const T*>(a.z) + r * a.ld;
     const Slice s = slice_of<T>(a, row, rank);
-    if (threadIdx.x == 0) {
-        sh.failed = 0;
-        te.bad = 0;
-    }
+    if (threadIdx.x == 0) sh.failed = 0;
     fetch_slice<T>(row, s, buf, smem_u32(&sh.bar));
-    __syncthreads();
     // slot j is thread j's: its id, and the student's logit there (read before any gradient may overwrite it)
     long long id = -1;
     float z_id = kNegInf;
     if (threadIdx.x < o.k) {
         id = load_id(o.ids, o.wide, r * o.k + threadIdx.x);
         const float u = o.teacher[r * o.k + threadIdx.x];
-        if (id >= a.vocab) te.bad = 1;
         const bool in_reach = GIVEN ? id >= s.first && id < s.first + s.n : id >= 0 && id < a.vocab;
         if (in_reach) z_id = Group<T>::to_f(row[id]);
         te.id[threadIdx.x] = id;
         te.lp[threadIdx.x] = id >= 0 ? u : kNegInf;
     }
-    __syncthreads();
-    if (threadIdx.x < 32) teacher_softmax(te, o.k, a.c2, a.t);
+    const float g = o.grad_loss[r];
+    const float2 given = GIVEN ? o.stats[r] : make_float2(0.0f, 0.0f);
+    const bool bad = __syncthreads_or(id >= a.vocab);
+    if (warp == 0) teacher_softmax(te, o.k, a.c2, a.t);
     await_slice(sh, a);
     RowSums sum;
     float log_s;
     if (GIVEN) {
-        const float2 st = o.stats[r];
-        sum = RowSums{st.x, 0.0f, 0.0f};
-        log_s = st.y;
+        sum = RowSums{given.x, 0.0f, 0.0f};
+        log_s = given.y;
         __syncthreads();
     } else {
         const RowSums mine = thread_sums<T, false>(buf, s.groups, a.c2);
@@ -862,74 +867,88 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_kernel(const RowArgs a
             cluster_arrive();
             cluster_wait();
             sum = join(sh, a.n_cta, a.c2);
+            cluster_arrive();                                // this CTA has read the others' sums
         }
         log_s = sum.s == 0.0f ? 0.0f : logf(sum.s);
     }
     const float zm = sum.m == kNegInf ? 0.0f : sum.m;
+    // g (q_i - p_i) / T, formed where the logits are.  A row without a teacher, or whose upstream gradient is 0, gets zeros
+    // whatever it holds.
+    const bool zero = g == 0.0f || (!te.any && !bad);
+    const float w = bad ? NAN : g / a.t;
+    const float off = log_s * kLog2e;                        // q = 2^(t - off)
+    // what the teacher's tokens have on top of it, once for each of them
+    if (threadIdx.x < o.k) {
+        int at = -1;
+        if (!zero && id >= s.first && id < s.first + s.n) {
+            float p = 0.0f;
+            at = s.shift + (int)(id - s.first);
+            for (int j = 0; j < o.k; j++)
+                if (te.id[j] == id) {
+                    if (j < (int)threadIdx.x) at = -1;
+                    p += te.p[j];
+                }
+            te.value[threadIdx.x] = (ex2((z_id - zm) * a.c2 - off) - p) * w;
+        }
+        te.at[threadIdx.x] = at;
+    }
+    __syncthreads();
+    T* dst = static_cast<T*>(o.grad) + r * o.ldg + s.first - s.shift;      // element 0 of the buffer
+    const bool alike = ((reinterpret_cast<uintptr_t>(dst) ^ reinterpret_cast<uintptr_t>(row + s.first - s.shift)) & 15) == 0;
+    T* el = reinterpret_cast<T*>(buf);
+    int lo, hi, at[kMaxTop / 32];
+    whole_groups<T>(s, lo, hi);
+#pragma unroll
+    for (int i = 0; i < kMaxTop / 32; i++) at[i] = lane + 32 * i < o.k ? te.at[lane + 32 * i] : -1;
+    // A warp takes 2 KB at a time, which leave as soon as they are done: what has been stored and what is still being formed overlap.
+    constexpr int kBlock = 128;
+    for (int b = warp * kBlock; b < s.groups; b += (kRowThreads / 32) * kBlock) {
+#pragma unroll
+        for (int i = 0; i < kBlock / 32; i++) {
+            const int group = b + i * 32 + lane;
+            if (group >= s.groups) break;
+            float2 f[N / 2];
+            Group<T>::unpack(buf[group], f);
+#pragma unroll
+            for (int p = 0; p < N / 2; p++) {
+                const float2 t = fma2(add2(f[p], make_float2(-zm, -zm)), make_float2(a.c2, a.c2), make_float2(-off, -off));
+                f[p] = mul2(make_float2(ex2(t.x), ex2(t.y)), make_float2(w, w));
+            }
+            buf[group] = zero ? make_uint4(0u, 0u, 0u, 0u) : Group<T>::pack(f);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kMaxTop / 32; i++)
+            if (at[i] >= b * N && at[i] < (b + kBlock) * N) el[at[i]] = Group<T>::from_f(te.value[lane + 32 * i]);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        const int e0 = max(lo, b * N), e1 = min(hi, (b + kBlock) * N);
+        if (alike && lane == 0 && e1 > e0) {
+            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
+                         ::"l"(dst + e0), "r"(smem_u32(el + e0)), "r"((e1 - e0) * (int)sizeof(T)) : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+    }
     if (!GIVEN && rank == 0) {
         const float loss = distill_loss(te, o.k, sum, log_s, z_id, a.t);
         if (threadIdx.x == 0) {
-            o.loss[r] = te.bad ? NAN : loss;
+            o.loss[r] = bad ? NAN : loss;
             o.stats[r] = make_float2(sum.m, sum.s != sum.s ? NAN : log_s);
         }
     }
-    // g (q_i - p_i) / T, formed where the logits are.  A row without a teacher, or whose upstream gradient is 0, gets zeros
-    // whatever it holds.
-    const float g = o.grad_loss[r];
-    const bool zero = g == 0.0f || (!te.any && !te.bad);
-    const float w = te.bad ? NAN : g / a.t;
-    const float off = log_s * kLog2e;                        // q = 2^(t - off)
-    T* out_row = static_cast<T*>(o.grad) + r * o.ldg;
-    T* el = reinterpret_cast<T*>(buf);
-    for (int i = threadIdx.x; i < s.groups; i += kRowThreads) {
-        float2 f[N / 2];
-        Group<T>::unpack(buf[i], f);
-#pragma unroll
-        for (int p = 0; p < N / 2; p++) {
-            const float2 t = add2(scaled2(f[p], zm, a.c2), make_float2(-off, -off));
-            const float2 q = mul2(make_float2(ex2(t.x), ex2(t.y)), make_float2(w, w));
-            f[p] = zero ? make_float2(0.0f, 0.0f) : q;
-        }
-        buf[i] = Group<T>::pack(f);
-    }
-    __syncthreads();
-    if (threadIdx.x < o.k && !zero && id >= s.first && id < s.first + s.n) {
-        float p = 0.0f;
-        bool first = true;
-        for (int j = 0; j < o.k; j++)
-            if (te.id[j] == id) {
-                if (j < (int)threadIdx.x) first = false;
-                p += te.p[j];
-            }
-        const float t = (z_id - zm) * a.c2 - off;
-        if (first) el[s.shift + (int)(id - s.first)] = Group<T>::from_f((ex2(t) - p) * w);
-    }
-    const bool alike = ((reinterpret_cast<uintptr_t>(out_row) ^ reinterpret_cast<uintptr_t>(row)) & 15) == 0;
-    T* dst = out_row + s.first - s.shift;                    // element 0 of the buffer
-    int lo, hi;
-    whole_groups<T>(s, lo, hi);
-    if (alike) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
     const int end = s.shift + s.n;
     if (alike) {
-        if (threadIdx.x == 0 && hi > lo) {
-            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
-                         ::"l"(dst + lo), "r"(smem_u32(el + lo)), "r"((hi - lo) * (int)sizeof(T)) : "memory");
-            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-        }
         const int t = threadIdx.x - 32;
         if (t >= 0 && t < 2 * N) {
             const int e = t < N ? s.shift + t : hi + (t - N);
             if (t < N ? e < lo && e < end : e < end) dst[e] = el[e];
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     } else {
         for (int e = s.shift + threadIdx.x; e < end; e += kRowThreads) dst[e] = el[e];
     }
-    if (!GIVEN && a.n_cta > 1) {                                 // nobody's sums are read any more
-        cluster_arrive();
-        cluster_wait();
-    }
+    if (!GIVEN && a.n_cta > 1) cluster_wait();                   // nobody's sums are read any more
     if (sh.failed) let_copies_land();
 }
 
@@ -956,6 +975,14 @@ Cut cut_rows(int rows, int vocab, int size, int sm_count, bool cluster)
     return c;
 }
 
+// Threads of a CTA whose rows pass through: 128, the fewest barriers and sums for each row, as long as the rows fill the SMs with them; more where they are few.
+int stream_threads(int rows, int sm_count)
+{
+    int t = 128;
+    while (t < 512 && (long long)rows * t * 2 <= 1024ll * sm_count) t *= 2;
+    return t;
+}
+
 // Rows that pass through are cut only where they are few: until the SMs have all the CTAs that they hold, down to slices of 8 KB.
 Cut cut_streams(int rows, int vocab, int size, int sm_count, int threads)
 {
@@ -974,7 +1001,7 @@ int launch_rows(void (*kernel)(Args...), int threads, std::atomic<bool>* ready, 
                 Args... args)
 {
     if (ctx->device >= 64) return FQ_ERR_ARG;
-    if (!ready[ctx->device].load(std::memory_order_acquire)) {
+    if (c.smem > 0 && !ready[ctx->device].load(std::memory_order_acquire)) {
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 208 * 1024) != cudaSuccess) return FQ_ERR_CUDA;
         ready[ctx->device].store(true, std::memory_order_release);
     }
@@ -1008,18 +1035,20 @@ RowArgs row_args(const Ctx* ctx, const void* logits, int vocab, long long ld, fl
 }
 
 template <class T>
-int logprobs_typed(const Ctx* ctx, int rows, const Cut& c, const RowArgs& a, const LogprobArgs& o, cudaStream_t st)
+int logprobs_typed(const Ctx* ctx, int threads, int rows, const Cut& c, const RowArgs& a, const LogprobArgs& o, cudaStream_t st)
 {
     static std::atomic<bool> ready[2][64];
-    return o.n_top <= kFewTop ? launch_rows(token_logprobs_kernel<T, 128>, 128, ready[0], ctx, rows, c, true, st, a, o)
-                              : launch_rows(token_logprobs_kernel<T, 256>, 256, ready[1], ctx, rows, c, true, st, a, o);
+    if (threads == 128) return launch_rows(token_logprobs_kernel<T, 128>, 128, ready[0], ctx, rows, c, true, st, a, o);
+    return launch_rows(token_logprobs_kernel<T, 256>, 256, ready[1], ctx, rows, c, true, st, a, o);
 }
 
 template <class T>
-int loss_typed(const Ctx* ctx, int rows, const Cut& c, const RowArgs& a, const DistillArgs& o, cudaStream_t st)
+int loss_typed(const Ctx* ctx, int threads, int rows, const Cut& c, const RowArgs& a, const DistillArgs& o, cudaStream_t st)
 {
-    static std::atomic<bool> ready[64];
-    return launch_rows(distill_loss_kernel<T, 128>, 128, ready, ctx, rows, c, true, st, a, o);
+    static std::atomic<bool> ready[3][64];
+    if (threads == 128) return launch_rows(distill_loss_kernel<T, 128>, 128, ready[0], ctx, rows, c, true, st, a, o);
+    if (threads == 256) return launch_rows(distill_loss_kernel<T, 256>, 256, ready[1], ctx, rows, c, true, st, a, o);
+    return launch_rows(distill_loss_kernel<T, 512>, 512, ready[2], ctx, rows, c, true, st, a, o);
 }
 
 template <class T, bool GIVEN>
@@ -1036,11 +1065,12 @@ int distill_any(const fq_ctx* ctx, int dtype, int rows, int vocab, long long ld,
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
     if (!o.grad) {
-        const Cut c = cut_streams(rows, vocab, type_size(dtype), ctx->sm_count, 128);
+        const int threads = stream_threads(rows, ctx->sm_count);
+        const Cut c = cut_streams(rows, vocab, type_size(dtype), ctx->sm_count, threads);
         const RowArgs a = row_args(ctx, logits, vocab, ld, temperature, c);
-        if (dtype == FQ_DT_F32) return loss_typed<float>(ctx, rows, c, a, o, st);
-        if (dtype == FQ_DT_F16) return loss_typed<__half>(ctx, rows, c, a, o, st);
-        return loss_typed<__nv_bfloat16>(ctx, rows, c, a, o, st);
+        if (dtype == FQ_DT_F32) return loss_typed<float>(ctx, threads, rows, c, a, o, st);
+        if (dtype == FQ_DT_F16) return loss_typed<__half>(ctx, threads, rows, c, a, o, st);
+        return loss_typed<__nv_bfloat16>(ctx, threads, rows, c, a, o, st);
     }
     const Cut c = cut_rows(rows, vocab, type_size(dtype), ctx->sm_count, !GIVEN);
     const RowArgs a = row_args(ctx, logits, vocab, ld, temperature, c);
@@ -1067,13 +1097,14 @@ int fq_token_logprobs(fq_ctx* ctx, const void* logits_dev, int dtype, int rows, 
         return FQ_ERR_ALIGN;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
-    const Cut c = cut_streams(rows, vocab, type_size(dtype), ctx->sm_count, n_top <= kFewTop ? 128 : 256);
+    const int threads = n_top <= kFewTop ? 128 : 256;
+    const Cut c = cut_streams(rows, vocab, type_size(dtype), ctx->sm_count, threads);
     const RowArgs a = row_args(ctx, logits_dev, vocab, ld, temperature, c);
     const LogprobArgs o{tokens_dev, id_bytes == 8, logprob_dev, entropy_dev, n_top, top_ids_dev, top_logprobs_dev};
     const cudaStream_t st = (cudaStream_t)stream;
-    if (dtype == FQ_DT_F32) return logprobs_typed<float>(ctx, rows, c, a, o, st);
-    if (dtype == FQ_DT_F16) return logprobs_typed<__half>(ctx, rows, c, a, o, st);
-    return logprobs_typed<__nv_bfloat16>(ctx, rows, c, a, o, st);
+    if (dtype == FQ_DT_F32) return logprobs_typed<float>(ctx, threads, rows, c, a, o, st);
+    if (dtype == FQ_DT_F16) return logprobs_typed<__half>(ctx, threads, rows, c, a, o, st);
+    return logprobs_typed<__nv_bfloat16>(ctx, threads, rows, c, a, o, st);
 }
 
 int fq_distill_topk(fq_ctx* ctx, const void* logits_dev, int dtype, int rows, int vocab, long long ld, const void* ids_dev, int id_bytes,

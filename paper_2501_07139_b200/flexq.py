@@ -470,7 +470,7 @@ class FlexQ:
         if n_top < 0:
             raise ValueError("n_top is negative")
         if out is None:                                  # one allocation for all four
-            logprob, entropy, tops, ids = torch.empty(rows * (2 + 2 * n_top), dtype=torch.float32, device=self.device).split(
+            logprob, entropy, tops, ids = torch.empty(rows * (2 + 2 * n_top), dtype=torch.float32, device=self.device).split_with_sizes(
                 (rows, rows, rows * n_top, rows * n_top))
             tops, ids = tops.view(rows, n_top), ids.view(torch.int32).view(rows, n_top)
         else:
@@ -509,7 +509,7 @@ class FlexQ:
         probabilities.  With `grad_loss` (fp32 [rows], upstream) the gradient with respect to the logits comes from the same call, into
         `grad` if that is given (it may be `logits`); without, fq_distill_topk_grad gives it later from `lse`."""
         rows, vocab, ld, n_top, grad, ldg = self._slots(logits, ids, teacher, grad_loss, grad)
-        lse, loss = torch.empty(3 * rows, dtype=torch.float32, device=self.device).split((2 * rows, rows))
+        lse, loss = torch.empty(3 * rows, dtype=torch.float32, device=self.device).split_with_sizes((2 * rows, rows))
         lse = lse.view(rows, 2)
         _check(lib().fq_distill_topk(self._h, logits.data_ptr(), _TYPES[logits.dtype], rows, vocab, ld, ids.data_ptr(), ids.element_size(),
                                      teacher.data_ptr(), n_top, temperature, None if grad_loss is None else grad_loss.data_ptr(),
