@@ -143,36 +143,6 @@ struct RowShared {
     int failed;
 };
 
-// Sums of the entries of this thread, against their own maximum (0 if that is -inf).  Nobody waits for the slice's maximum: the
-// threads' sums are put on a common one when they are added up.
-template <class T, bool ENTROPY>
-__device__ __forceinline__ RowSums thread_sums(const uint4* buf, int groups, float c2)
-{
-    constexpr int P = Group<T>::N / 2;
-    typename Group<T>::Max best = Group<T>::lowest();
-#pragma unroll 4
-    for (int i = threadIdx.x; i < groups; i += kRowThreads) Group<T>::take_max(best, buf[i]);
-    const float m = Group<T>::of_max(best), mm = m == kNegInf ? 0.0f : m;
-    float2 s = make_float2(0.0f, 0.0f), s1 = make_float2(0.0f, 0.0f);
-#pragma unroll 2
-    for (int i = threadIdx.x; i < groups; i += kRowThreads) {
-        float2 f[P];
-        Group<T>::unpack(buf[i], f);
-#pragma unroll
-        for (int p = 0; p < P; p++) {
-            float2 t = scaled2(f[p], mm, c2);
-            if (ENTROPY) {                                       // exp(-160 ln 2) is 0 in 32 bits; 0 * -inf would be NaN
-                t.x = max_nan(t.x, -160.0f);
-                t.y = max_nan(t.y, -160.0f);
-            }
-            const float2 e = make_float2(ex2(t.x), ex2(t.y));
-            s = add2(s, e);
-            if (ENTROPY) s1 = fma2(e, t, s1);
-        }
-    }
-    return RowSums{m, s.x + s.y, ENTROPY ? s1.x + s1.y : 0.0f};
-}
-
 // `part`, which is against its own maximum, added to `r` against `r.m`, the larger one.
 __device__ __forceinline__ void add_part(RowSums& r, const RowSums& part, float c2)
 {
@@ -182,7 +152,7 @@ __device__ __forceinline__ void add_part(RowSums& r, const RowSums& part, float 
     if (f > 0.0f) r.s1 += f * (part.s1 + part.s * t);
 }
 
-// Sums of the slice, in every thread; `least` is the smallest of the threads' keys (of those that have an entry).
+// Sums of the slice, from its first THREADS threads, in every thread; `least` is the smallest of the threads' keys (of those that have an entry).
 template <int THREADS, bool ENTROPY>
 __device__ __forceinline__ RowSums slice_sums(const RowSums& mine, uint32_t my_key, float c2, RowShared& sh, uint32_t& least)
 {
@@ -193,7 +163,7 @@ __device__ __forceinline__ RowSums slice_sums(const RowSums& mine, uint32_t my_k
     w.s = warp_sum(w.s);
     if (ENTROPY) w.s1 = warp_sum(w.s1);
     const uint32_t low = __reduce_min_sync(0xffffffffu, my_key ? my_key : 0xffffffffu);
-    if ((threadIdx.x & 31) == 0) sh.warp[threadIdx.x >> 5] = make_float4(w.m, w.s, w.s1, __uint_as_float(low));
+    if ((threadIdx.x & 31) == 0 && threadIdx.x < THREADS) sh.warp[threadIdx.x >> 5] = make_float4(w.m, w.s, w.s1, __uint_as_float(low));
     __syncthreads();
     // every warp adds the warps' up, one to a lane
     const int lane = threadIdx.x & ((THREADS / 32) - 1);
@@ -338,6 +308,26 @@ struct Running {
     }
     __device__ __forceinline__ RowSums sums() const { return RowSums{m, s.x + s.y, ENTROPY ? s1.x + s1.y : 0.0f}; }
 };
+
+// Sums of this thread's groups of a slice on chip.
+template <class T, int THREADS>
+__device__ __forceinline__ RowSums kept_sums(const uint4* buf, int groups, float c2)
+{
+    constexpr int U = kBatch;
+    Running<T, false> run;
+    int i = threadIdx.x;
+    for (; i + (U - 1) * THREADS < groups; i += U * THREADS) {
+        uint4 v[U];
+#pragma unroll
+        for (int g = 0; g < U; g++) v[g] = buf[i + g * THREADS];
+        run.take(v, c2);
+    }
+    for (; i < groups; i += THREADS) {
+        const uint4 one[1] = {buf[i]};
+        run.take(one, c2);
+    }
+    return run.sums();
+}
 
 // Sums of this thread's groups lo + thread, + THREADS ..., kBatch of them at a time; those at the ends are the first threads' of two
 // warps.  largest (or NULL): [kSlots][THREADS], -inf before; gets the largest entry of the thread's batches b, b + kSlots, ... in [b].
@@ -724,84 +714,87 @@ struct DistillArgs {
 
 struct TeacherShared {
     long long id[kMaxTop];
-    float p[kMaxTop], lp[kMaxTop];        // probability, its logarithm (first: the logits)
-    float part[kMaxTop / 32];
-    float value[kMaxTop];                 // gradient at the slot's token
-    int at[kMaxTop];                      // where that is in the buffer, or -1
-    int any;
+    float p[kMaxTop];
+    float all[kMaxTop];                   // the probability of the slot's token, in all of its slots
+    int at[kMaxTop];                      // where the token is in the buffer; -1: not there, or the token of an earlier slot
+    int any, bad;
 };
 
-// The teacher's distribution over its slots (threads 0..31 after the slots are written).
-__device__ __forceinline__ void teacher_softmax(TeacherShared& sh, int k, float c2, float t)
+// The teacher's distribution over the warp's slots, kMaxTop / 32 to a lane: from logits (-inf: empty) to log probabilities, and probabilities.
+// Returns whether there is one (a NaN is).
+__device__ __forceinline__ bool teacher_softmax(float (&p)[kMaxTop / 32], float (&lp)[kMaxTop / 32], float c2, float t)
 {
-    const int lane = threadIdx.x;
-    float u[kMaxTop / 32], m = kNegInf, s = 0.0f;
+    float m = kNegInf, s = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kMaxTop / 32; i++) {
-        u[i] = lane + 32 * i < k ? sh.lp[lane + 32 * i] : kNegInf;
-        m = max_nan(m, u[i]);
-    }
+    for (int i = 0; i < kMaxTop / 32; i++) m = max_nan(m, lp[i]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
     const float mm = m == kNegInf ? 0.0f : m;
-    float e[kMaxTop / 32];
 #pragma unroll
     for (int i = 0; i < kMaxTop / 32; i++) {
-        e[i] = ex2((u[i] - mm) * c2);
-        s += e[i];
+        p[i] = ex2((lp[i] - mm) * c2);
+        s += p[i];
     }
     s = warp_sum(s);
     const float inv = s == 0.0f ? 0.0f : 1.0f / s, log_s = s == 0.0f ? 0.0f : logf(s);
 #pragma unroll
-    for (int i = 0; i < kMaxTop / 32; i++)
-        if (lane + 32 * i < k) {
-            sh.p[lane + 32 * i] = e[i] * inv;
-            sh.lp[lane + 32 * i] = (u[i] - mm) / t - log_s;
-        }
-    if (lane == 0) sh.any = s != 0.0f;                                       // (NaN: true)
+    for (int i = 0; i < kMaxTop / 32; i++) {
+        p[i] *= inv;
+        lp[i] = (lp[i] - mm) / t - log_s;
+    }
+    return s != 0.0f;
 }
 
-// sum p (log p - log q), in every lane of warp 0.  All threads; slot j is thread j's.
-__device__ __forceinline__ float distill_loss(TeacherShared& te, int k, const RowSums& sum, float log_s, float z_id, float t)
+// A warp's slots, kMaxTop / 32 to a lane: ids, the teacher's logits (-inf: empty) and, if `row` is not NULL, the student's at the ids.  Those are on
+// their way when the function returns: nothing waits for them before they are used.  (They are read before any gradient may overwrite them.)
+template <class T>
+__device__ __forceinline__ void load_slots(const DistillArgs& o, long long r, const T* row, int vocab, long long (&id)[kMaxTop / 32], float (&u)[kMaxTop / 32],
+                                           T (&z)[kMaxTop / 32], bool& bad)
 {
-    const float zm = sum.m == kNegInf ? 0.0f : sum.m;
-    float term = 0.0f;
-    if (threadIdx.x < k) {
-        const float p = te.p[threadIdx.x];
-        // p times a distance that 32 bits do not hold may well be one that they do
-        if (!(p == 0.0f)) term = p * (te.lp[threadIdx.x] + log_s) - p * (z_id - zm) / t;
-    }
-    if (threadIdx.x < kMaxTop) {
-        term = warp_sum(term);
-        if ((threadIdx.x & 31) == 0) te.part[threadIdx.x >> 5] = term;
-    }
-    __syncthreads();
-    float loss = 0.0f;
+    const int lane = threadIdx.x & 31;
+    bad = false;
 #pragma unroll
-    for (int i = 0; i < kMaxTop / 32; i++) loss += te.part[i];
-    return loss;
+    for (int i = 0; i < kMaxTop / 32; i++) {
+        const int j = lane + 32 * i;
+        id[i] = j < o.k ? load_id(o.ids, o.wide, r * o.k + j) : -1;
+        u[i] = j < o.k ? o.teacher[r * o.k + j] : kNegInf;
+    }
+#pragma unroll
+    for (int i = 0; i < kMaxTop / 32; i++) {
+        z[i] = row && id[i] >= 0 && id[i] < vocab ? row[id[i]] : Group<T>::from_f(kNegInf);
+        if (id[i] < 0) u[i] = kNegInf;
+        bad |= id[i] >= vocab;
+    }
+    bad = __any_sync(0xffffffffu, bad);
+}
+
+// p (log p - log q); p times a distance that 32 bits do not hold may well be one that they do.
+__device__ __forceinline__ float loss_term(float p, float lp, float z_id, float zm, float log_s, float t)
+{
+    return p == 0.0f ? 0.0f : p * (lp + log_s) - p * (z_id - zm) / t;
 }
 
 // The value alone: the logits pass through once.
 template <class T, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_loss_kernel(const RowArgs a, const DistillArgs o)
+__global__ void __launch_bounds__(THREADS + 32, 1024 / THREADS) distill_loss_kernel(const RowArgs a, const DistillArgs o)
 {
     __shared__ RowShared sh;
-    __shared__ TeacherShared te;
-    const int rank = a.n_cta > 1 ? (int)cluster_cta() : 0;
+    constexpr int kPer = kMaxTop / 32;
+    const int rank = a.n_cta > 1 ? (int)cluster_cta() : 0, lane = threadIdx.x & 31;
     const long long r = blockIdx.x / a.n_cta;
     const T* row = static_cast<const T*>(a.z) + r * a.ld;
-    long long id = -1;
-    float z_id = kNegInf;
-    if (rank == 0 && threadIdx.x < o.k) {
-        id = load_id(o.ids, o.wide, r * o.k + threadIdx.x);
-        const float u = o.teacher[r * o.k + threadIdx.x];
-        if (id >= 0 && id < a.vocab) z_id = Group<T>::to_f(row[id]);
-        te.lp[threadIdx.x] = id >= 0 ? u : kNegInf;
+    const bool teaches = rank == 0 && threadIdx.x >= THREADS;    // one warp more than those that see to the logits
+    RowSums mine{kNegInf, 0.0f, 0.0f};
+    float p[kPer], lp[kPer];
+    T z_id[kPer];
+    bool bad = false;
+    if (teaches) {
+        long long id[kPer];
+        load_slots<T>(o, r, row, a.vocab, id, lp, z_id, bad);
+        teacher_softmax(p, lp, a.c2, a.t);
+    } else if (threadIdx.x < THREADS) {
+        mine = stream_sums<T, THREADS, false>(Stream<T>(row, slice_of<T>(a, row, rank)), a.c2, nullptr);
     }
-    const RowSums mine = stream_sums<T, THREADS, false>(Stream<T>(row, slice_of<T>(a, row, rank)), a.c2, nullptr);
-    const bool bad = __syncthreads_or(id >= a.vocab);
-    if (rank == 0 && threadIdx.x < 32) teacher_softmax(te, o.k, a.c2, a.t);
     uint32_t least;
     RowSums sum = slice_sums<THREADS, false>(mine, mine.m > kNegInf ? key_of(mine.m) : 0u, a.c2, sh, least);
     if (a.n_cta > 1) {
@@ -811,10 +804,13 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_loss_kernel(c
         if (rank == 0) sum = join(sh, a.n_cta, a.c2);
         cluster_arrive();                                        // nobody's sums are read any more
     }
-    if (rank == 0) {
-        const float log_s = sum.s == 0.0f ? 0.0f : logf(sum.s);
-        const float loss = distill_loss(te, o.k, sum, log_s, z_id, a.t);
-        if (threadIdx.x == 0) {
+    if (teaches) {
+        const float log_s = sum.s == 0.0f ? 0.0f : logf(sum.s), zm = sum.m == kNegInf ? 0.0f : sum.m;
+        float loss = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kPer; i++) loss += loss_term(p[i], lp[i], Group<T>::to_f(z_id[i]), zm, log_s, a.t);
+        loss = warp_sum(loss);
+        if (lane == 0) {
             o.loss[r] = bad ? NAN : loss;
             o.stats[r] = make_float2(sum.m, sum.s != sum.s ? NAN : log_s);
         }
@@ -823,35 +819,66 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_loss_kernel(c
 }
 
 // GIVEN: the gradient alone, from the (m, log S) that an earlier call kept; slices then need nothing from one another.
+//   Eight warps see to the logits.  A ninth one sees to the teacher: its distribution, the student's logits at its tokens (two loads, one after the
+// other, and a chain of dependent arithmetic that would hold the others up), and at the end the loss.
 template <class T, bool GIVEN>
-__global__ void __launch_bounds__(kRowThreads, 4) distill_kernel(const RowArgs a, const DistillArgs o)
+__global__ void __launch_bounds__(kRowThreads + 32, 4) distill_kernel(const RowArgs a, const DistillArgs o)
 {
     extern __shared__ __align__(16) uint4 buf[];
     __shared__ RowShared sh;
     __shared__ TeacherShared te;
-    constexpr int N = Group<T>::N;
+    constexpr int N = Group<T>::N, kPer = kMaxTop / 32;
     const int rank = (int)(blockIdx.x % a.n_cta), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const long long r = blockIdx.x / a.n_cta;
     const T* row = static_cast<const T*>(a.z) + r * a.ld;
     const Slice s = slice_of<T>(a, row, rank);
+    const bool teaches = warp == kRowThreads / 32;
     if (threadIdx.x == 0) sh.failed = 0;
     fetch_slice<T>(row, s, buf, smem_u32(&sh.bar));
-    // slot j is thread j's: its id, and the student's logit there (read before any gradient may overwrite it)
-    long long id = -1;
-    float z_id = kNegInf;
-    if (threadIdx.x < o.k) {
-        id = load_id(o.ids, o.wide, r * o.k + threadIdx.x);
-        const float u = o.teacher[r * o.k + threadIdx.x];
-        const bool in_reach = GIVEN ? id >= s.first && id < s.first + s.n : id >= 0 && id < a.vocab;
-        if (in_reach) z_id = Group<T>::to_f(row[id]);
-        te.id[threadIdx.x] = id;
-        te.lp[threadIdx.x] = id >= 0 ? u : kNegInf;
-    }
     const float g = o.grad_loss[r];
     const float2 given = GIVEN ? o.stats[r] : make_float2(0.0f, 0.0f);
-    const bool bad = __syncthreads_or(id >= a.vocab);
-    if (warp == 0) teacher_softmax(te, o.k, a.c2, a.t);
-    await_slice(sh, a);
+    __syncthreads();
+    RowSums mine{kNegInf, 0.0f, 0.0f};
+    float p[kPer], lp[kPer];                                     // of the ninth warp: slots lane, lane + 32, ...
+    T z_id[kPer];
+    if (teaches) {
+        bool bad;
+        long long id[kPer];
+        load_slots<T>(o, r, rank == 0 && !GIVEN ? row : nullptr, a.vocab, id, lp, z_id, bad);
+        const bool some = teacher_softmax(p, lp, a.c2, a.t);
+        // a token's probabilities, added up once for all of its slots
+#pragma unroll
+        for (int i = 0; i < kPer; i++)
+            if (lane + 32 * i < o.k) {
+                te.id[lane + 32 * i] = id[i];
+                te.p[lane + 32 * i] = p[i];
+            }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kPer; i++) {
+            const int j = lane + 32 * i;
+            if (j >= o.k) break;
+            int at = -1;
+            float all = 0.0f;
+            if (id[i] >= s.first && id[i] < s.first + s.n) {
+                at = s.shift + (int)(id[i] - s.first);
+                for (int l = 0; l < o.k; l++)
+                    if (te.id[l] == id[i]) {
+                        if (l < j) at = -1;
+                        all += te.p[l];
+                    }
+            }
+            te.at[j] = at;
+            te.all[j] = all;
+        }
+        if (lane == 0) {
+            te.any = some;
+            te.bad = bad;
+        }
+    } else {
+        await_slice(sh, a);
+        if (!GIVEN) mine = kept_sums<T, kRowThreads>(buf, s.groups, a.c2);
+    }
     RowSums sum;
     float log_s;
     if (GIVEN) {
@@ -859,7 +886,6 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_kernel(const RowArgs a
         log_s = given.y;
         __syncthreads();
     } else {
-        const RowSums mine = thread_sums<T, false>(buf, s.groups, a.c2);
         uint32_t least;
         sum = slice_sums<kRowThreads, false>(mine, mine.m > kNegInf ? key_of(mine.m) : 0u, a.c2, sh, least);
         if (a.n_cta > 1) {
@@ -872,81 +898,72 @@ __global__ void __launch_bounds__(kRowThreads, 4) distill_kernel(const RowArgs a
         log_s = sum.s == 0.0f ? 0.0f : logf(sum.s);
     }
     const float zm = sum.m == kNegInf ? 0.0f : sum.m;
-    // g (q_i - p_i) / T, formed where the logits are.  A row without a teacher, or whose upstream gradient is 0, gets zeros
-    // whatever it holds.
-    const bool zero = g == 0.0f || (!te.any && !bad);
-    const float w = bad ? NAN : g / a.t;
-    const float off = log_s * kLog2e;                        // q = 2^(t - off)
-    // what the teacher's tokens have on top of it, once for each of them
-    if (threadIdx.x < o.k) {
-        int at = -1;
-        if (!zero && id >= s.first && id < s.first + s.n) {
-            float p = 0.0f;
-            at = s.shift + (int)(id - s.first);
-            for (int j = 0; j < o.k; j++)
-                if (te.id[j] == id) {
-                    if (j < (int)threadIdx.x) at = -1;
-                    p += te.p[j];
-                }
-            te.value[threadIdx.x] = (ex2((z_id - zm) * a.c2 - off) - p) * w;
-        }
-        te.at[threadIdx.x] = at;
-    }
-    __syncthreads();
-    T* dst = static_cast<T*>(o.grad) + r * o.ldg + s.first - s.shift;      // element 0 of the buffer
-    const bool alike = ((reinterpret_cast<uintptr_t>(dst) ^ reinterpret_cast<uintptr_t>(row + s.first - s.shift)) & 15) == 0;
-    T* el = reinterpret_cast<T*>(buf);
-    int lo, hi, at[kMaxTop / 32];
-    whole_groups<T>(s, lo, hi);
+    if (teaches) {
+        if (!GIVEN && rank == 0) {
+            float loss = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kMaxTop / 32; i++) at[i] = lane + 32 * i < o.k ? te.at[lane + 32 * i] : -1;
-    // A warp takes 2 KB at a time, which leave as soon as they are done: what has been stored and what is still being formed overlap.
-    constexpr int kBlock = 128;
-    for (int b = warp * kBlock; b < s.groups; b += (kRowThreads / 32) * kBlock) {
-#pragma unroll
-        for (int i = 0; i < kBlock / 32; i++) {
-            const int group = b + i * 32 + lane;
-            if (group >= s.groups) break;
-            float2 f[N / 2];
-            Group<T>::unpack(buf[group], f);
-#pragma unroll
-            for (int p = 0; p < N / 2; p++) {
-                const float2 t = fma2(add2(f[p], make_float2(-zm, -zm)), make_float2(a.c2, a.c2), make_float2(-off, -off));
-                f[p] = mul2(make_float2(ex2(t.x), ex2(t.y)), make_float2(w, w));
+            for (int i = 0; i < kPer; i++) loss += loss_term(p[i], lp[i], Group<T>::to_f(z_id[i]), zm, log_s, a.t);
+            loss = warp_sum(loss);
+            if (lane == 0) {
+                o.loss[r] = te.bad ? NAN : loss;
+                o.stats[r] = make_float2(sum.m, sum.s != sum.s ? NAN : log_s);
             }
-            buf[group] = zero ? make_uint4(0u, 0u, 0u, 0u) : Group<T>::pack(f);
         }
-        __syncwarp();
+    } else {
+        // g (q_i - p_i) / T, formed where the logits are.  A row without a teacher, or whose upstream gradient is 0, gets zeros
+        // whatever it holds.
+        const bool bad = te.bad, zero = g == 0.0f || (!te.any && !bad);
+        const float w = bad ? NAN : g / a.t;
+        const float off = log_s * kLog2e;                    // q = 2^(t - off)
+        T* dst = static_cast<T*>(o.grad) + r * o.ldg + s.first - s.shift;      // element 0 of the buffer
+        const bool alike = ((reinterpret_cast<uintptr_t>(dst) ^ reinterpret_cast<uintptr_t>(row + s.first - s.shift)) & 15) == 0;
+        T* el = reinterpret_cast<T*>(buf);
+        int lo, hi, at[kPer];
+        whole_groups<T>(s, lo, hi);
+        const int end = s.shift + s.n;
 #pragma unroll
-        for (int i = 0; i < kMaxTop / 32; i++)
-            if (at[i] >= b * N && at[i] < (b + kBlock) * N) el[at[i]] = Group<T>::from_f(te.value[lane + 32 * i]);
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        const int e0 = max(lo, b * N), e1 = min(hi, (b + kBlock) * N);
-        if (alike && lane == 0 && e1 > e0) {
-            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
-                         ::"l"(dst + e0), "r"(smem_u32(el + e0)), "r"((e1 - e0) * (int)sizeof(T)) : "memory");
-            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-        }
-    }
-    if (!GIVEN && rank == 0) {
-        const float loss = distill_loss(te, o.k, sum, log_s, z_id, a.t);
-        if (threadIdx.x == 0) {
-            o.loss[r] = bad ? NAN : loss;
-            o.stats[r] = make_float2(sum.m, sum.s != sum.s ? NAN : log_s);
-        }
-    }
-    __syncthreads();
-    const int end = s.shift + s.n;
-    if (alike) {
-        const int t = threadIdx.x - 32;
-        if (t >= 0 && t < 2 * N) {
-            const int e = t < N ? s.shift + t : hi + (t - N);
-            if (t < N ? e < lo && e < end : e < end) dst[e] = el[e];
+        for (int i = 0; i < kPer; i++) at[i] = !zero && lane + 32 * i < o.k ? te.at[lane + 32 * i] : -1;
+        // A warp takes 2 KB at a time, which leave as soon as they are done: what has been stored and what is still being formed overlap.
+        constexpr int kBlock = 128;
+        for (int b = warp * kBlock; b < s.groups; b += (kRowThreads / 32) * kBlock) {
+            const int b0 = b * N, b1 = (b + kBlock) * N, e0 = max(lo, b0), e1 = min(hi, b1);
+            float z[kPer];
+#pragma unroll
+            for (int i = 0; i < kPer; i++) z[i] = at[i] >= b0 && at[i] < b1 ? Group<T>::to_f(el[at[i]]) : 0.0f;
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < kBlock / 32; i++) {
+                const int group = b + i * 32 + lane;
+                if (group >= s.groups) break;
+                float2 f[N / 2];
+                Group<T>::unpack(buf[group], f);
+#pragma unroll
+                for (int h = 0; h < N / 2; h++) {
+                    const float2 t = fma2(add2(f[h], make_float2(-zm, -zm)), make_float2(a.c2, a.c2), make_float2(-off, -off));
+                    f[h] = mul2(make_float2(ex2(t.x), ex2(t.y)), make_float2(w, w));
+                }
+                buf[group] = zero ? make_uint4(0u, 0u, 0u, 0u) : Group<T>::pack(f);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < kPer; i++)
+                if (at[i] >= b0 && at[i] < b1) el[at[i]] = Group<T>::from_f((ex2((z[i] - zm) * a.c2 - off) - te.all[lane + 32 * i]) * w);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (!alike) {
+                for (int e = max(b0, s.shift) + lane; e < min(b1, end); e += 32) dst[e] = el[e];
+                continue;
+            }
+            if (lane == 0 && e1 > e0) {
+                asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
+                             ::"l"(dst + e0), "r"(smem_u32(el + e0)), "r"((e1 - e0) * (int)sizeof(T)) : "memory");
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+            // the ends of the slice, where its groups are not whole
+            if (b == 0 && s.shift + lane < min(lo, end)) dst[s.shift + lane] = el[s.shift + lane];
+            if (hi >= b0 && hi < b1 && hi + lane < end) dst[hi + lane] = el[hi + lane];
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-    } else {
-        for (int e = s.shift + threadIdx.x; e < end; e += kRowThreads) dst[e] = el[e];
     }
     if (!GIVEN && a.n_cta > 1) cluster_wait();                   // nobody's sums are read any more
     if (sh.failed) let_copies_land();
@@ -1046,16 +1063,16 @@ template <class T>
 int loss_typed(const Ctx* ctx, int threads, int rows, const Cut& c, const RowArgs& a, const DistillArgs& o, cudaStream_t st)
 {
     static std::atomic<bool> ready[3][64];
-    if (threads == 128) return launch_rows(distill_loss_kernel<T, 128>, 128, ready[0], ctx, rows, c, true, st, a, o);
-    if (threads == 256) return launch_rows(distill_loss_kernel<T, 256>, 256, ready[1], ctx, rows, c, true, st, a, o);
-    return launch_rows(distill_loss_kernel<T, 512>, 512, ready[2], ctx, rows, c, true, st, a, o);
+    if (threads == 128) return launch_rows(distill_loss_kernel<T, 128>, 128 + 32, ready[0], ctx, rows, c, true, st, a, o);
+    if (threads == 256) return launch_rows(distill_loss_kernel<T, 256>, 256 + 32, ready[1], ctx, rows, c, true, st, a, o);
+    return launch_rows(distill_loss_kernel<T, 512>, 512 + 32, ready[2], ctx, rows, c, true, st, a, o);
 }
 
 template <class T, bool GIVEN>
 int distill_typed(const Ctx* ctx, int rows, const Cut& c, const RowArgs& a, const DistillArgs& o, cudaStream_t st)
 {
     static std::atomic<bool> ready[64];
-    return launch_rows(distill_kernel<T, GIVEN>, kRowThreads, ready, ctx, rows, c, !GIVEN, st, a, o);
+    return launch_rows(distill_kernel<T, GIVEN>, kRowThreads + 32, ready, ctx, rows, c, !GIVEN, st, a, o);
 }
 
 template <bool GIVEN>
