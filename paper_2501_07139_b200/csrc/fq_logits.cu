@@ -22,7 +22,6 @@
 namespace fq {
 namespace {
 
-constexpr int kRowThreads = 256;
 constexpr int kMaxTop = FQ_MAX_TOP;
 constexpr int kCandidates = 512;
 constexpr int kBatchBits = 2, kBatch = 1 << kBatchBits;       // 16-byte groups that a thread reads at a time
@@ -712,8 +711,8 @@ struct DistillArgs {
     long long ldg;
 };
 
-struct TeacherShared {
-    long long id[kMaxTop];
+struct __align__(16) TeacherShared {
+    int id[kMaxTop];                      // -1: none
     float p[kMaxTop];
     float all[kMaxTop];                   // the probability of the slot's token, in all of its slots
     int at[kMaxTop];                      // where the token is in the buffer; -1: not there, or the token of an earlier slot
@@ -819,10 +818,10 @@ __global__ void __launch_bounds__(THREADS + 32, 1024 / THREADS) distill_loss_ker
 }
 
 // GIVEN: the gradient alone, from the (m, log S) that an earlier call kept; slices then need nothing from one another.
-//   Eight warps see to the logits.  A ninth one sees to the teacher: its distribution, the student's logits at its tokens (two loads, one after the
+//   THREADS threads see to the logits.  One warp more sees to the teacher: its distribution, the student's logits at its tokens (two loads, one after the
 // other, and a chain of dependent arithmetic that would hold the others up), and at the end the loss.
-template <class T, bool GIVEN>
-__global__ void __launch_bounds__(kRowThreads + 32, 4) distill_kernel(const RowArgs a, const DistillArgs o)
+template <class T, int THREADS, bool GIVEN>
+__global__ void __launch_bounds__(THREADS + 32, 1024 / THREADS) distill_kernel(const RowArgs a, const DistillArgs o)
 {
     extern __shared__ __align__(16) uint4 buf[];
     __shared__ RowShared sh;
@@ -832,14 +831,14 @@ __global__ void __launch_bounds__(kRowThreads + 32, 4) distill_kernel(const RowA
     const long long r = blockIdx.x / a.n_cta;
     const T* row = static_cast<const T*>(a.z) + r * a.ld;
     const Slice s = slice_of<T>(a, row, rank);
-    const bool teaches = warp == kRowThreads / 32;
+    const bool teaches = warp == THREADS / 32;
     if (threadIdx.x == 0) sh.failed = 0;
     fetch_slice<T>(row, s, buf, smem_u32(&sh.bar));
     const float g = o.grad_loss[r];
     const float2 given = GIVEN ? o.stats[r] : make_float2(0.0f, 0.0f);
     __syncthreads();
     RowSums mine{kNegInf, 0.0f, 0.0f};
-    float p[kPer], lp[kPer];                                     // of the ninth warp: slots lane, lane + 32, ...
+    float p[kPer], lp[kPer];                                     // of the last warp: slots lane, lane + 32, ...
     T z_id[kPer];
     if (teaches) {
         bool bad;
@@ -848,25 +847,27 @@ __global__ void __launch_bounds__(kRowThreads + 32, 4) distill_kernel(const RowA
         const bool some = teacher_softmax(p, lp, a.c2, a.t);
         // a token's probabilities, added up once for all of its slots
 #pragma unroll
-        for (int i = 0; i < kPer; i++)
-            if (lane + 32 * i < o.k) {
-                te.id[lane + 32 * i] = id[i];
-                te.p[lane + 32 * i] = p[i];
-            }
+        for (int i = 0; i < kPer; i++) {
+            te.id[lane + 32 * i] = id[i] >= 0 && id[i] < a.vocab ? (int)id[i] : -1;
+            te.p[lane + 32 * i] = p[i];
+        }
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < kPer; i++) {
             const int j = lane + 32 * i;
-            if (j >= o.k) break;
-            int at = -1;
+            const bool here = id[i] >= s.first && id[i] < s.first + s.n;
+            int at = here ? s.shift + (int)(id[i] - s.first) : -1;
             float all = 0.0f;
-            if (id[i] >= s.first && id[i] < s.first + s.n) {
-                at = s.shift + (int)(id[i] - s.first);
-                for (int l = 0; l < o.k; l++)
-                    if (te.id[l] == id[i]) {
-                        if (l < j) at = -1;
-                        all += te.p[l];
-                    }
+            if (__any_sync(0xffffffffu, here)) {
+                const int mine = here ? (int)id[i] : -2;
+                for (int l = 0; l < o.k; l += 4) {
+                    const int4 v = *reinterpret_cast<const int4*>(te.id + l);
+                    const float4 q = *reinterpret_cast<const float4*>(te.p + l);
+                    if (v.x == mine) { all += q.x; if (l < j) at = -1; }
+                    if (v.y == mine) { all += q.y; if (l + 1 < j) at = -1; }
+                    if (v.z == mine) { all += q.z; if (l + 2 < j) at = -1; }
+                    if (v.w == mine) { all += q.w; if (l + 3 < j) at = -1; }
+                }
             }
             te.at[j] = at;
             te.all[j] = all;
@@ -877,7 +878,7 @@ __global__ void __launch_bounds__(kRowThreads + 32, 4) distill_kernel(const RowA
         }
     } else {
         await_slice(sh, a);
-        if (!GIVEN) mine = kept_sums<T, kRowThreads>(buf, s.groups, a.c2);
+        if (!GIVEN) mine = kept_sums<T, THREADS>(buf, s.groups, a.c2);
     }
     RowSums sum;
     float log_s;
@@ -887,7 +888,7 @@ __global__ void __launch_bounds__(kRowThreads + 32, 4) distill_kernel(const RowA
         __syncthreads();
     } else {
         uint32_t least;
-        sum = slice_sums<kRowThreads, false>(mine, mine.m > kNegInf ? key_of(mine.m) : 0u, a.c2, sh, least);
+        sum = slice_sums<THREADS, false>(mine, mine.m > kNegInf ? key_of(mine.m) : 0u, a.c2, sh, least);
         if (a.n_cta > 1) {
             if (threadIdx.x == 0) sh.sums = sum;
             cluster_arrive();
@@ -925,7 +926,7 @@ __global__ void __launch_bounds__(kRowThreads + 32, 4) distill_kernel(const RowA
         for (int i = 0; i < kPer; i++) at[i] = !zero && lane + 32 * i < o.k ? te.at[lane + 32 * i] : -1;
         // A warp takes 2 KB at a time, which leave as soon as they are done: what has been stored and what is still being formed overlap.
         constexpr int kBlock = 128;
-        for (int b = warp * kBlock; b < s.groups; b += (kRowThreads / 32) * kBlock) {
+        for (int b = warp * kBlock; b < s.groups; b += (THREADS / 32) * kBlock) {
             const int b0 = b * N, b1 = (b + kBlock) * N, e0 = max(lo, b0), e1 = min(hi, b1);
             float z[kPer];
 #pragma unroll
@@ -1071,8 +1072,12 @@ int loss_typed(const Ctx* ctx, int threads, int rows, const Cut& c, const RowArg
 template <class T, bool GIVEN>
 int distill_typed(const Ctx* ctx, int rows, const Cut& c, const RowArgs& a, const DistillArgs& o, cudaStream_t st)
 {
-    static std::atomic<bool> ready[64];
-    return launch_rows(distill_kernel<T, GIVEN>, kRowThreads + 32, ready, ctx, rows, c, !GIVEN, st, a, o);
+    static std::atomic<bool> ready[2][64];
+    // (rows of up to 36 KB: six CTAs to an SM, if they have half the threads)
+    if constexpr (!GIVEN) {
+        if (c.smem <= 36 * 1024) return launch_rows(distill_kernel<T, 128, false>, 128 + 32, ready[0], ctx, rows, c, true, st, a, o);
+    }
+    return launch_rows(distill_kernel<T, 256, GIVEN>, 256 + 32, ready[1], ctx, rows, c, !GIVEN, st, a, o);
 }
 
 template <bool GIVEN>

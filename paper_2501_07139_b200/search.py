@@ -4,25 +4,68 @@ library's tree search (Sec. III-B, Algorithm 1) and pruning (Sec. III-C) on them
 The paper evaluates candidates by perplexity on a calibration set; without trained weights and datasets the
 evaluation here is the relative output error of each linear layer on seeded calibration activations,
 || Y_b - Y_8 ||^2 / || Y_8 ||^2, summed over the layers of a module (and over modules for a configuration).
+The output head, whose outputs are logits, can be evaluated by what it answers instead: the divergence of its
+distribution from that of the highest precision's top tokens (`head`), and the perplexity of given tokens (head_answers).
 The library does the heavy work: fq_gemm for the outputs, fq_sqdiff for the two fp64 sums of every comparison,
-fq_code_bytes for the sizes, fq_search_chain / fq_prune_chain for the search.  This module only divides each pair
-of sums and adds the per-layer ratios and sizes up per module (a few hundred host operations)."""
+fq_token_logprobs and fq_distill_topk for the head's, fq_code_bytes for the sizes, fq_search_chain / fq_prune_chain for
+the search.  This module only divides each pair of sums and adds the per-layer ratios and sizes up per module (a few
+hundred host operations)."""
 from __future__ import annotations
 
-from typing import Dict, List, Sequence
+import math
+from typing import Dict, List, NamedTuple, Optional, Sequence
 
 import torch
 
 from . import flexq as F
 
 
+class Head(NamedTuple):
+    """The layer whose outputs are logits, a next token for every calibration token (negative: none), and how many of the highest
+    precision's tokens a lower one is held to."""
+    layer: int
+    targets: torch.Tensor
+    n_top: int = 32
+    temperature: float = 1.0
+
+
+def _outputs(tokens: int, n_out: int, device) -> torch.Tensor:
+    """bf16 outputs with the row pitch that fq_gemm takes."""
+    return torch.empty((tokens, -(-n_out // 8) * 8), dtype=torch.bfloat16, device=device)[:, :n_out]
+
+
+def head_answers(fq: "F.FlexQ", head: Head, n_out: int, levels: Sequence[int], x: torch.Tensor) -> List[dict]:
+    """What the head answers to the bf16 activations `x` at every bit-width of `levels` (the other layers stay as they are, the head is left
+    at levels[0]): mean negative log likelihood `nll` of the targets, its exponential `perplexity`, mean `entropy`, and `kl`, the
+    mean divergence from the tokens that levels[0] finds most likely."""
+    bits = [fq.fq_active_bits(i) for i in range(fq.n_layers)]
+    y, out, teacher = _outputs(x.shape[0], n_out, x.device), [], None
+    asked = (head.targets >= 0).sum()
+    for b in list(levels) + [levels[0]]:
+        bits[head.layer] = int(b)
+        fq.fq_set_config(bits)
+        if len(out) == len(levels):
+            break
+        fq.fq_gemm(head.layer, x, y)
+        logprob, entropy, ids, tops = fq.fq_token_logprobs(y, head.targets, n_top=head.n_top, temperature=head.temperature)
+        if teacher is None:
+            # log probabilities at T: T times as much are logits (up to a constant of the row, which does not matter)
+            teacher = (ids, tops * head.temperature)
+        kl = fq.fq_distill_topk(y, *teacher, temperature=head.temperature)[0]
+        out.append((-logprob.double().sum() / asked, entropy.double().mean(), kl.double().mean()))
+    rows = torch.stack([torch.stack(o) for o in out]).tolist()
+    return [{"bits": int(b), "nll": n, "perplexity": math.inf if n >= 700.0 else math.exp(n), "entropy": e, "kl": k}
+            for b, (n, e, k) in zip(levels, rows)]
+
+
 def module_tables(fq: "F.FlexQ", shapes: Sequence, modules: Sequence[Sequence[int]], levels: Sequence[int],
-                  calib: Dict[int, torch.Tensor], sens_tokens: int):
+                  calib: Dict[int, torch.Tensor], sens_tokens: int, head: Optional[Head] = None):
     """cost, sens, foot tables [module][level] of a stack whose layers are nested (8-bit parents).
 
     shapes[i] has n_out / k_in; modules[j] lists the layers of module j; levels are bit-widths from n_up down
     to n_low; calib[k_in] is a bf16 [tokens][k_in] activation matrix.  cost uses every token, sens only the
-    first `sens_tokens` (the cheaper, pre-generated analysis of Sec. III-B)."""
+    first `sens_tokens` (the cheaper, pre-generated analysis of Sec. III-B).  `head`: that layer's error is the mean divergence of its
+    distribution from the tokens that levels[0] finds most likely."""
     L = len(shapes)
     n_lev = len(levels)
     err = [[None] * n_lev for _ in range(L)]
@@ -31,9 +74,12 @@ def module_tables(fq: "F.FlexQ", shapes: Sequence, modules: Sequence[Sequence[in
     fq.fq_set_config(cur)
     for i, sh in enumerate(shapes):
         x = calib[sh.k_in]
-        y_up = torch.empty((x.shape[0], sh.n_out), dtype=torch.bfloat16, device=x.device)
-        y = torch.empty_like(y_up)
+        y_up, y = (_outputs(x.shape[0], sh.n_out, x.device) for _ in range(2))
         fq.fq_gemm(i, x, y_up)
+        teacher = None
+        if head is not None and i == head.layer:
+            _, _, ids, tops = fq.fq_token_logprobs(y_up, head.targets, n_top=head.n_top, temperature=head.temperature)
+            teacher = (ids, tops * head.temperature)
         for li, b in enumerate(levels):
             if li == 0:
                 err[i][0] = err_s[i][0] = torch.zeros(2, dtype=torch.float64, device=x.device)
@@ -41,7 +87,12 @@ def module_tables(fq: "F.FlexQ", shapes: Sequence, modules: Sequence[Sequence[in
             cur[i] = int(b)
             fq.fq_set_config(cur)
             fq.fq_gemm(i, x, y)
-            err[i][li] = F.fq_sqdiff(y, y_up)
+            if teacher is not None:
+                kl = fq.fq_distill_topk(y, *teacher, temperature=head.temperature)[0].double()
+                err[i][li] = torch.stack((kl.sum(), torch.ones_like(kl).sum()))
+                err_s[i][li] = torch.stack((kl[:sens_tokens].sum(), torch.ones_like(kl[:sens_tokens]).sum()))
+                continue
+            err[i][li] = F.fq_sqdiff(y.contiguous(), y_up.contiguous())
             err_s[i][li] = F.fq_sqdiff(y[:sens_tokens].contiguous(), y_up[:sens_tokens].contiguous())
         cur[i] = int(levels[0])
         fq.fq_set_config(cur)
@@ -70,8 +121,8 @@ def chain_to_bits(chain: List[List[int]], modules: Sequence[Sequence[int]], leve
 
 
 def generate_ensemble(fq, shapes, modules, levels, calib, stems: int = 2, branches: int = 3, sens_tokens: int = 32,
-                      prune_fraction: float = 0.0):
-    cost, sens, foot = module_tables(fq, shapes, modules, levels, calib, sens_tokens)
+                      prune_fraction: float = 0.0, head: Optional[Head] = None):
+    cost, sens, foot = module_tables(fq, shapes, modules, levels, calib, sens_tokens, head)
     chain, curve = F.fq_search_chain(cost, sens, foot, stems, branches)
     pruned, dropped, before, after = F.fq_prune_chain(chain, len(levels), foot, prune_fraction)
     return {"cost": cost, "sens": sens, "foot": foot, "chain": chain, "curve": curve, "pruned_chain": pruned,
