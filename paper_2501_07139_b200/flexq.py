@@ -222,6 +222,7 @@ class FlexQ:
     def __init__(self, n_layers: int, device: int = 0):
         self._h = C.c_void_p()
         self.device = torch.device("cuda", device)
+        self._index = device
         _check(lib().fq_create(C.byref(self._h), device, n_layers), "fq_create")
         self.n_layers = n_layers
         self._keep = {}          # (layer, bits) -> stored variant retained by the context
@@ -395,14 +396,14 @@ class FlexQ:
     def _matrix(self, t: torch.Tensor, name: str, types) -> tuple:
         """(rows, columns, elements from one row to the next; of one row, any that the library takes)"""
         shape, st = t.shape, t.stride()
-        if len(shape) != 2 or t.dtype not in types or t.device != self.device or (st[1] != 1 and shape[1] > 1):
+        if len(shape) != 2 or t.dtype not in types or t.get_device() != self._index or (st[1] != 1 and shape[1] > 1):
             raise ValueError(f"{name}: a matrix of {', '.join(str(d) for d in types)} on {self.device} with dense rows is needed, not "
                              f"{t.dtype} {tuple(shape)} with strides {st} on {t.device}")
         rows, cols = shape
         return rows, cols, st[0] if rows > 1 else -(-cols // 16) * 16
 
     def _dense(self, t: torch.Tensor, name: str, types, shape: tuple) -> torch.Tensor:
-        if t.shape != shape or t.dtype not in types or t.device != self.device or not t.is_contiguous():
+        if t.shape != shape or t.dtype not in types or t.get_device() != self._index or not t.is_contiguous():
             raise ValueError(f"{name}: dense {shape} values of {', '.join(str(d) for d in types)} on {self.device} are needed, not "
                              f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
         return t
@@ -470,9 +471,10 @@ class FlexQ:
         if n_top < 0:
             raise ValueError("n_top is negative")
         if out is None:                                  # one allocation for all four
-            logprob, entropy, tops, ids = torch.empty(rows * (2 + 2 * n_top), dtype=torch.float32, device=self.device).split_with_sizes(
-                (rows, rows, rows * n_top, rows * n_top))
-            tops, ids = tops.view(rows, n_top), ids.view(torch.int32).view(rows, n_top)
+            all4 = torch.empty(rows * (2 + 2 * n_top), dtype=torch.float32, device=self.device)
+            logprob, entropy = all4.as_strided((rows,), (1,), 0), all4.as_strided((rows,), (1,), rows)
+            tops = all4.as_strided((rows, n_top), (n_top, 1), 2 * rows)
+            ids = all4.view(torch.int32).as_strided((rows, n_top), (n_top, 1), (2 + n_top) * rows)
         else:
             logprob, entropy, ids, tops = out
             self._dense(logprob, "logprob", _F32, (rows,))
@@ -509,8 +511,8 @@ class FlexQ:
         probabilities.  With `grad_loss` (fp32 [rows], upstream) the gradient with respect to the logits comes from the same call, into
         `grad` if that is given (it may be `logits`); without, fq_distill_topk_grad gives it later from `lse`."""
         rows, vocab, ld, n_top, grad, ldg = self._slots(logits, ids, teacher, grad_loss, grad)
-        lse, loss = torch.empty(3 * rows, dtype=torch.float32, device=self.device).split_with_sizes((2 * rows, rows))
-        lse = lse.view(rows, 2)
+        both = torch.empty(3 * rows, dtype=torch.float32, device=self.device)
+        lse, loss = both.as_strided((rows, 2), (2, 1), 0), both.as_strided((rows,), (1,), 2 * rows)
         _check(lib().fq_distill_topk(self._h, logits.data_ptr(), _TYPES[logits.dtype], rows, vocab, ld, ids.data_ptr(), ids.element_size(),
                                      teacher.data_ptr(), n_top, temperature, None if grad_loss is None else grad_loss.data_ptr(),
                                      loss.data_ptr(), lse.data_ptr(), None if grad is None else grad.data_ptr(), ldg,

@@ -57,7 +57,7 @@ def test_methods_name_what_does_not_fit():
     """The binding's own checks, on CPU tensors: a context without a device refuses them all."""
     import torch
     fq = P.FlexQ.__new__(P.FlexQ)
-    fq._h, fq.device = C.c_void_p(), torch.device("cuda", 0)
+    fq._h, fq.device, fq._index = C.c_void_p(), torch.device("cuda", 0), 0
     x = torch.zeros((2, 8), dtype=torch.float16)
     for call in (lambda: fq.fq_quantize_rows(x), lambda: fq.fq_token_logprobs(x, torch.zeros(2, dtype=torch.int64)),
                  lambda: fq.fq_distill_topk(x, torch.zeros((2, 3), dtype=torch.int32), torch.zeros((2, 3))),
