@@ -717,6 +717,7 @@ struct __align__(16) TeacherShared {
     float all[kMaxTop];                   // the probability of the slot's token, in all of its slots
     int at[kMaxTop];                      // where the token is in the buffer; -1: not there, or the token of an earlier slot
     int any, bad;
+    volatile int seen;
 };
 
 // The teacher's distribution over the warp's slots, kMaxTop / 32 to a lane: from logits (-inf: empty) to log probabilities, and probabilities.
@@ -875,6 +876,13 @@ __global__ void __launch_bounds__(THREADS + 32, 1024 / THREADS) distill_kernel(c
         if (lane == 0) {
             te.any = some;
             te.bad = bad;
+        }
+        if (o.grad == a.z) {
+            // in place: these logits have arrived before any warp's gradient leaves
+            bool seen = false;
+#pragma unroll
+            for (int i = 0; i < kPer; i++) seen |= Group<T>::to_f(z_id[i]) > 0.0f;
+            te.seen = __any_sync(0xffffffffu, seen);
         }
     } else {
         await_slice(sh, a);
@@ -1037,7 +1045,7 @@ int check_rows(const fq_ctx* ctx, const void* logits, int dtype, int rows, int v
 {
     const int size = type_size(dtype);
     if (!ctx || !logits || !size || (id_bytes != 4 && id_bytes != 8)) return FQ_ERR_ARG;
-    if (!(temperature > 0.0f) || std::isinf(temperature)) return FQ_ERR_ARG;
+    if (!(temperature >= 1e-30f && temperature <= 1e30f)) return FQ_ERR_ARG;
     if (rows < 1 || rows > FQ_MAX_ROWS || vocab < 1 || vocab > FQ_MAX_VOCAB || ld < vocab || n_top < 0 || n_top > FQ_MAX_TOP) return FQ_ERR_SHAPE;
     if (!aligned(logits, (size_t)size)) return FQ_ERR_ALIGN;
     return FQ_OK;

@@ -25,7 +25,7 @@ GRAD = dict(ctx=CTX, z=BUF, dtype=BF16, rows=4, vocab=100, ld=100, ids=BUF, id_b
 
 ROWS = [("rows", 0, SHAPE), ("rows", -1, SHAPE), ("rows", (1 << 20) + 1, SHAPE), ("vocab", 0, SHAPE), ("vocab", P.FQ_MAX_VOCAB + 1, SHAPE),
         ("ld", 99, SHAPE), ("z", 0, ARG), ("z", BUF + 1, ALIGN), ("dtype", 3, ARG), ("dtype", -1, ARG), ("id_bytes", 2, ARG), ("t", 0.0, ARG),
-        ("t", -1.0, ARG), ("t", float("inf"), ARG), ("t", float("nan"), ARG), ("n_top", 129, SHAPE), ("ctx", None, ARG)]
+        ("t", -1.0, ARG), ("t", float("inf"), ARG), ("t", float("nan"), ARG), ("t", 1e-31, ARG), ("t", 1e31, ARG), ("n_top", 129, SHAPE), ("ctx", None, ARG)]
 SLOTS = [("ids", 0, ARG), ("ids", BUF + 2, ALIGN), ("teacher", 0, ARG), ("teacher", BUF + 2, ALIGN), ("n_top", 0, SHAPE), ("lse", 0, ARG),
          ("lse", BUF + 4, ALIGN), ("grad", BUF + 1, ALIGN), ("ldg", 99, SHAPE), ("g", 0, ARG), ("g", BUF + 1, ALIGN)]
 WEIGHTS = [("m", 0, SHAPE), ("m", (1 << 20) + 1, SHAPE), ("n", 0, SHAPE), ("k", 0, SHAPE), ("k", 131072, SHAPE), ("ldw", 32, SHAPE),
