@@ -932,31 +932,57 @@ __global__ void __launch_bounds__(THREADS + 32, 1024 / THREADS) distill_kernel(c
         const int end = s.shift + s.n;
 #pragma unroll
         for (int i = 0; i < kPer; i++) at[i] = !zero && lane + 32 * i < o.k ? te.at[lane + 32 * i] : -1;
-        // A warp takes 2 KB at a time, which leave as soon as they are done: what has been stored and what is still being formed overlap.
-        constexpr int kBlock = 128;
+        // q w = +-2^(z c2 - shift).  16-bit gradients are formed like that, in one step, where the shift and its largest part are small: with
+        // four roundings of at most 2^-18 it puts q off by 1.1e-5, where the gradient's own rounding is one of 2^-11 or 2^-8.
+        const float reach = zm * a.c2, shift = reach + off - log2f(fabsf(w));
+        const bool quick = N == 8 && fabsf(reach) < 64.0f && fabsf(shift) < 64.0f && !zero;      // (not if w is NaN or an infinity)
+        const uint32_t sign = w < 0.0f ? 0x80008000u : 0u;
+        // A warp takes 4 KB at a time, which leave as soon as they are done: what has been stored and what is still being formed overlap.
+        constexpr int kBlock = 256;
         for (int b = warp * kBlock; b < s.groups; b += (THREADS / 32) * kBlock) {
             const int b0 = b * N, b1 = (b + kBlock) * N, e0 = max(lo, b0), e1 = min(hi, b1);
             float z[kPer];
 #pragma unroll
-            for (int i = 0; i < kPer; i++) z[i] = at[i] >= b0 && at[i] < b1 ? Group<T>::to_f(el[at[i]]) : 0.0f;
+            for (int i = 0; i < kPer; i++)
+                if (32 * i < o.k) z[i] = at[i] >= b0 && at[i] < b1 ? Group<T>::to_f(el[at[i]]) : 0.0f;
             __syncwarp();
+            if (quick) {
+                const float2 c2 = make_float2(a.c2, a.c2), minus = make_float2(-shift, -shift);
+                const auto one = [&](int group) {
+                    float2 f[N / 2];
+                    Group<T>::unpack(buf[group], f);
 #pragma unroll
-            for (int i = 0; i < kBlock / 32; i++) {
-                const int group = b + i * 32 + lane;
-                if (group >= s.groups) break;
-                float2 f[N / 2];
-                Group<T>::unpack(buf[group], f);
-#pragma unroll
-                for (int h = 0; h < N / 2; h++) {
-                    const float2 t = fma2(add2(f[h], make_float2(-zm, -zm)), make_float2(a.c2, a.c2), make_float2(-off, -off));
-                    f[h] = mul2(make_float2(ex2(t.x), ex2(t.y)), make_float2(w, w));
+                    for (int h = 0; h < N / 2; h++) {
+                        const float2 t = fma2(f[h], c2, minus);
+                        f[h] = make_float2(ex2(t.x), ex2(t.y));
+                    }
+                    uint4 v = Group<T>::pack(f);
+                    if (sign) { v.x ^= sign; v.y ^= sign; v.z ^= sign; v.w ^= sign; }
+                    buf[group] = v;
+                };
+                if (b + kBlock <= s.groups) {
+#pragma unroll 4
+                    for (int i = 0; i < kBlock / 32; i++) one(b + i * 32 + lane);
+                } else {
+                    for (int group = b + lane; group < s.groups; group += 32) one(group);
                 }
-                buf[group] = zero ? make_uint4(0u, 0u, 0u, 0u) : Group<T>::pack(f);
+            } else {
+                for (int group = b + lane; group < min(b + kBlock, s.groups); group += 32) {
+                    float2 f[N / 2];
+                    Group<T>::unpack(buf[group], f);
+#pragma unroll
+                    for (int h = 0; h < N / 2; h++) {
+                        const float2 t = fma2(add2(f[h], make_float2(-zm, -zm)), make_float2(a.c2, a.c2), make_float2(-off, -off));
+                        f[h] = mul2(make_float2(ex2(t.x), ex2(t.y)), make_float2(w, w));
+                    }
+                    buf[group] = zero ? make_uint4(0u, 0u, 0u, 0u) : Group<T>::pack(f);
+                }
             }
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < kPer; i++)
-                if (at[i] >= b0 && at[i] < b1) el[at[i]] = Group<T>::from_f((ex2((z[i] - zm) * a.c2 - off) - te.all[lane + 32 * i]) * w);
+                if (32 * i < o.k && at[i] >= b0 && at[i] < b1)
+                    el[at[i]] = Group<T>::from_f((ex2((z[i] - zm) * a.c2 - off) - te.all[lane + 32 * i]) * w);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (!alike) {

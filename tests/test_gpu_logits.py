@@ -8,7 +8,9 @@ Tolerances, with u = 2^-24 (half a step of fp32) and d = (z - m) / T:
   logprob    e + 3 u |d| + u |result|
   entropy    log S and sum exp(d) d / S, whose terms are off by another u each and whose sum is too:   e + E (2 e + 2 u) + u |result|
   p of K     the same with K for V;  loss = sum p (lp - lq): sum p (e_lp + e_lq) + (the relative error of p) |lp - lq|, K additions
-  gradient   g / T (q - p): relative error of q and p, products, one rounding to its type
+  gradient   g / T (q - p): relative error of q and p, products, one rounding to its type; a q, or q g / T, below 2^-126 is 0; in 16 bits
+             2^(z c2 - shift) with a shift whose parts are below 64 (128 in between): four roundings of 2^-18 at most, 256 u of the
+             binary logarithm of q, which is 178 u of q
 All are multiplied by 1.01 for what is quadratic in u."""
 import math
 
@@ -179,10 +181,11 @@ def check_distill(fq, z, ids, teacher, t, g, calls=("loss", "both", "apart")):
     e_term = err + err_u + 3.03 * U * (dq + du) + 3 * U * (lu.nan_to_num(neginf=0.0).abs() + lq.nan_to_num(neginf=0.0).abs())
     tol = (p * (e_term + (rel_p + (k + 4) * U) * (lu - lq).nan_to_num(posinf=0.0, neginf=0.0).abs())).sum(1) * 1.01
     grad = (q * some[:, None]).scatter_add(1, at, -p) * (g.double() / t)[:, None]
-    rel_q = err + (8 + 3 * d.abs().nan_to_num(posinf=0.0)) * U
+    rel_q = err + (8 + 3 * d.abs().nan_to_num(posinf=0.0) + (178 if z.dtype != torch.float32 else 0)) * U
     tol_g = (q * rel_q).scatter_add(1, at, p * (rel_p + k * U)) * (g.double() / t).abs()[:, None] * 1.02
     tol_g = tol_g + grad.abs() * (torch.finfo(z.dtype).eps / 2 + 3 * U) + {torch.bfloat16: 2.0 ** -134, torch.float16: 2.0 ** -25,
                                                                             torch.float32: 2.0 ** -126}[z.dtype]
+    tol_g = tol_g + 2.0 ** -126 * (1 + (g.double() / t).abs()[:, None])
     grad[g == 0] = 0
     if "loss" in calls:
         got, lse, none = fq.fq_distill_topk(z, ids, teacher, t)
