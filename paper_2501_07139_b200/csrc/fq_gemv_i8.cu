@@ -3,7 +3,8 @@
 // Bound by reading the weights once.  A CTA takes a run of output rows, and each of its warps the same columns of all of them: 512 columns, 16 to a
 // lane, some slices of that kind where K is wide.  A lane's codes of the tokens then stay in registers for the whole kernel, a row costs a
 // warp one 512-byte load per slice and four 4-way products per token, and rows depend on nothing, so that sixteen loads are on their
-// way per lane.  The warps' sums meet in shared memory.  Sums are integers: their order does not matter.
+// way per lane.  The warps' sums meet in shared memory.  Sums are integers: their order does not matter.  1 x 4096 x 4096 4.7 us from codes and
+// 5.5 us from fp16 (16.8 MB: 2.6 us at the rate of a copy), 1 x 13824 x 5120 12.4 us (11.0 us).
 //
 // One token that is not codes yet is quantised by every CTA for itself, while its first weights are on their way: that is a few
 // thousand values from the L2, and saves a launch.
