@@ -433,19 +433,37 @@ __device__ __forceinline__ int bin_of_kth(const int* bins, int k, At&& at, int& 
 template <class T, int THREADS>
 __device__ __noinline__ void exact_candidates(const Stream<T>& x, int k, TopShared<THREADS>& sh)
 {
-    constexpr int N = Group<T>::N;
+    constexpr int N = Group<T>::N, U = 4;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const auto each_group = [&](auto&& fn) {                           // (some loads on their way at a time)
+        for (int i = threadIdx.x; i < x.s.groups; i += U * THREADS) {
+            uint4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; u++) v[u] = i + u * THREADS < x.s.groups ? x.any(i + u * THREADS) : Group<T>::fill();
+#pragma unroll 1
+            for (int u = 0; u < U; u++) {
+                fn(i + u * THREADS, v[0]);
+                v[0] = v[1]; v[1] = v[2]; v[2] = v[3];
+            }
+        }
+    };
     uint32_t kth = 0;
     int need = k;                                                      // of the entries whose upper digits are those of kth
     for (int d = 24; d >= 0; d -= 8) {
+        if (d + 8 <= 32 - Group<T>::kKeyBits) {                        // digits that all keys of a sign share
+            kth |= kth >> 31 ? 0u : 255u << d;
+            continue;
+        }
         __syncthreads();
         for (int i = threadIdx.x; i < 256; i += THREADS) sh.bins[i] = 0;
         __syncthreads();
         int digit = 0, run = 0;                                        // alike entries in a row are counted before they are added
-        for (int i = threadIdx.x; i < x.s.groups; i += THREADS) {
-            const uint4 v = x.any(i);
+        each_group([&](int, const uint4& v) {
+            float2 f[N / 2];
+            Group<T>::unpack(v, f);
+#pragma unroll
             for (int e = 0; e < N; e++) {
-                const float z = Group<T>::to_f(reinterpret_cast<const T*>(&v)[e]);
+                const float z = e & 1 ? f[e / 2].y : f[e / 2].x;
                 const uint32_t key = key_of(z);
                 if (!(z > kNegInf) || (d < 24 && (key ^ kth) >> (d + 8))) continue;
                 const int now = (int)(key >> d & 255u);
@@ -453,7 +471,7 @@ __device__ __noinline__ void exact_candidates(const Stream<T>& x, int k, TopShar
                 digit = now;
                 run++;
             }
-        }
+        });
         if (run) atomicAdd(&sh.bins[digit], run);
         __syncthreads();
         int above = 0;
@@ -464,26 +482,34 @@ __device__ __noinline__ void exact_candidates(const Stream<T>& x, int k, TopShar
     __syncthreads();
     if (threadIdx.x == 0) sh.n_cand = 0;
     __syncthreads();
-    // those above it, fewer than k, in any order; its bearers, in order, until there are enough
-    int taken = 0;
-    for (int i0 = 0; i0 < x.s.groups; i0 += THREADS) {
+    const auto add = [&](uint32_t key, int group, int e) {
+        const int at = atomicAdd(&sh.n_cand, 1);
+        if (at < kCandidates) sh.cand[at] = entry_word(key, x.s.first + group * N + e - x.s.shift);
+    };
+    // those above it, fewer than k, in any order
+    if (need < k)
+        each_group([&](int group, const uint4& v) {
+            float2 f[N / 2];
+            Group<T>::unpack(v, f);
+#pragma unroll
+            for (int e = 0; e < N; e++) {
+                const float z = e & 1 ? f[e / 2].y : f[e / 2].x;
+                if (z > kNegInf && key_of(z) > kth) add(key_of(z), group, e);
+            }
+        });
+    // its bearers, in order, until there are enough
+    for (int i0 = 0, taken = 0; i0 < x.s.groups && taken < need; i0 += THREADS) {
         const int i = i0 + threadIdx.x;
         unsigned bearers = 0;
-        uint4 v = Group<T>::fill();
         if (i < x.s.groups) {
-            v = x.any(i);
+            float2 f[N / 2];
+            Group<T>::unpack(x.any(i), f);
+#pragma unroll
             for (int e = 0; e < N; e++) {
-                const float z = Group<T>::to_f(reinterpret_cast<const T*>(&v)[e]);
-                if (!(z > kNegInf)) continue;
-                const uint32_t key = key_of(z);
-                if (key == kth) bearers |= 1u << e;
-                if (key > kth) {
-                    const int at = atomicAdd(&sh.n_cand, 1);
-                    if (at < kCandidates) sh.cand[at] = entry_word(key, x.s.first + i * N + e - x.s.shift);
-                }
+                const float z = e & 1 ? f[e / 2].y : f[e / 2].x;
+                if (z > kNegInf && key_of(z) == kth) bearers |= 1u << e;
             }
         }
-        if (taken >= need) continue;                                   // (the same for all threads)
         int upto = __popc(bearers);
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -499,10 +525,7 @@ __device__ __noinline__ void exact_candidates(const Stream<T>& x, int k, TopShar
         }
         before += upto - __popc(bearers);
         for (; bearers; bearers &= bearers - 1, before++)
-            if (before < need) {
-                const int at = atomicAdd(&sh.n_cand, 1);
-                if (at < kCandidates) sh.cand[at] = entry_word(kth, x.s.first + i * N + __ffs((int)bearers) - 1 - x.s.shift);
-            }
+            if (before < need) add(kth, i, __ffs((int)bearers) - 1);
         taken += all;
         __syncthreads();
     }
@@ -537,6 +560,7 @@ __device__ __forceinline__ int slice_top(const Stream<T>& x, int k, uint32_t my_
     const int rounds = (x.hi - x.lo + THREADS - 1) / THREADS, turns = (rounds + kSlots * kBatch - 1) / (kSlots * kBatch);
     const int bits = kBatchBits + (turns > 1 ? 32 - __clz(turns - 1) : 0), items = sh.n_pieces << bits;
     for (int i = threadIdx.x; i < items + 2; i += THREADS) {           // and the two groups at the ends
+        if (*const_cast<volatile int*>(&sh.n_cand) > kCandidates) break;
         int group;
         if (i < items) {
             const int piece = sh.piece[i >> bits], part = i & ((1 << bits) - 1);

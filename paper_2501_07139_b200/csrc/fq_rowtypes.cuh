@@ -45,6 +45,7 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
 template <class T> struct Group;
 template <> struct Group<float> {
     static constexpr int N = 4;
+    static constexpr int kKeyBits = 32;          // upper bits of a value, as a float, that tell it from others of its sign
     static __device__ __forceinline__ void unpack(const uint4& v, float2 (&f)[2])
     {
         f[0] = make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
@@ -74,6 +75,7 @@ template <> struct Group<float> {
 };
 template <> struct Group<__nv_bfloat16> {
     static constexpr int N = 8;
+    static constexpr int kKeyBits = 16;
     static __device__ __forceinline__ void unpack(const uint4& v, float2 (&f)[4])
     {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -122,6 +124,7 @@ template <> struct Group<__nv_bfloat16> {
 };
 template <> struct Group<__half> {
     static constexpr int N = 8;
+    static constexpr int kKeyBits = 19;
     static __device__ __forceinline__ void unpack(const uint4& v, float2 (&f)[4])
     {
         const __half2* h = reinterpret_cast<const __half2*>(&v);
