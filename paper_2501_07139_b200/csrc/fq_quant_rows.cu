@@ -3,6 +3,8 @@
 // A code is that of the exact quotient: in fp32 alone a value next to the border between two codes could fall on either side, and
 // 127 x / a does meet borders (x = a / 2 is 63.5; among 4096 bf16 values some seven are).  x times a little inexact 127 / a is off by at most
 // 3.1e-5; where it is closer than 5e-5 to a border, the side is settled by the exact sign of 127 x - border a.
+#include <algorithm>
+
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -54,14 +56,15 @@ __global__ void __launch_bounds__(THREADS) quantize_rows_kernel(const QuantArgs 
 }
 
 // Rows that stay in registers, U pieces of 8 values to a thread: pieces are 16-byte aligned on both sides, and there is a whole number of them.
-// A CTA goes from row to row, the next one on its way while one is worked on.  (8192 x 4096 bf16: 39 us with a CTA for every row.)
-template <class T, int THREADS, int U>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) quantize_rows_kept_kernel(const QuantArgs a)
+// Many rows: four pieces, so that a row's maximum, two reductions and a reciprocal, is shared by 32 values of a thread (8192 x 4096 bf16 27.5 us,
+// with one piece a thread 45 us; the next row on its way while one is worked on gains nothing).  Few rows: one or two, for the latency.
+template <class T, int U>
+__global__ void __launch_bounds__(1024, 1) quantize_rows_kept_kernel(const QuantArgs a)
 {
-    __shared__ float red[2][THREADS / 32];
+    __shared__ float red[2][32];
     constexpr int G = 8 / Group<T>::N;                   // 16-byte groups of a piece
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int pieces = a.cols / 8;
+    const int pieces = a.cols / 8, threads = blockDim.x, lane = threadIdx.x & 31, warps = threads >> 5;
     const auto load = [&](uint4 (&v)[U][G], int r) {
         const T* x = static_cast<const T*>(a.x) + (long long)r * a.ldx;
 #pragma unroll
@@ -69,7 +72,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) quantize_rows_kept_ke
 #pragma unroll
             for (int g = 0; g < G; g++) {
                 v[u][g] = make_uint4(0u, 0u, 0u, 0u);
-                const int p = u * THREADS + threadIdx.x;
+                const int p = u * threads + threadIdx.x;
                 if (p < pieces && r < a.rows) v[u][g] = *reinterpret_cast<const uint4*>(x + p * 8 + g * Group<T>::N);
             }
     };
@@ -77,19 +80,20 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) quantize_rows_kept_ke
     load(v, (int)blockIdx.x);
     int turn = 0;
     for (int r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
-        uint4 next[U][G];
-        load(next, r + (int)gridDim.x);
         typename Group<T>::Max most = Group<T>::nothing();
 #pragma unroll
         for (int u = 0; u < U; u++)
 #pragma unroll
             for (int g = 0; g < G; g++) Group<T>::take_abs(most, v[u][g]);
-        const float m = block_max<THREADS>(Group<T>::of_abs(most), red[turn]);
+        float m = warp_max_nan(Group<T>::of_abs(most));
+        if (lane == 0) red[turn][threadIdx.x >> 5] = m;
+        __syncthreads();                                 // (a warp writes to the other half next, which all have left by then)
+        m = warp_max_nan(lane < warps ? red[turn][lane] : 0.0f);
         const RowScale s(m);
         int8_t* q = a.codes + (long long)r * a.ldc;
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            const int p = u * THREADS + threadIdx.x;
+            const int p = u * threads + threadIdx.x;
             uint32_t w[2];
 #pragma unroll
             for (int g = 0; g < G; g++) {
@@ -102,32 +106,29 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) quantize_rows_kept_ke
             if (p < pieces) *reinterpret_cast<uint2*>(q + p * 8) = make_uint2(w[0], w[1]);
         }
         if (threadIdx.x == 0) a.scales[r] = RowScale::scale(m);
-#pragma unroll
-        for (int u = 0; u < U; u++)
-#pragma unroll
-            for (int g = 0; g < G; g++) v[u][g] = next[u][g];
+        if (r + (int)gridDim.x < a.rows) load(v, r + (int)gridDim.x);
     }
 }
 
-template <class T, int THREADS>
-int launch_threads(const QuantArgs& a, int sm_count, cudaStream_t st)
+template <class T, int U>
+int launch_kept(const QuantArgs& a, int sm_count, cudaStream_t st)
 {
-    const int per_thread = (a.cols / 8 + THREADS - 1) / THREADS, grid = a.rows < sm_count * (1024 / THREADS) ? a.rows : sm_count * (1024 / THREADS);
-    const bool pieces = a.cols % 8 == 0 && aligned(a.x, 16) && a.ldx * sizeof(T) % 16 == 0 && aligned(a.codes, 8) && a.ldc % 8 == 0;
-    if (pieces && per_thread <= 1) quantize_rows_kept_kernel<T, THREADS, 1><<<(unsigned)grid, THREADS, 0, st>>>(a);
-    else if (pieces && per_thread <= 2) quantize_rows_kept_kernel<T, THREADS, 2><<<(unsigned)grid, THREADS, 0, st>>>(a);
-    else quantize_rows_kernel<T, THREADS><<<(unsigned)a.rows, THREADS, 0, st>>>(a);
+    const int pieces = a.cols / 8, threads = std::max(32, ((pieces + U - 1) / U + 31) / 32 * 32);
+    const int most = sm_count * (1024 / threads);
+    quantize_rows_kept_kernel<T, U><<<(unsigned)std::min(a.rows, most), threads, 0, st>>>(a);
     return cudaGetLastError() == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
 }
 
-// A thread has one or two pieces of a row: few rows get more threads each, many of them only as many as it takes.
 template <class T>
 int launch_typed(const QuantArgs& a, int sm_count, cudaStream_t st)
 {
-    if (a.cols > 8192 || (a.cols > 2048 && a.rows <= sm_count)) return launch_threads<T, 1024>(a, sm_count, st);
-    if (a.cols > 4096) return launch_threads<T, 512>(a, sm_count, st);
-    if (a.cols > 2048) return launch_threads<T, 256>(a, sm_count, st);
-    return launch_threads<T, 128>(a, sm_count, st);
+    const int pieces = a.cols / 8;
+    const bool kept = a.cols % 8 == 0 && aligned(a.x, 16) && a.ldx * sizeof(T) % 16 == 0 && aligned(a.codes, 8) && a.ldc % 8 == 0;
+    if (kept && a.rows <= sm_count && pieces <= 1024) return launch_kept<T, 1>(a, sm_count, st);
+    if (kept && a.rows <= sm_count && pieces <= 2048) return launch_kept<T, 2>(a, sm_count, st);
+    if (kept && pieces <= 4096) return launch_kept<T, 4>(a, sm_count, st);
+    quantize_rows_kernel<T, 256><<<(unsigned)a.rows, 256, 0, st>>>(a);
+    return cudaGetLastError() == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
 }
 
 }  // namespace
