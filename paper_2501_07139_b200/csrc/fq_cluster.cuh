@@ -34,12 +34,6 @@ __device__ __forceinline__ float cluster_ld_f32(uint32_t addr)
     asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
     return v;
 }
-__device__ __forceinline__ int cluster_ld_s32(uint32_t addr)
-{
-    int v;
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-    return v;
-}
 __device__ __forceinline__ int4 cluster_ld_s32x4(uint32_t addr)
 {
     int4 v;

@@ -25,16 +25,17 @@ namespace {
 constexpr int kBM = 128;                 // tokens per CTA (UMMA M = 256 over the pair)
 constexpr int kBN = 256;                 // outputs per tile, at most (UMMA N)
 constexpr int kBK = 128;                 // K per stage: one 128-byte swizzle span
-constexpr int kStages = 6;
+constexpr int kMaxStages = 8;
 constexpr int kThreads = 192;            // warp 0: TMA, warp 1: TMEM owner, of the leading CTA also MMA; warps 2..5: epilogue
 constexpr int kTmemCols = 512;           // two accumulators of up to kBN columns
 
+// A stage holds 128 tokens and half of the tile's outputs: six stages of 256 outputs, seven or eight of fewer, where a tile's time is that of
+// its loads more than that of its products (512 x 4096 x 4096, 128 outputs: 15.7 us with six stages, 15.0 us with eight).
 struct PairSmem {
     static constexpr int kABytes = kBM * kBK;                      // 16 KB
-    static constexpr int kBBytes = kBN / 2 * kBK;                  // 16 KB
-    static constexpr int kStageBytes = kABytes + kBBytes;
-    static constexpr int oBars = kStages * kStageBytes;            // full[S], empty[S], tmem_full[2], tmem_empty[2]
-    static constexpr int oTmemPtr = oBars + (2 * kStages + 4) * 8;
+    static constexpr int kTiles = 6 * (kABytes + kBN / 2 * kBK);   // 192 KB
+    static constexpr int oBars = kTiles;                           // full[S], empty[S], tmem_full[2], tmem_empty[2]
+    static constexpr int oTmemPtr = oBars + (2 * kMaxStages + 4) * 8;
     static constexpr int oFlag = oTmemPtr + 8;
     static constexpr int kTotal = oFlag + 8 + 1024;                // + slack for the 1024-byte alignment of the tiles
 };
@@ -130,13 +131,15 @@ gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     const int rank = (int)cluster_rank(), pair = (int)(blockIdx.x >> 1), n_pairs = (int)(gridDim.x >> 1);
     const uint32_t bars = g_smem_u32(smem + PairSmem::oBars);
     // a stage's "full" and an accumulator's "empty" barriers are those of the leading CTA, the others exist in both
-    const uint32_t full0 = bars, empty0 = bars + 8 * kStages;
-    const uint32_t tfull0 = bars + 16 * kStages, tempty0 = tfull0 + 16;
+    const uint32_t full0 = bars, empty0 = bars + 8 * kMaxStages;
+    const uint32_t tfull0 = bars + 16 * kMaxStages, tempty0 = tfull0 + 16;
+    const int tile_n = a.tile_n, stage_bytes = PairSmem::kABytes + tile_n / 2 * kBK;
+    const int stages = min(kMaxStages, PairSmem::kTiles / stage_bytes);
     volatile uint32_t* tmem_ptr = reinterpret_cast<volatile uint32_t*>(smem + PairSmem::oTmemPtr);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + PairSmem::oFlag);
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; s++) {
+        for (int s = 0; s < stages; s++) {
             mbar_init(full0 + 8 * s, 1);
             mbar_init(empty0 + 8 * s, 1);
         }
@@ -160,7 +163,6 @@ gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     const uint32_t tmem_base = *tmem_ptr;
     asm volatile("griddepcontrol.wait;" ::: "memory");                  // the codes are the previous kernel's output
 
-    const int tile_n = a.tile_n;
     const int m_blocks = (a.M + 2 * kBM - 1) / (2 * kBM), n_blocks = (a.N + tile_n - 1) / tile_n;
     const int n_tiles = m_blocks * n_blocks;
     const int k_steps = (a.K + kBK - 1) / kBK;
@@ -168,7 +170,7 @@ gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     if (warp == 0) {
         // ================================================================== TMA producer
         if (lane == 0) {
-            const uint32_t bytes = 2u * (uint32_t)(PairSmem::kABytes + tile_n / 2 * kBK);        // of both CTAs
+            const uint32_t bytes = 2u * (uint32_t)stage_bytes;        // of both CTAs
             int stage = 0;
             uint32_t wraps = 0;
             bool ok = true;
@@ -177,11 +179,11 @@ gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                 for (int ks = 0; ks < k_steps; ks++) {
                     if (wraps > 0 && !g_wait(empty0 + 8 * stage, (wraps - 1u) & 1u, abort_flag)) { ok = false; break; }
                     const uint32_t full = in_leader(full0 + 8 * stage);
-                    const uint32_t a_dst = g_smem_u32(smem + stage * PairSmem::kStageBytes);
+                    const uint32_t a_dst = g_smem_u32(smem + stage * stage_bytes);
                     if (rank == 0) mbar_expect_tx(full0 + 8 * stage, bytes);
                     tma_load_pair(a_dst, &map_x, ks * kBK, mb * (2 * kBM) + rank * kBM, full);
                     tma_load_pair(a_dst + PairSmem::kABytes, &map_w, ks * kBK, nb * tile_n + rank * (tile_n / 2), full);
-                    if (++stage == kStages) { stage = 0; wraps++; }
+                    if (++stage == stages) { stage = 0; wraps++; }
                 }
             }
             if (!ok) { atomicCAS(a.status, 0, FQ_ERR_TIMEOUT); *abort_flag = 1; }
@@ -206,7 +208,7 @@ gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                     ok = __all_sync(0xffffffffu, g_wait(full0 + 8 * stage, wraps & 1u, abort_flag));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t step = (uint64_t)(stage * (PairSmem::kStageBytes >> 4));
+                    const uint64_t step = (uint64_t)(uint32_t)(stage * (stage_bytes >> 4));
                     const uint32_t more = ks > 0 ? 1u : 0u;
                     if (elect_one()) {
 #pragma unroll
@@ -220,7 +222,7 @@ gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                         commit_pair(empty0 + 8 * stage);               // the stage may be refilled once these MMAs have read it
                     }
                     __syncwarp();
-                    if (++stage == kStages) { stage = 0; wraps++; }
+                    if (++stage == stages) { stage = 0; wraps++; }
                 }
                 if (!ok) break;
                 if (elect_one()) commit_pair(tfull0 + 8 * buf);
