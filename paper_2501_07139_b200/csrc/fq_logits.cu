@@ -101,7 +101,8 @@ __device__ __forceinline__ Slice slice_of(const RowArgs& a, const T* row, int ra
     return s;
 }
 
-// Starts the copies and fills the ends.  (A barrier for every 16 KB, so that sums start with the first, gains nothing.)  The caller synchronises the CTA, then waits for `bar`.
+// Starts the copies and fills the ends.  The caller synchronises the CTA, then waits for `bar`.  (A barrier for every 16 KB, so that
+// sums start with the first, gains nothing.)
 template <class T>
 __device__ __forceinline__ void fetch_slice(const T* row, const Slice& s, uint4* buf, uint32_t bar)
 {
