@@ -285,30 +285,49 @@ struct Running {
         // all the same, at half the cost of doing so with the scaled differences.
         const float floor2 = (Group<T>::kFloor - mm) * c2;
         if (ENTROPY && Group<T>::N == 8 && floor2 < -160.0f && floor2 > -1e37f) {
+            uint4 w[G];
 #pragma unroll
-            for (int g = 0; g < G; g++) add<false>(Group<T>::above_floor(v[g]), mm, c2);
+            for (int g = 0; g < G; g++) w[g] = Group<T>::above_floor(v[g]);
+            add<false>(w, mm, c2);
         } else {
-#pragma unroll
-            for (int g = 0; g < G; g++) add<ENTROPY>(v[g], mm, c2);
+            add<ENTROPY>(v, mm, c2);
         }
         return here;
     }
-    template <bool CLAMP>
-    __device__ __forceinline__ void add(const uint4& v, float mm, float c2)
+    // A batch is added up before it is added to the sums: a long row takes a thread vocab / 2048 (fp32) or vocab / 4096 additions to them instead
+    // of vocab / 256, which round alike where terms are (393216 equal ones: a log probability off by 13 of 2^-24 instead of 371).  Within it pairwise, or one by one
+    // beside the entropy's products (pairwise there too: 4094 x 32000 bf16 67.8 us instead of 66.3 us).
+    template <bool CLAMP, int G>
+    __device__ __forceinline__ void add(const uint4 (&v)[G], float mm, float c2)
     {
-        float2 f[Group<T>::N / 2];
-        Group<T>::unpack(v, f);
+        float2 batch, batch1;
 #pragma unroll
-        for (int p = 0; p < Group<T>::N / 2; p++) {
-            float2 t = scaled2(f[p], mm, c2);
-            if (CLAMP) {                                         // (exp(-160 ln 2) is 0 in 32 bits)
-                t.x = max_nan(t.x, -160.0f);
-                t.y = max_nan(t.y, -160.0f);
+        for (int g = 0; g < G; g++) {
+            float2 f[Group<T>::N / 2];
+            Group<T>::unpack(v[g], f);
+#pragma unroll
+            for (int p = 0; p < Group<T>::N / 2; p++) {
+                float2 t = scaled2(f[p], mm, c2);
+                if (CLAMP) {                                     // (exp(-160 ln 2) is 0 in 32 bits)
+                    t.x = max_nan(t.x, -160.0f);
+                    t.y = max_nan(t.y, -160.0f);
+                }
+                f[p] = make_float2(ex2(t.x), ex2(t.y));
+                if (ENTROPY) {
+                    batch = g + p == 0 ? f[p] : add2(batch, f[p]);
+                    batch1 = g + p == 0 ? mul2(f[p], t) : fma2(f[p], t, batch1);
+                }
             }
-            const float2 e = make_float2(ex2(t.x), ex2(t.y));
-            s = add2(s, e);
-            if (ENTROPY) s1 = fma2(e, t, s1);
+            if (!ENTROPY) {
+#pragma unroll
+                for (int n = Group<T>::N / 4; n > 0; n /= 2)
+#pragma unroll
+                    for (int p = 0; p < n; p++) f[p] = add2(f[p], f[p + n]);
+                batch = g == 0 ? f[0] : add2(batch, f[0]);
+            }
         }
+        s = add2(s, batch);
+        if (ENTROPY) s1 = add2(s1, batch1);
     }
     __device__ __forceinline__ RowSums sums() const { return RowSums{m, s.x + s.y, ENTROPY ? s1.x + s1.y : 0.0f}; }
 };
