@@ -344,8 +344,9 @@ int fq_token_logprobs(fq_ctx* ctx, const void* logits_dev, int dtype, int rows, 
 
 /* Distillation from a teacher's top logits: with p = softmax(teacher / T) over a row's slots and q = softmax(z / T) over its whole vocabulary,
  *   loss = sum_j p_j (log p_j - log q_[ids_j]),     d loss / d z_i = (q_i - sum_{j: ids_j = i} p_j) / T.
- * A slot whose id is negative or whose teacher logit is -inf is empty; ids may repeat (their p add up).  A row without a slot: loss 0,
- * gradient 0.  A slot on a logit of -inf: loss +inf.  An id >= vocab: loss NaN, gradient NaN.  A row that holds a NaN or +inf: NaN.
+ * A slot whose id is negative or whose teacher logit is -inf is empty, whatever else it holds; ids may repeat (their p add up).  A row
+ * without a slot: loss 0, gradient 0.  A slot on a logit of -inf: loss +inf.  An id >= vocab: loss NaN, gradient NaN.  A row that holds a NaN
+ * or +inf: NaN.
  * A row of nothing but -inf has q = 0.  A q, or a gradient's q times its weight, below 2^-126 counts as 0.
  *   logits_dev, tokens as in fq_token_logprobs;  ids_dev int32 or int64, teacher_dev float [rows][n_top], 1 <= n_top <= FQ_MAX_TOP;
  *   grad_loss_dev float [rows]: upstream gradient of every row's loss (a row whose is 0 gets a gradient of 0 whatever it holds);

@@ -814,7 +814,7 @@ __device__ __forceinline__ void load_slots(const DistillArgs& o, long long r, co
     for (int i = 0; i < kMaxTop / 32; i++) {
         z[i] = row && id[i] >= 0 && id[i] < vocab ? row[id[i]] : Group<T>::from_f(kNegInf);
         if (id[i] < 0) u[i] = kNegInf;
-        bad |= id[i] >= vocab;
+        bad |= id[i] >= vocab && u[i] != kNegInf;                // (an empty slot may have any id)
     }
     bad = __any_sync(0xffffffffu, bad);
 }

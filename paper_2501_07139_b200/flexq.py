@@ -507,8 +507,8 @@ class FlexQ:
     def fq_distill_topk(self, logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, temperature: float = 1.0,
                         grad_loss: Optional[torch.Tensor] = None, grad: Optional[torch.Tensor] = None):
         """KL of every row's distribution from its teacher's top logits -> (loss fp32 [rows], lse fp32 [rows][2], gradient or None).
-        ids int32 / int64 [rows][n] (negative: an empty slot) and teacher fp32 [rows][n] are the teacher's tokens and logits, or log
-        probabilities.  With `grad_loss` (fp32 [rows], upstream) the gradient with respect to the logits comes from the same call, into
+        ids int32 / int64 [rows][n] and teacher fp32 [rows][n] are the teacher's tokens and logits, or log probabilities (an empty slot: a negative
+        id, or a logit of -inf).  With `grad_loss` (fp32 [rows], upstream) the gradient with respect to the logits comes from the same call, into
         `grad` if that is given (it may be `logits`); without, fq_distill_topk_grad gives it later from `lse`."""
         rows, vocab, ld, n_top, grad, ldg = self._slots(logits, ids, teacher, grad_loss, grad)
         both = torch.empty(3 * rows, dtype=torch.float32, device=self.device)
