@@ -351,7 +351,8 @@ int fq_token_logprobs(fq_ctx* ctx, const void* logits_dev, int dtype, int rows, 
  *   logits_dev, tokens as in fq_token_logprobs;  ids_dev int32 or int64, teacher_dev float [rows][n_top], 1 <= n_top <= FQ_MAX_TOP;
  *   grad_loss_dev float [rows]: upstream gradient of every row's loss (a row whose is 0 gets a gradient of 0 whatever it holds);
  *   loss_dev float [rows];  lse_dev float [rows][2], 8-byte aligned: (m, log S), so that m / T + log S is the log-sum-exp;
- *   grad_dev dtype [rows][ldg >= vocab]: may be logits_dev itself, with the same pitch (the gradient then replaces the logits).
+ *   grad_dev dtype [rows][ldg >= vocab]: may be logits_dev itself, with the same pitch (the gradient then replaces the logits;
+ *   with another pitch the call is refused).
  * fq_distill_topk writes loss and lse and, if grad_dev is not NULL, the gradient in the same pass over the logits;
  * fq_distill_topk_grad writes the gradient alone, from the lse of an earlier call on the same logits, temperature and slots. */
 int fq_distill_topk(fq_ctx* ctx, const void* logits_dev, int dtype, int rows, int vocab, long long ld, const void* ids_dev, int id_bytes,

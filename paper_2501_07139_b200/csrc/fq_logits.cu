@@ -1129,6 +1129,9 @@ int check_rows(const fq_ctx* ctx, const void* logits, int dtype, int rows, int v
     return FQ_OK;
 }
 
+// A gradient in place of the logits has to have their pitch: one row's gradient would overwrite another's logits.
+bool other_pitch(const void* logits, long long ld, const void* grad, long long ldg, int rows) { return grad == logits && ldg != ld && rows > 1; }
+
 RowArgs row_args(const Ctx* ctx, const void* logits, int vocab, long long ld, float temperature, const Cut& c)
 {
     RowArgs a{};
@@ -1223,6 +1226,7 @@ int fq_distill_topk(fq_ctx* ctx, const void* logits_dev, int dtype, int rows, in
     if (rc != FQ_OK) return rc;
     if (!ids_dev || !teacher_dev || !loss_dev || !lse_dev || (grad_dev && !grad_loss_dev)) return FQ_ERR_ARG;
     if (n_top < 1 || (grad_dev && ldg < vocab)) return FQ_ERR_SHAPE;
+    if (other_pitch(logits_dev, ld, grad_dev, ldg, rows)) return FQ_ERR_ARG;
     if (!aligned(ids_dev, (size_t)id_bytes) || !aligned(teacher_dev, 4) || !aligned(grad_loss_dev, 4) || !aligned(loss_dev, 4) ||
         !aligned(lse_dev, 8) || !aligned(grad_dev, (size_t)type_size(dtype)))
         return FQ_ERR_ALIGN;
@@ -1238,6 +1242,7 @@ int fq_distill_topk_grad(fq_ctx* ctx, const void* logits_dev, int dtype, int row
     if (rc != FQ_OK) return rc;
     if (!ids_dev || !teacher_dev || !grad_loss_dev || !lse_dev || !grad_dev) return FQ_ERR_ARG;
     if (n_top < 1 || ldg < vocab) return FQ_ERR_SHAPE;
+    if (other_pitch(logits_dev, ld, grad_dev, ldg, rows)) return FQ_ERR_ARG;
     if (!aligned(ids_dev, (size_t)id_bytes) || !aligned(teacher_dev, 4) || !aligned(grad_loss_dev, 4) || !aligned(lse_dev, 8) ||
         !aligned(grad_dev, (size_t)type_size(dtype)))
         return FQ_ERR_ALIGN;
