@@ -5,7 +5,8 @@ The paper evaluates candidates by perplexity on a calibration set; without train
 evaluation here is the relative output error of each linear layer on seeded calibration activations,
 || Y_b - Y_8 ||^2 / || Y_8 ||^2, summed over the layers of a module (and over modules for a configuration).
 The output head, whose outputs are logits, can be evaluated by what it answers instead: the divergence of its
-distribution from that of the highest precision's top tokens (`head`), and the perplexity of given tokens (head_answers).
+distribution from that of the highest precision's top tokens (`head`; the search scales it to the other layers' errors),
+and the perplexity of given tokens (head_answers).
 The library does the heavy work: fq_gemm for the outputs, fq_sqdiff for the two fp64 sums of every comparison,
 fq_token_logprobs and fq_distill_topk for the head's, fq_code_bytes for the sizes, fq_search_chain / fq_prune_chain for
 the search.  This module only divides each pair of sums and adds the per-layer ratios and sizes up per module (a few
@@ -58,18 +59,15 @@ def head_answers(fq: "F.FlexQ", head: Head, n_out: int, levels: Sequence[int], x
             for b, (n, e, k) in zip(levels, rows)]
 
 
-def module_tables(fq: "F.FlexQ", shapes: Sequence, modules: Sequence[Sequence[int]], levels: Sequence[int],
-                  calib: Dict[int, torch.Tensor], sens_tokens: int, head: Optional[Head] = None):
-    """cost, sens, foot tables [module][level] of a stack whose layers are nested (8-bit parents).
-
-    shapes[i] has n_out / k_in; modules[j] lists the layers of module j; levels are bit-widths from n_up down
-    to n_low; calib[k_in] is a bf16 [tokens][k_in] activation matrix.  cost uses every token, sens only the
-    first `sens_tokens` (the cheaper, pre-generated analysis of Sec. III-B).  `head`: that layer's error is the mean divergence of its
-    distribution from the tokens that levels[0] finds most likely."""
+def _tables(fq, shapes, modules, levels, calib, sens_tokens, head):
+    """module_tables, and what a nat of the head's divergence counts as relative output error (1 without a head)."""
+    if head is not None and any(head.layer in mod and len(mod) > 1 for mod in modules):
+        raise ValueError("the head has to be a module of its own: its error is a divergence, those of other layers are relative output errors")
     L = len(shapes)
     n_lev = len(levels)
     err = [[None] * n_lev for _ in range(L)]
     err_s = [[None] * n_lev for _ in range(L)]
+    lowest = None                        # the head's error at levels[-1] as that of any other layer
     cur = [int(levels[0])] * L
     fq.fq_set_config(cur)
     for i, sh in enumerate(shapes):
@@ -91,6 +89,8 @@ def module_tables(fq: "F.FlexQ", shapes: Sequence, modules: Sequence[Sequence[in
                 kl = fq.fq_distill_topk(y, *teacher, temperature=head.temperature)[0].double()
                 err[i][li] = torch.stack((kl.sum(), torch.ones_like(kl).sum()))
                 err_s[i][li] = torch.stack((kl[:sens_tokens].sum(), torch.ones_like(kl[:sens_tokens]).sum()))
+                if li == n_lev - 1:
+                    lowest = F.fq_sqdiff(y.contiguous(), y_up.contiguous())
                 continue
             err[i][li] = F.fq_sqdiff(y.contiguous(), y_up.contiguous())
             err_s[i][li] = F.fq_sqdiff(y[:sens_tokens].contiguous(), y_up[:sens_tokens].contiguous())
@@ -105,7 +105,20 @@ def module_tables(fq: "F.FlexQ", shapes: Sequence, modules: Sequence[Sequence[in
     cost = [[sum(rel(err[i][li]) for i in mod) for li in range(n_lev)] for mod in modules]
     sens = [[sum(rel(err_s[i][li]) for i in mod) for li in range(n_lev)] for mod in modules]
     foot = [[sum(F.fq_code_bytes(shapes[i].n_out, shapes[i].k_in, int(b)) for i in mod) for b in levels] for mod in modules]
-    return cost, sens, foot
+    nats = rel(err[head.layer][-1]) if lowest is not None else 0.0
+    return cost, sens, foot, rel(lowest) / nats if 0.0 < nats < math.inf else 1.0
+
+
+def module_tables(fq: "F.FlexQ", shapes: Sequence, modules: Sequence[Sequence[int]], levels: Sequence[int],
+                  calib: Dict[int, torch.Tensor], sens_tokens: int, head: Optional[Head] = None):
+    """cost, sens, foot tables [module][level] of a stack whose layers are nested (8-bit parents).
+
+    shapes[i] has n_out / k_in; modules[j] lists the layers of module j; levels are bit-widths from n_up down
+    to n_low; calib[k_in] is a bf16 [tokens][k_in] activation matrix.  cost uses every token, sens only the
+    first `sens_tokens` (the cheaper, pre-generated analysis of Sec. III-B).  `head`: that layer, a module of its own, has for its error the
+    mean divergence, in nats, of its distribution from the tokens that levels[0] finds most likely.  Other rows are relative output
+    errors: before rows are added up or compared, the head's wants a scale (generate_ensemble gives it one)."""
+    return _tables(fq, shapes, modules, levels, calib, sens_tokens, head)[:3]
 
 
 def chain_to_bits(chain: List[List[int]], modules: Sequence[Sequence[int]], levels: Sequence[int], n_layers: int):
@@ -122,8 +135,12 @@ def chain_to_bits(chain: List[List[int]], modules: Sequence[Sequence[int]], leve
 
 def generate_ensemble(fq, shapes, modules, levels, calib, stems: int = 2, branches: int = 3, sens_tokens: int = 32,
                       prune_fraction: float = 0.0, head: Optional[Head] = None):
-    cost, sens, foot = module_tables(fq, shapes, modules, levels, calib, sens_tokens, head)
-    chain, curve = F.fq_search_chain(cost, sens, foot, stems, branches)
+    """Tables, search and pruning.  With `head` the search sees the head's row of cost and sens times `head_scale`: the scale at which the divergence
+    at levels[-1] counts as much as the relative output error of the head there, so that the divergence says how the head's error grows with fewer
+    bits, and all rows are errors of one unit.  `cost` and `sens` are returned in the units of module_tables, `curve` is in those of the search."""
+    cost, sens, foot, scale = _tables(fq, shapes, modules, levels, calib, sens_tokens, head)
+    weights = [scale if head is not None and head.layer in mod else 1.0 for mod in modules]
+    chain, curve = F.fq_search_chain(*([[w * e for e in row] for w, row in zip(weights, table)] for table in (cost, sens)), foot, stems, branches)
     pruned, dropped, before, after = F.fq_prune_chain(chain, len(levels), foot, prune_fraction)
     return {"cost": cost, "sens": sens, "foot": foot, "chain": chain, "curve": curve, "pruned_chain": pruned,
-            "dropped": dropped, "storage_before": before, "storage_after": after}
+            "dropped": dropped, "storage_before": before, "storage_after": after, "head_scale": scale}
