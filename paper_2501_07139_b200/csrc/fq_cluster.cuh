@@ -4,7 +4,8 @@
 
 namespace fq {
 
-__device__ __forceinline__ uint32_t cluster_cta()
+// This CTA's place in its cluster.
+__device__ __forceinline__ uint32_t cluster_rank()
 {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));

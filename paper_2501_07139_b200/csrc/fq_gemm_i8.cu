@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_strip_kernel(const __grid_co
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = q.splits > 1 ? (int)cluster_cta() : 0, tile = (int)blockIdx.x / q.splits, m0 = (int)blockIdx.y * q.nt;
+    const int rank = q.splits > 1 ? (int)cluster_rank() : 0, tile = (int)blockIdx.x / q.splits, m0 = (int)blockIdx.y * q.nt;
     const int stage_bytes = kStripStageW + q.nt * kBK;
     uint8_t* tail = smem + q.stages * stage_bytes;
     const uint32_t bars = g_smem_u32(tail), full0 = bars, empty0 = bars + 8 * kStripMaxStages, done = bars + 16 * kStripMaxStages;

@@ -34,60 +34,52 @@ struct GemvArgs {
     long long ldy;
     int y_dtype;
     int N, K, rows;              // rows: output rows of a CTA
-    int x_groups;                // activations come in 16-byte groups
+    int x_groups;                // the activations of a token come in 16-byte groups
 };
 
-// Largest absolute values of the tokens, then their codes, zero behind the last column.  Values stay in registers in between where they come in
-// 16-byte groups of 16-bit ones (`groups`), two for every thread and slice.
-template <class T, int M, int S>
-__device__ __forceinline__ void quantise_here(const GemvArgs& a, int8_t* codes, float (&red)[M][kWarps], float (&scale)[M])
+// The largest absolute value of one token of up to kWarps * kSliceCols columns, then its codes, zero behind the last column.  Values stay in registers in
+// between where they come in 16-byte groups of 16-bit ones, two for every thread.
+template <class T>
+__device__ __forceinline__ void quantise_here(const GemvArgs& a, int8_t* codes, float (&red)[kWarps], float& scale)
 {
-    constexpr int cols = S * kWarps * kSliceCols, U = 2 * S;
+    constexpr int cols = kWarps * kSliceCols, U = 2;
     const T* x = static_cast<const T*>(a.x);
     const bool groups = sizeof(T) == 2 && a.x_groups;
-    uint4 v[M][U];
+    uint4 v[U];
 #pragma unroll
-    for (int t = 0; t < M; t++)
+    for (int u = 0; u < U; u++) {
+        const int c = (u * kThreads + (int)threadIdx.x) * 8;
+        v[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (groups && c < a.K) v[u] = *reinterpret_cast<const uint4*>(x + c);
+    }
+    float m = 0.0f;
+    if (groups) {
+        typename Group<T>::Max most = Group<T>::nothing();
+#pragma unroll
+        for (int u = 0; u < U; u++) Group<T>::take_abs(most, v[u]);
+        m = Group<T>::of_abs(most);
+    } else {
+        for (int c = threadIdx.x; c < a.K; c += kThreads) m = max_nan(m, fabsf(Group<T>::to_f(x[c])));
+    }
+    m = warp_max_nan(m);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = m;
+    __syncthreads();
+    m = red[0];
+#pragma unroll
+    for (int w = 1; w < kWarps; w++) m = max_nan(m, red[w]);
+    const RowScale s(m);
+    scale = RowScale::scale(m);
+    if (groups) {
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            const int c = (u * kThreads + (int)threadIdx.x) * 8;
-            v[t][u] = make_uint4(0u, 0u, 0u, 0u);
-            if (groups && c < a.K) v[t][u] = *reinterpret_cast<const uint4*>(x + t * a.ldx + c);
+            float2 f[Group<T>::N / 2];
+            Group<T>::unpack(v[u], f);
+            const uint32_t lo = s.four(f[0], f[1]);
+            const uint32_t hi = Group<T>::N == 8 ? s.four(f[Group<T>::N / 2 - 2], f[Group<T>::N / 2 - 1]) : 0u;
+            *reinterpret_cast<uint2*>(codes + (u * kThreads + (int)threadIdx.x) * 8) = make_uint2(lo, hi);
         }
-#pragma unroll
-    for (int t = 0; t < M; t++) {
-        float m = 0.0f;
-        if (groups) {
-            typename Group<T>::Max most = Group<T>::nothing();
-#pragma unroll
-            for (int u = 0; u < U; u++) Group<T>::take_abs(most, v[t][u]);
-            m = Group<T>::of_abs(most);
-        } else {
-            for (int c = threadIdx.x; c < a.K; c += kThreads) m = max_nan(m, fabsf(Group<T>::to_f(x[t * a.ldx + c])));
-        }
-        m = warp_max_nan(m);
-        if ((threadIdx.x & 31) == 0) red[t][threadIdx.x >> 5] = m;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int t = 0; t < M; t++) {
-        float m = red[t][0];
-#pragma unroll
-        for (int w = 1; w < kWarps; w++) m = max_nan(m, red[t][w]);
-        const RowScale s(m);
-        scale[t] = RowScale::scale(m);
-        if (groups) {
-#pragma unroll
-            for (int u = 0; u < U; u++) {
-                float2 f[Group<T>::N / 2];
-                Group<T>::unpack(v[t][u], f);
-                const uint32_t lo = s.four(f[0], f[1]);
-                const uint32_t hi = Group<T>::N == 8 ? s.four(f[Group<T>::N / 2 - 2], f[Group<T>::N / 2 - 1]) : 0u;
-                *reinterpret_cast<uint2*>(codes + t * cols + (u * kThreads + (int)threadIdx.x) * 8) = make_uint2(lo, hi);
-            }
-        } else {
-            for (int c = threadIdx.x; c < cols; c += kThreads) codes[t * cols + c] = c < a.K ? s.one(Group<T>::to_f(x[t * a.ldx + c])) : (int8_t)0;
-        }
+    } else {
+        for (int c = threadIdx.x; c < cols; c += kThreads) codes[c] = c < a.K ? s.one(Group<T>::to_f(x[c])) : (int8_t)0;
     }
     __syncthreads();
 }
@@ -95,14 +87,14 @@ __device__ __forceinline__ void quantise_here(const GemvArgs& a, int8_t* codes, 
 template <class T, int M, int S>
 __global__ void __launch_bounds__(kThreads, 2) gemv_i8_kernel(const GemvArgs a)
 {
-    extern __shared__ __align__(16) int8_t smem[];       // [M][columns] codes, then int [warps][rows][M]
-    __shared__ float red[M][kWarps];
+    extern __shared__ __align__(16) int8_t smem[];       // the codes of a token that is quantised here, then int [warps][rows][M]
+    __shared__ float red[kWarps];
     constexpr int R = S <= 2 && M * S <= 4 ? kRowsAtATime : kRowsAtATime / 2;
     constexpr bool kCodes = sizeof(T) == 1;
-    constexpr int cols = S * kWarps * kSliceCols;
+    static_assert(kCodes || (M == 1 && S == 1), "one token of one slice a warp is quantised here");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int r0 = (int)blockIdx.x * a.rows, r1 = min(a.N, r0 + a.rows);
-    int* part = reinterpret_cast<int*>(smem + (kCodes ? 0 : M * cols));
+    int* part = reinterpret_cast<int*>(smem + (kCodes ? 0 : kWarps * kSliceCols));
     const int col0 = warp * kSliceCols + lane * 16;      // of slice s: + s * kWarps * kSliceCols
 
     const auto load = [&](uint4 (&w)[R], int r, int s) {
@@ -140,11 +132,8 @@ __global__ void __launch_bounds__(kThreads, 2) gemv_i8_kernel(const GemvArgs a)
                 }
             }
     } else {
-        quantise_here<T, M, S>(a, smem, red, scale);
-#pragma unroll
-        for (int s = 0; s < S; s++)
-#pragma unroll
-            for (int t = 0; t < M; t++) xq[s][t] = *reinterpret_cast<const uint4*>(smem + t * cols + col0 + s * kWarps * kSliceCols);
+        quantise_here<T>(a, smem, red, scale[0]);
+        xq[0][0] = *reinterpret_cast<const uint4*>(smem + col0);
     }
     const auto multiply = [&](const uint4 (&v)[R], int s, int (&acc)[R][M]) {
 #pragma unroll
@@ -206,11 +195,10 @@ __global__ void __launch_bounds__(kThreads, 2) gemv_i8_kernel(const GemvArgs a)
 template <class T, int M, int S>
 int launch(const Ctx* ctx, GemvArgs a, bool early, cudaStream_t st)
 {
-    constexpr int cols = S * kWarps * kSliceCols;
     const int ctas = 2 * ctx->sm_count;
     // the rows in even shares for two CTAs on every SM
     a.rows = std::min(kMaxRows, std::max(1, (a.N + ctas - 1) / ctas));
-    const size_t smem = (sizeof(T) == 1 ? 0 : (size_t)M * cols) + sizeof(int) * kWarps * (size_t)a.rows * M;
+    const size_t smem = (sizeof(T) == 1 ? 0 : (size_t)kWarps * kSliceCols) + sizeof(int) * kWarps * (size_t)a.rows * M;
     static std::atomic<bool> ready[64];
     if (!ready[ctx->device].load(std::memory_order_acquire)) {
         if (cudaFuncSetAttribute(gemv_i8_kernel<T, M, S>, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != cudaSuccess) return FQ_ERR_CUDA;
@@ -248,7 +236,7 @@ int launch_gemv_i8(const Ctx* ctx, const void* x, int x_dtype, long long ldx, co
                    int k_in, long long ldw, void* y, int y_dtype, long long ldy, bool early, cudaStream_t st)
 {
     if (ctx->device >= 64) return FQ_ERR_ARG;
-    const GemvArgs a{x, ldx, sx, w, ldw, sw, y, ldy, y_dtype, n_out, k_in, 0, k_in % 8 == 0 && aligned(x, 16) && (M == 1 || ldx % 8 == 0)};
+    const GemvArgs a{x, ldx, sx, w, ldw, sw, y, ldy, y_dtype, n_out, k_in, 0, k_in % 8 == 0 && aligned(x, 16)};
     if (x_dtype == FQ_DT_F32) return launch<float, 1, 1>(ctx, a, early, st);
     if (x_dtype == FQ_DT_F16) return launch<__half, 1, 1>(ctx, a, early, st);
     if (x_dtype == FQ_DT_BF16) return launch<__nv_bfloat16, 1, 1>(ctx, a, early, st);

@@ -283,15 +283,17 @@ struct Running {
         const float mm = m == kNegInf ? 0.0f : m;
         // exp(d) d of a masked entry would be 0 * -inf.  Entries of two to a register are kept above a floor whose exponential is 0
         // all the same, at half the cost of doing so with the scaled differences.
-        const float floor2 = (Group<T>::kFloor - mm) * c2;
-        if (ENTROPY && Group<T>::N == 8 && floor2 < -160.0f && floor2 > -1e37f) {
-            uint4 w[G];
+        if constexpr (ENTROPY && Group<T>::N == 8) {
+            const float floor2 = (Group<T>::kFloor - mm) * c2;
+            if (floor2 < -160.0f && floor2 > -1e37f) {
+                uint4 w[G];
 #pragma unroll
-            for (int g = 0; g < G; g++) w[g] = Group<T>::above_floor(v[g]);
-            add<false>(w, mm, c2);
-        } else {
-            add<ENTROPY>(v, mm, c2);
+                for (int g = 0; g < G; g++) w[g] = Group<T>::above_floor(v[g]);
+                add<false>(w, mm, c2);
+                return here;
+            }
         }
+        add<ENTROPY>(v, mm, c2);
         return here;
     }
     // A batch is added up before it is added to the sums: a long row takes a thread vocab / 2048 (fp32) or vocab / 4096 additions to them instead
@@ -676,7 +678,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
 {
     __shared__ RowShared sh;
     __shared__ TopShared<THREADS> top;
-    const int rank = a.n_cta > 1 ? (int)cluster_cta() : 0;
+    const int rank = a.n_cta > 1 ? (int)cluster_rank() : 0;
     const long long r = blockIdx.x / a.n_cta;
     const T* row = static_cast<const T*>(a.z) + r * a.ld;
     const Stream<T> x(row, slice_of<T>(a, row, rank));
@@ -831,7 +833,7 @@ __global__ void __launch_bounds__(THREADS + 32, 1024 / THREADS) distill_loss_ker
 {
     __shared__ RowShared sh;
     constexpr int kPer = kMaxTop / 32;
-    const int rank = a.n_cta > 1 ? (int)cluster_cta() : 0, lane = threadIdx.x & 31;
+    const int rank = a.n_cta > 1 ? (int)cluster_rank() : 0, lane = threadIdx.x & 31;
     const long long r = blockIdx.x / a.n_cta;
     const T* row = static_cast<const T*>(a.z) + r * a.ld;
     const bool teaches = rank == 0 && threadIdx.x >= THREADS;    // one warp more than those that see to the logits
@@ -1074,8 +1076,6 @@ Cut cut_rows(int rows, int vocab, int size, int sm_count, bool cluster)
     while (c.n_cta < kMaxCluster && (long long)rows * c.n_cta * 2 <= sm_count && per(2 * c.n_cta) * size >= kLeastBytes) c.n_cta *= 2;
     c.slice = per(c.n_cta);
     c.smem = (size_t)c.slice * size + 32;
-    const size_t lists = c.n_cta > 1 ? (size_t)c.n_cta * kMaxTop * 8 : 0;
-    if (c.smem < lists) c.smem = lists;
     return c;
 }
 
@@ -1100,12 +1100,13 @@ Cut cut_streams(int rows, int vocab, int size, int sm_count, int threads)
     return c;
 }
 
+// ready: of the kernels with slices on chip, for which devices they may have as much shared memory as they ask for.
 template <class... Args>
 int launch_rows(void (*kernel)(Args...), int threads, std::atomic<bool>* ready, const Ctx* ctx, int rows, const Cut& c, bool cluster, cudaStream_t st,
                 Args... args)
 {
-    if (ctx->device >= 64) return FQ_ERR_ARG;
-    if (c.smem > 0 && !ready[ctx->device].load(std::memory_order_acquire)) {
+    if (ready && ctx->device >= 64) return FQ_ERR_ARG;
+    if (ready && !ready[ctx->device].load(std::memory_order_acquire)) {
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 208 * 1024) != cudaSuccess) return FQ_ERR_CUDA;
         ready[ctx->device].store(true, std::memory_order_release);
     }
@@ -1144,18 +1145,16 @@ RowArgs row_args(const Ctx* ctx, const void* logits, int vocab, long long ld, fl
 template <class T>
 int logprobs_typed(const Ctx* ctx, int threads, int rows, const Cut& c, const RowArgs& a, const LogprobArgs& o, cudaStream_t st)
 {
-    static std::atomic<bool> ready[2][64];
-    if (threads == 128) return launch_rows(token_logprobs_kernel<T, 128>, 128, ready[0], ctx, rows, c, true, st, a, o);
-    return launch_rows(token_logprobs_kernel<T, 256>, 256, ready[1], ctx, rows, c, true, st, a, o);
+    if (threads == 128) return launch_rows(token_logprobs_kernel<T, 128>, 128, nullptr, ctx, rows, c, true, st, a, o);
+    return launch_rows(token_logprobs_kernel<T, 256>, 256, nullptr, ctx, rows, c, true, st, a, o);
 }
 
 template <class T>
 int loss_typed(const Ctx* ctx, int threads, int rows, const Cut& c, const RowArgs& a, const DistillArgs& o, cudaStream_t st)
 {
-    static std::atomic<bool> ready[3][64];
-    if (threads == 128) return launch_rows(distill_loss_kernel<T, 128>, 128 + 32, ready[0], ctx, rows, c, true, st, a, o);
-    if (threads == 256) return launch_rows(distill_loss_kernel<T, 256>, 256 + 32, ready[1], ctx, rows, c, true, st, a, o);
-    return launch_rows(distill_loss_kernel<T, 512>, 512 + 32, ready[2], ctx, rows, c, true, st, a, o);
+    if (threads == 128) return launch_rows(distill_loss_kernel<T, 128>, 128 + 32, nullptr, ctx, rows, c, true, st, a, o);
+    if (threads == 256) return launch_rows(distill_loss_kernel<T, 256>, 256 + 32, nullptr, ctx, rows, c, true, st, a, o);
+    return launch_rows(distill_loss_kernel<T, 512>, 512 + 32, nullptr, ctx, rows, c, true, st, a, o);
 }
 
 template <class T, bool GIVEN>

@@ -68,8 +68,6 @@ template <> struct Group<float> {
     static __device__ __forceinline__ void take_abs(Max& m, const uint4& v);
     static __device__ __forceinline__ float of_abs(Max m) { return m; }
     static __device__ __forceinline__ uint4 fill() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }      // -inf
-    static constexpr float kFloor = -1e30f;
-    static __device__ __forceinline__ uint4 above_floor(const uint4& v) { return v; }                                             // (not used)
     static __device__ __forceinline__ float to_f(float v) { return v; }
     static __device__ __forceinline__ float from_f(float v) { return v; }
 };

@@ -7,6 +7,7 @@
 
 #include <atomic>
 
+#include "fq_cluster.cuh"
 #include "fq_internal.cuh"
 
 namespace fq {
@@ -86,19 +87,8 @@ static __device__ __forceinline__ uint32_t umma_idesc_bf16(int m, int n)
 }
 
 // ---- pairs of SMs (cta_group::2)
-static __device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
 // The same shared-memory location in the leading CTA of the pair.
-static __device__ __forceinline__ uint32_t in_leader(uint32_t addr)
-{
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
-    return r;
-}
+static __device__ __forceinline__ uint32_t in_leader(uint32_t addr) { return cluster_map(addr, 0u); }
 static __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
