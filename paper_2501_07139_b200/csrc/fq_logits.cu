@@ -296,9 +296,9 @@ struct Running {
         add<ENTROPY>(v, mm, c2);
         return here;
     }
-    // A batch is added up before it is added to the sums: a long row takes a thread vocab / 2048 (fp32) or vocab / 4096 additions to them instead
-    // of vocab / 256, which round alike where terms are (393216 equal ones: a log probability off by 13 of 2^-24 instead of 371).  Within it pairwise, or one by one
-    // beside the entropy's products (pairwise there too: 4094 x 32000 bf16 67.8 us instead of 66.3 us).
+    // A batch is added up before it is added to the sums: a long row takes a thread vocab / 2048 (fp32) or vocab / 4096 additions to them
+    // instead of vocab / 256, which round alike where terms are (393216 equal ones: a log probability off by 13 of 2^-24 instead of 371).
+    // (Pairwise within the batch: 4094 x 32000 fp16 96.0 us instead of 95.4 us, the loss alone 47.8 us instead of 47.1 us.)
     template <bool CLAMP, int G>
     __device__ __forceinline__ void add(const uint4 (&v)[G], float mm, float c2)
     {
@@ -314,18 +314,9 @@ struct Running {
                     t.x = max_nan(t.x, -160.0f);
                     t.y = max_nan(t.y, -160.0f);
                 }
-                f[p] = make_float2(ex2(t.x), ex2(t.y));
-                if (ENTROPY) {
-                    batch = g + p == 0 ? f[p] : add2(batch, f[p]);
-                    batch1 = g + p == 0 ? mul2(f[p], t) : fma2(f[p], t, batch1);
-                }
-            }
-            if (!ENTROPY) {
-#pragma unroll
-                for (int n = Group<T>::N / 4; n > 0; n /= 2)
-#pragma unroll
-                    for (int p = 0; p < n; p++) f[p] = add2(f[p], f[p + n]);
-                batch = g == 0 ? f[0] : add2(batch, f[0]);
+                const float2 e = make_float2(ex2(t.x), ex2(t.y));
+                batch = g + p == 0 ? e : add2(batch, e);
+                if (ENTROPY) batch1 = g + p == 0 ? mul2(e, t) : fma2(e, t, batch1);
             }
         }
         s = add2(s, batch);
