@@ -11,9 +11,10 @@
 // whole, the elements before the first and behind the last of them one by one, and the rest of those two groups counts as -inf,
 // which no maximum and no sum sees.
 //
-// What bounds it: rows of 16-bit logits the instructions per logit and the exponential pipe as much as HBM.  4094 x 32000 bf16: m, S and
-// entropy 53 us, with 32 alternatives 66 us, the loss alone 48 us (a pass that only reads: 47 us); value and gradient 96 us, the
-// gradient alone 81 us (a copy: 82 us).  fp32, half as many logits: 44, 56, 44, 107 and 81 us.
+// What bounds it: passes without alternatives and the gradient alone HBM.  Alternatives, and value and gradient, add phases that other CTAs of the
+// SM cover in part: no pipe is full (exponentials 53 - 66 %, issue slots 55 - 60 % of 16-bit rows, HBM 50 - 60 %).  4094 x 32000 bf16: m, S and
+// entropy 50 us, with 32 alternatives 66 us, the loss alone 48 us (a pass that only reads: 47 us); value and gradient 95 us, the
+// gradient alone 79 us (a copy: 82 us).  fp32, half as many logits: 47, 57, 46, 104 and 79 us.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -661,8 +662,8 @@ struct RowAnswer {
     }
 };
 
-// A CTA to a row, or to a slice of one.  128 threads a row: with 256, and their barriers, 4094 x 32000 bf16 takes 81 us instead of 67 us; more than 64
-// alternatives need the closer bound of 256 threads' maxima.  One row of 32000 and 20 alternatives: 7.2 us, a chain of launch, loads, seven barriers
+// A CTA to a row, or to a slice of one.  128 threads a row: with 256, and their barriers, 4094 x 32000 bf16 takes 73 us instead of 66 us; more than 64
+// alternatives need the closer bound of 256 threads' maxima.  One row of 32000 and 20 alternatives: 7.6 us, a chain of launch, loads, seven barriers
 // and the exchange between four CTAs.
 template <class T, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel(const RowArgs a, const LogprobArgs o)
@@ -818,7 +819,7 @@ __device__ __forceinline__ float loss_term(float p, float lp, float z_id, float 
     return p == 0.0f ? 0.0f : p * (lp + log_s) - p * (z_id - zm) / t;
 }
 
-// The value alone: the logits pass through once (4094 x 32000 bf16 48 us, 255 x 32000 7.4 us: with 128 threads and clusters of four 10.5 us).
+// The value alone: the logits pass through once (4094 x 32000 bf16 48 us, 255 x 32000 7.3 us: with 128 threads and clusters of four 10.2 us).
 template <class T, int THREADS>
 __global__ void __launch_bounds__(THREADS + 32, 1024 / THREADS) distill_loss_kernel(const RowArgs a, const DistillArgs o)
 {
@@ -864,8 +865,8 @@ __global__ void __launch_bounds__(THREADS + 32, 1024 / THREADS) distill_loss_ker
 
 // GIVEN: the gradient alone, from the (m, log S) that an earlier call kept; slices then need nothing from one another.
 //   THREADS threads see to the logits.  One warp more sees to the teacher: its distribution, the student's logits at its tokens (two loads, one after the
-// other, and a chain of dependent arithmetic that would hold the others up: 108 us instead of 101 us), and at the end the loss.  The gradient
-// leaves in pieces while the next ones are formed.  Three CTAs of 64 KB fill an SM; smaller ones in clusters lose more in the exchange than they win.
+// other, and a chain of dependent arithmetic that would hold the others up, 7 % of the time), and at the end the loss.  The gradient
+// leaves in pieces while the next ones are formed.  Three CTAs with slices of up to 68 KB fill an SM; smaller ones in clusters lose more in the exchange than they win.
 template <class T, int THREADS, bool GIVEN>
 __global__ void __launch_bounds__(THREADS + 32, 1024 / THREADS) distill_kernel(const RowArgs a, const DistillArgs o)
 {
@@ -1051,9 +1052,9 @@ __global__ void __launch_bounds__(THREADS + 32, 1024 / THREADS) distill_kernel(c
 
 // ------------------------------------------------------------------------------- host side
 // How rows that stay on chip are cut.  A slice of up to 68 KB leaves room for three CTAs on an SM, so that one computes while the copies
-// of the others are on their way.  Where the CTAs of a row need nothing from one another, slices of up to 36 KB, six to an SM, are better
-// (gradient alone, 4096 x 32000 bf16: 87 us against 93; with clusters of two, value and gradient: 146 us against 109).  With few
-// rows a row is spread over more SMs, down to slices of 8 KB.
+// of the others are on their way.  Where the CTAs of a row need nothing from one another, slices of up to 36 KB leave room for four (their registers)
+// and cost no exchange: the gradient alone of 4094 x 32000 bf16 takes 79.4 us against 80.5 us.  In clusters of two, value and gradient take 114 us
+// against 95 us.  With few rows a row is spread over more SMs, down to slices of 8 KB.
 struct Cut { int n_cta, slice; size_t smem; };
 Cut cut_rows(int rows, int vocab, int size, int sm_count, bool cluster)
 {
@@ -1152,7 +1153,7 @@ template <class T, bool GIVEN>
 int distill_typed(const Ctx* ctx, int rows, const Cut& c, const RowArgs& a, const DistillArgs& o, cudaStream_t st)
 {
     static std::atomic<bool> ready[2][64];
-    // (rows of up to 36 KB: six CTAs to an SM, if they have half the threads)
+    // (rows of up to 36 KB: five CTAs to an SM and more, if they have half the threads)
     if constexpr (!GIVEN) {
         if (c.smem <= 36 * 1024) return launch_rows(distill_kernel<T, 128, false>, 128 + 32, ready[0], ctx, rows, c, true, st, a, o);
     }

@@ -56,8 +56,9 @@ __global__ void __launch_bounds__(THREADS) quantize_rows_kernel(const QuantArgs 
 }
 
 // Rows that stay in registers, U pieces of 8 values to a thread: pieces are 16-byte aligned on both sides, and there is a whole number of them.
-// Many rows: four pieces, so that a row's maximum, two reductions and a reciprocal, is shared by 32 values of a thread (8192 x 4096 bf16 27.5 us,
-// with one piece a thread 45 us; the next row on its way while one is worked on gains nothing).  Few rows: one or two, for the latency.
+// Many rows: four pieces, so that a row's maximum, two reductions and a reciprocal, is shared by 32 values of a thread (8192 x 4096 bf16 27 us,
+// of which HBM needs 16, with one piece a thread 45 us; the next row on its way while one is worked on gains nothing).  What is left are phases: a
+// row's loads, its maximum behind a barrier, its codes (issue slots 63 %, HBM 36 %; most stalls are waits for loads).  Few rows: one or two, for the latency.
 template <class T, int U>
 __global__ void __launch_bounds__(1024, 1) quantize_rows_kept_kernel(const QuantArgs a)
 {

@@ -465,7 +465,8 @@ class FlexQ:
     # -- what a model answers ------------------------------------------------------------------
     def fq_token_logprobs(self, logits: torch.Tensor, tokens: torch.Tensor, n_top: int = 0, temperature: float = 1.0, out=None):
         """Rows of logits and one token each -> (log probability fp32 [rows], entropy fp32 [rows], ids int32 [rows][n_top] of the most
-        likely tokens, their log probabilities fp32 [rows][n_top]).  `out`: the four tensors to write to."""
+        likely tokens, their log probabilities fp32 [rows][n_top]).  `out`: the four tensors to write to; new ones are parts of one
+        allocation, which lives as long as any of them."""
         rows, vocab, ld = self._matrix(logits, "logits", _TYPES)
         self._dense(tokens, "tokens", _IDS, (rows,))
         if n_top < 0:
