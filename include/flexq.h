@@ -337,7 +337,7 @@ int fq_linear_i8(fq_ctx* ctx, const void* X_dev, int x_dtype, int M, long long l
  *   logprob_dev, entropy_dev float [rows];  top_ids_dev int32, top_logprobs_dev float [rows][n_top] (n_top <= FQ_MAX_TOP; may be NULL if it is 0).
  * 1e-30 <= temperature <= 1e30.  Sums in fp32: with E = sum exp(d_i) |d_i| / S, at most log vocab, S is off by at most
  * 2^-24 (40 + 3 E + vocab / 2048) of itself, and by 2^-24 vocab / 400 more where logits rise all along a row; a log probability by as much, by
- * 3 * 2^-24 |d| and by its own rounding. */
+ * 3 * 2^-24 |d| and by its own rounding.  z_i - m is formed in fp32: a difference beyond its range counts as infinite. */
 int fq_token_logprobs(fq_ctx* ctx, const void* logits_dev, int dtype, int rows, int vocab, long long ld, const void* tokens_dev, int id_bytes,
                       float temperature, float* logprob_dev, float* entropy_dev, int n_top, int* top_ids_dev, float* top_logprobs_dev,
                       void* stream);
