@@ -52,6 +52,8 @@ enum { FQ_OK = 0,
        FQ_ERR_IO = -11,         /* file could not be opened, read or written, or is malformed */
        FQ_ERR_BOUNDS = -12 };   /* checked build only (-DFQ_CHECKED): a kernel computed an address outside its
                                    buffer; the access was skipped (see fq_status)                         */
+enum { FQ_ERR_BLOCKS = -13,     /* too few free blocks, or a sequence that does not fit its block table (fq_cache_step, see fq_status) */
+       FQ_ERR_INDEX = -14 };    /* a length, block, slot or token number on the device that cannot be (see fq_status) */
 
 #define FQ_MAX_BATCH 8          /* decode batch handled by the GEMV family */
 
@@ -287,7 +289,7 @@ int fq_gemm_two_pass(fq_ctx* ctx, int layer, const uint16_t* X_dev, int M, int l
 
 enum { FQ_DT_F16 = 0, FQ_DT_BF16 = 1, FQ_DT_F32 = 2 };     /* types of the buffers that cross as void* */
 
-/* The calls from here to fq_distill_topk_grad take their matrices with a row pitch (in elements), allocate nothing, use none of the
+/* The calls from here to fq_tree_attention take their matrices with a row pitch (in elements), allocate nothing, use none of the
  * context's workspaces and keep nothing from one call for the next: they may run on any stream of the context's device, several at
  * a time, and be captured and replayed.  Only the status word (fq_status) is shared.  An output may not overlap an input or
  * another output, except where that is said. */
@@ -361,6 +363,109 @@ int fq_distill_topk(fq_ctx* ctx, const void* logits_dev, int dtype, int rows, in
 int fq_distill_topk_grad(fq_ctx* ctx, const void* logits_dev, int dtype, int rows, int vocab, long long ld, const void* ids_dev, int id_bytes,
                          const float* teacher_dev, int n_top, float temperature, const float* grad_loss_dev, const float* lse_dev,
                          void* grad_dev, long long ldg, void* stream);
+
+/* Between the linear layers of a block ------------------------------------------------ */
+
+/* A sequence's keys and values lie in blocks of `block_size` tokens that may be anywhere in a layer's cache; its row of a block table names them in order,
+ * the same for all layers.  Cell p of a sequence is token p % block_size of block table[p / block_size]; a slot is block * block_size + that.
+ * What these calls read from device memory is checked there: a number that cannot be (a block outside the cache, a negative length) is never
+ * followed; it is recorded for fq_status, and each call says what its outputs are then. */
+
+#define FQ_MAX_SEQS 16384       /* sequences of one call */
+#define FQ_MAX_TREE_WORDS 16    /* 64-bit words of a row of tree bits */
+
+/* Heads of a batch of tokens, [tokens][heads][head_dim]: head_dim values in a row, strides in elements. */
+typedef struct fq_heads {
+    void* dev;
+    long long token_stride, head_stride;
+    int heads;
+} fq_heads;
+
+/* The keys and values of one layer, each [blocks][block_size][heads][head_dim] with the same strides (in elements; in any order, as long as
+ * cells do not overlap): 16-byte aligned, rows of head_dim values a multiple of 16 bytes apart. */
+typedef struct fq_cache {
+    void* k_dev;
+    void* v_dev;
+    long long block_stride, token_stride, head_stride;
+    int blocks, block_size, heads;
+} fq_cache;
+
+/* One step of a batch's caches: every sequence is cut back to its first keep[b] tokens, then grows by new_tokens[b].  keep = lens: it goes on;
+ * less: drafted tokens were refused; 0: another request takes its place.  Blocks that are no longer needed go to the end of the free list, in the order of sequences
+ * and cells; then the needed ones come from its end.
+ *   lens_dev      int [n_seqs]                tokens in the cache before (read) and after (written: keep + new)
+ *   keep_dev, new_dev int [n_seqs]            0 <= keep <= lens, new >= 0
+ *   table_dev     int [n_seqs][ld >= max_blocks]   block numbers (updated; entries that no token uses any more become -1)
+ *   free_dev      int [free_room], free_count_dev int [1]   the free list and how many it holds (updated)
+ *   parents_dev   int [tokens] or NULL        drafted trees: for every new token the number (within its sequence's new tokens) of the one before it in
+ *                                             its branch, always a smaller number; -1: it follows what is cached
+ *   starts_dev    int [n_seqs + 1]            first row of every sequence's new tokens in the batch; the last entry is how many there are (written)
+ *   slots_dev     int64 [tokens]              where each new token's key and value go (written; -1 in rows behind the last new token)
+ *   positions_dev int [tokens]                its position: keep + number in the sequence, or with parents keep + tokens above it (written; 0 behind the last)
+ *   mask_dev      uint64 [tokens][words]      with parents: bit j of a row is set where the token sees new token j of its sequence, itself
+ *                                             and those above it (written; 0 behind the last).  words <= FQ_MAX_TREE_WORDS
+ * If there are too few free blocks, a sequence does not fit its row of the table or the new tokens are more than `tokens` (FQ_ERR_BLOCKS), or a number
+ * cannot be (FQ_ERR_INDEX; with parents also more than 64 * words new tokens), nothing of lens, table and free list changes, starts are all 0
+ * and slots all -1.  A parent that is not a smaller number counts as -1 (FQ_ERR_INDEX).
+ * 1 <= n_seqs <= FQ_MAX_SEQS, 1 <= tokens <= FQ_MAX_ROWS, 1 <= max_blocks <= 2^20, 1 <= block_size <= 2^16, max_blocks * block_size < 2^30.
+ * Calls that share any of the updated arrays have to be ordered. */
+int fq_cache_step(fq_ctx* ctx, int n_seqs, int* lens_dev, const int* keep_dev, const int* new_dev, int* table_dev, long long ld, int max_blocks,
+                  int block_size, int* free_dev, int free_room, int* free_count_dev, const int* parents_dev, int tokens, int* starts_dev,
+                  long long* slots_dev, int* positions_dev, uint64_t* mask_dev, int words, void* stream);
+
+/* The accepted branch of every sequence's drafted tokens is moved together, in n_caches caches (keys or values of a layer each): the key or value of new token
+ * kept[b][i] goes to cell before + i, where `before` = lens[b] less the sequence's new tokens, for i < n_kept[b].  kept[b][0 .. n_kept) rises
+ * and names new tokens of the sequence; else (FQ_ERR_INDEX) nothing of that sequence moves and keep is `before`.
+ *   caches_host   host array of n_caches device pointers, each a cache as in fq_cache (dtype, strides and sizes are those of all)
+ *   kept_dev      int [n_seqs][ld_kept >= max_kept], n_kept_dev int [n_seqs];  1 <= max_kept <= 1024
+ *   keep_dev      int [n_seqs]                before + n_kept: what fq_cache_step is to keep next (written) */
+int fq_cache_move(fq_ctx* ctx, void* const* caches_host, int n_caches, const fq_cache* layout, int dtype, int head_dim, int n_seqs, const int* table_dev,
+                  long long ld, int max_blocks, const int* starts_dev, const int* lens_dev, const int* kept_dev, long long ld_kept,
+                  int max_kept, const int* n_kept_dev, int* keep_dev, void* stream);
+
+/* Angles of rotary positions: pair i of rot_dim / 2 turns by f_i radians a position, f_i = base^(-2i / rot_dim), in a longer context than the trained one
+ * scaled by parts:  r = context * f_i / (2 pi) turns within the original context,  g = (r - low) / (high - low) kept within [0, 1],
+ * f_i' = g f_i + (1 - g) f_i / factor;  with context 0 all are divided by factor.
+ *   turns_host uint64 [rot_dim / 2]: f' / (2 pi) * 2^64, rounded: the angle of position p is p * turns modulo 2^64, exactly, however far p is.
+ * Host only.  rot_dim even, 2 .. 1024; base > 1; factor >= 1; 0 <= low < high. */
+int fq_rotary_table(int rot_dim, double base, double factor, int context, double low, double high, uint64_t* turns_host);
+
+/* Rotary positions.  Of every head the first rot_dim values are turned in pairs (x_i, x_{i + rot_dim/2}), or (x_2i, x_{2i+1}) if `interleaved`:
+ *   y = magnitude (x cos a - x' sin a),   y' = magnitude (x sin a + x' cos a),   a = angle of pair i at the token's position;
+ * the others are copied.  `inverse` turns the other way, which with the same magnitude is the gradient.  fp32 arithmetic, one rounding.
+ *   x, y          n (1 .. 4) tensors and where they go; y[i] may be x[i] itself, with the same strides
+ *   positions_dev int32 or int64 [tokens] (id_bytes 4 or 8)
+ *   turns_dev     uint64 [rot_dim / 2], 8-byte aligned, from fq_rotary_table
+ * rot_dim even, 2 <= rot_dim <= head_dim <= 1024; 1 <= tokens <= FQ_MAX_ROWS; up to 1024 heads; any alignment to the type. */
+int fq_rotary(fq_ctx* ctx, const fq_heads* x, const fq_heads* y, int n, int dtype, int tokens, int head_dim, int rot_dim, const void* positions_dev,
+              int id_bytes, const uint64_t* turns_dev, int interleaved, int inverse, float magnitude, void* stream);
+
+/* The same in a serving step: q is turned into q_out (may be q), k is turned and stored with v in the layer's cache, at slots_dev int64 [tokens].  Tokens with a
+ * negative slot are not stored; nor are those with a slot outside the cache (FQ_ERR_INDEX).  No two tokens may have the same slot. */
+int fq_rotary_cache(fq_ctx* ctx, const fq_heads* q, const fq_heads* q_out, const fq_heads* k, const fq_heads* v, const fq_cache* cache, int dtype,
+                    int tokens, int head_dim, int rot_dim, const void* positions_dev, int id_bytes, const long long* slots_dev,
+                    const uint64_t* turns_dev, int interleaved, float magnitude, void* stream);
+
+/* Attention of every sequence's new tokens, which are the last ones in its cache, over all that is cached and those of the new ones that they see:
+ *   out = sum_j p_j v_j,   p = softmax(scale q . k_j) over the cells j that the token sees;   lse = log sum exp(scale q . k_j)
+ * Query heads share key heads in groups: head h uses key head h / (q heads / cache heads).  A token sees all cells before the new ones and, of the new ones,
+ * those of its bits in mask_dev; with mask_dev NULL those up to itself (single tokens, drafted chains, prompts).  A row that sees nothing: out 0,
+ * lse -inf.  What a row does not see does not touch it, an infinity or a NaN in it neither; one that it sees makes its values infinite or NaN.
+ *   q, out        dtype fp16 or bf16, [tokens][q heads][head_dim]; 16-byte aligned, strides multiples of 8; out may not overlap q
+ *   cache         of the same dtype
+ *   starts_dev    int [n_seqs + 1]: rows of the sequences' new tokens (may be none); rows behind the last are left as they are
+ *   lens_dev      int [n_seqs]: tokens in the cache, the new ones among them
+ *   mask_dev      uint64 [tokens][words] or NULL
+ *   lse_dev       float [tokens][q heads], or NULL
+ *   new_tokens    how many new tokens a sequence has, about: it decides how rows are dealt, not what comes out
+ *   scratch_dev   fq_tree_attention_scratch bytes, 16-byte aligned; calls that may overlap need scratch of their own
+ * head_dim a multiple of 8, up to 256; up to 1024 heads; sizes as in fq_cache_step.  Scores and sums in fp32, p rounded to dtype for the product with v, out rounded
+ * once.  The result does not depend on what else is in the batch beyond the order in which fp32 sums are formed; the same call gives the same bits.
+ * Cells in a block outside the cache count as zeros, and a sequence with fewer cells than new tokens as one whose rows see nothing (FQ_ERR_INDEX). */
+size_t fq_tree_attention_scratch(const fq_ctx* ctx, int n_seqs, int tokens, int q_heads, int cache_heads, int head_dim, int new_tokens);
+int fq_tree_attention(fq_ctx* ctx, const fq_heads* q, const fq_heads* out, const fq_cache* cache, int dtype, int head_dim, int tokens, int n_seqs,
+                      const int* starts_dev, const int* lens_dev, const int* table_dev, long long ld, int max_blocks, const uint64_t* mask_dev, int words,
+                      int new_tokens, float scale, float* lse_dev, void* scratch_dev, size_t scratch_bytes, void* stream);
 
 /* Test / reporting support ------------------------------------------------------------ */
 

@@ -1,0 +1,248 @@
+// What the attention kernels share: their arguments, how the work of a batch is dealt to thread blocks, and what a row sees.
+//
+// Work.  A unit is one key head of one sequence and a tile of its query rows: the query heads that share the key head, for all new tokens, are rows
+// r = token * share + head, so that keys and values are read once for all of them.  A unit costs the key tiles that its rows see and
+// one more for its ends.  The host does not know the lengths, so every CTA adds the costs up for itself and takes an equal share of the sum: units of
+// long sequences are cut, and each part leaves (sum, maximum, values) in scratch, which a second small kernel joins.  The parts and
+// their order depend on the lengths alone.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "fq_internal.cuh"
+#include "fq_ptx.cuh"
+
+namespace fq {
+
+struct AttnArgs {
+    const void* q;
+    void* out;
+    long long q_token, q_head, out_token, out_head;
+    const void* k;
+    const void* v;
+    long long block_stride, cell_stride, head_stride;
+    int blocks, block_size;
+    int tokens, n_seqs, kv_heads, share;         // share: query heads of a key head
+    int head_dim;
+    const int* starts;
+    const int* lens;
+    const int* table;
+    long long ld;
+    int max_blocks;
+    const uint64_t* mask;                        // null: a token sees those before it
+    int words;
+    float scale;                                 // times log2 e
+    float* lse;
+    float* parts;                                // two slots a CTA: rows x (head_dim + 2)
+    struct AttnJoin* joins;                      // one a CTA
+    int* status;
+};
+
+// A unit that begins in this CTA and ends in another.
+struct AttnJoin {
+    int seq, row0, head, others;                 // others: CTAs behind this one that hold parts (0: nothing to join)
+    int rows;                                    // rows of the unit
+    int pad[3];
+};
+
+struct Seq {
+    int row0, fresh, len, ctx;                   // first row in the batch, new tokens, cells, cells before the new ones
+    // Numbers that cannot be never lead outside the arrays.
+    __device__ __forceinline__ Seq(const AttnArgs& a, int b)
+    {
+        row0 = a.starts[b];
+        const int end = a.starts[b + 1];
+        len = a.lens[b];
+        fresh = end - row0;
+        if (row0 < 0 || fresh < 0 || end > a.tokens || len < fresh || len > (long long)a.max_blocks * a.block_size) {
+            if (row0 < 0 || fresh < 0 || end > a.tokens) row0 = fresh = 0;
+            len = 0;
+            atomicCAS(a.status, 0, FQ_ERR_INDEX);
+        }
+        ctx = max(0, len - fresh);
+    }
+    __device__ __forceinline__ Seq() {}
+};
+
+// Key tiles of KEYS cells that a tile of ROWS query rows sees (rows r0 .. of a sequence).
+template <int ROWS, int KEYS>
+__device__ __forceinline__ int key_tiles(const AttnArgs& a, const Seq& s, int row_tile)
+{
+    int last = s.len;                            // with a tree's bits any row may see any new token
+    if (!a.mask) last = min(last, s.ctx + ((row_tile + 1) * ROWS - 1) / a.share + 1);
+    return (last + KEYS - 1) / KEYS;
+}
+template <int ROWS>
+__device__ __forceinline__ int row_tiles(const AttnArgs& a, const Seq& s) { return (s.fresh * a.share + ROWS - 1) / ROWS; }
+
+// Cost of one key head of a sequence.
+template <int ROWS, int KEYS>
+__device__ __forceinline__ long long head_cost(const AttnArgs& a, const Seq& s)
+{
+    const int n = row_tiles<ROWS>(a, s);
+    if (a.mask || n <= 1) return (long long)n * (1 + key_tiles<ROWS, KEYS>(a, s, n - 1));
+    long long c = 0;
+    for (int r = 0; r < n; r++) c += 1 + key_tiles<ROWS, KEYS>(a, s, r);
+    return c;
+}
+
+// This CTA's parts of units, one after the other.
+template <int ROWS, int KEYS, int THREADS>
+struct Deal {
+    long long at, end, total;                    // cost position, of the CTA's end, of all work
+    int b, head, tile;                           // sequence, key head, row tile
+    Seq s;
+    int tiles;                                   // key tiles of the unit
+    long long unit;                              // where the unit begins
+
+    // CTAs with work: each has one position at least.  (total < 2^51: cells of a sequence < 2^30, rows of the batch <= 2^30.)
+    static __device__ __forceinline__ unsigned ctas(long long total) { return (unsigned)min((long long)gridDim.x, total); }
+    static __device__ __forceinline__ long long share_of(long long total, unsigned cta)
+    {
+        const unsigned n = ctas(total);
+        return cta >= n ? total : (long long)((unsigned long long)total * cta / n);
+    }
+
+    // All threads of the CTA; `sums` is shared memory of THREADS / 32 + 4 long longs.  False: nothing to do.
+    __device__ __forceinline__ bool begin(const AttnArgs& a, long long* sums)
+    {
+        constexpr int W = THREADS / 32;
+        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+        long long base = 0, from = 0;
+        total = 0;
+        for (int pass = 0; pass < 2; pass++) {
+            base = 0;
+            for (int b0 = 0; b0 < a.n_seqs; b0 += THREADS) {
+                long long c = 0;
+                if (b0 + tid < a.n_seqs) {
+                    const Seq q(a, b0 + tid);
+                    c = q.fresh > 0 ? a.kv_heads * head_cost<ROWS, KEYS>(a, q) : 0;
+                }
+                long long in = c;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const long long up = __shfl_up_sync(0xffffffffu, in, o);
+                    if (lane >= o) in += up;
+                }
+                __syncthreads();
+                if (lane == 31) sums[warp] = in;
+                __syncthreads();
+                long long before = 0, all = 0;
+#pragma unroll
+                for (int w = 0; w < W; w++) {
+                    if (w < warp) before += sums[w];
+                    all += sums[w];
+                }
+                const long long excl = base + before + in - c;
+                if (a.n_seqs <= THREADS) {       // one look is enough
+                    total = all;
+                    from = share_of(total, blockIdx.x);
+                    pass = 1;
+                }
+                if (pass == 1 && c > 0 && from >= excl && from < excl + c) {
+                    sums[W] = b0 + tid;
+                    sums[W + 1] = excl;
+                }
+                base += all;
+            }
+            if (pass == 0) {
+                total = base;
+                from = share_of(total, blockIdx.x);
+            }
+        }
+        __syncthreads();
+        at = from;
+        end = share_of(total, blockIdx.x + 1);
+        if (at >= end) return false;
+        b = (int)sums[W];
+        s = Seq(a, b);
+        unit = sums[W + 1];
+        const long long hc = head_cost<ROWS, KEYS>(a, s);
+        head = (int)((at - unit) / hc);
+        unit += head * hc;
+        tile = 0;
+        tiles = key_tiles<ROWS, KEYS>(a, s, 0);
+        while (at >= unit + 1 + tiles) {
+            unit += 1 + tiles;
+            tile++;
+            tiles = key_tiles<ROWS, KEYS>(a, s, tile);
+        }
+        return true;
+    }
+    // Key tiles [t0, t1) of the unit are this CTA's.  Its outputs are, if `whole`; else a part is left in scratch.
+    __device__ __forceinline__ int t0() const { return (int)max(0ll, at - unit - 1); }
+    __device__ __forceinline__ int t1() const { return (int)max(0ll, min(end - unit, 1ll + tiles) - 1); }
+    __device__ __forceinline__ bool any() const { return t1() > t0() || (tiles == 0 && at == unit); }
+    __device__ __forceinline__ bool whole() const { return t0() == 0 && t1() == tiles; }
+    // CTAs behind this one that hold the unit's other parts
+    __device__ __forceinline__ int others() const
+    {
+        const long long last = unit + tiles;     // the last cost position of the unit
+        // the CTA whose share holds it: share_of(c) <= last < share_of(c + 1)
+        long long c = (long long)((unsigned long long)last * ctas(total) / (unsigned long long)total);
+        while (share_of(total, (unsigned)c + 1) <= last) c++;
+        while (share_of(total, (unsigned)c) > last) c--;
+        return (int)c - (int)blockIdx.x;
+    }
+    __device__ __forceinline__ bool next(const AttnArgs& a)
+    {
+        unit += 1 + tiles;
+        at = unit;
+        if (at >= end) return false;
+        if (++tile >= row_tiles<ROWS>(a, s)) {
+            tile = 0;
+            if (++head >= a.kv_heads) {
+                head = 0;
+                do {
+                    if (++b >= a.n_seqs) return false;
+                    s = Seq(a, b);
+                } while (s.fresh <= 0);
+            }
+        }
+        tiles = key_tiles<ROWS, KEYS>(a, s, tile);
+        return true;
+    }
+};
+
+// Does new token `t` (its row of bits: `row` of the batch) see cell `cell` of its sequence?
+__device__ __forceinline__ bool sees(const AttnArgs& a, const Seq& s, int t, int row, int cell)
+{
+    if (cell >= s.len) return false;
+    const int nth = cell - s.ctx;
+    if (nth < 0) return true;
+    if (!a.mask) return nth <= t;
+    return (nth >> 6) < a.words && (a.mask[(long long)row * a.words + (nth >> 6)] >> (nth & 63) & 1);
+}
+
+// Offset (in values) of a cell's row in the cache, or -1 (recorded) where its block is not one.
+__device__ __forceinline__ long long cell_place(const AttnArgs& a, int b, int cell)
+{
+    const int nth = cell / a.block_size, block = a.table[b * a.ld + nth];
+    if ((unsigned)block >= (unsigned)a.blocks) {
+        atomicCAS(a.status, 0, FQ_ERR_INDEX);
+        return -1;
+    }
+    return block * a.block_stride + (cell - nth * a.block_size) * a.cell_stride;
+}
+
+template <class T> __device__ __forceinline__ bool finite16(uint32_t two);       // both of two 16-bit values
+template <> __device__ __forceinline__ bool finite16<__nv_bfloat16>(uint32_t v) { return (v & 0x7f80u) != 0x7f80u && (v & 0x7f800000u) != 0x7f800000u; }
+template <> __device__ __forceinline__ bool finite16<__half>(uint32_t v) { return (v & 0x7c00u) != 0x7c00u && (v & 0x7c000000u) != 0x7c000000u; }
+
+// Infinities and NaNs among the values of new tokens are taken out before the product, where a weight of 0 would spread them to rows that do not
+// see them; this puts them where they belong.  Rare: a unit whose tiles had any comes here.  Returns what is to be added to value d of a row.
+template <class T>
+__device__ __noinline__ float unseen_spoils(const AttnArgs& a, const Seq& s, int b, int head, int t, int row, int d, int cell0, int cell1)
+{
+    float sum = 0.0f;
+    for (int cell = max(cell0, s.ctx); cell < min(cell1, s.len); cell++) {
+        if (!sees(a, s, t, row, cell)) continue;
+        const long long place = cell_place(a, b, cell);
+        if (place < 0) continue;
+        const float v = (float)static_cast<const T*>(a.v)[place + head * a.head_stride + d];
+        if (!isfinite(v)) sum += v;
+    }
+    return sum;
+}
+
+}  // namespace fq

@@ -225,6 +225,8 @@ const char* fq_strerror(int code)
         case FQ_ERR_ONE_WAY: return "transition would raise a layer's bit-width";
         case FQ_ERR_IO: return "file could not be opened, read or written, or is malformed";
         case FQ_ERR_BOUNDS: return "a kernel computed an address outside its buffer (checked build)";
+        case FQ_ERR_BLOCKS: return "too few free blocks, or a sequence that does not fit its block table";
+        case FQ_ERR_INDEX: return "a length, block, slot or token number on the device that cannot be";
         default: return "unknown error";
     }
 }

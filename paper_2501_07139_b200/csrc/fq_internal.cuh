@@ -219,6 +219,11 @@ bool gemv_i8_quantises(int M, int k_in);       // as activations
 int launch_gemv_i8(const Ctx* ctx, const void* x, int x_dtype, long long ldx, const float* sx, int M, const int8_t* w, const float* sw, int n_out,
                    int k_in, long long ldw, void* y, int y_dtype, long long ldy, bool early, cudaStream_t st);
 
+// between the linear layers: arguments that several calls take
+int check_heads(const fq_heads* x, int dtype, int tokens, int head_dim);       // (an output: rows may not overlap)
+int check_cache(const fq_cache* c, int dtype, int head_dim);
+int check_table(const int* table, long long ld, int n_seqs, int max_blocks, int block_size);
+
 int launch_gemm(Ctx* ctx, const void* store, int blob_stride, const FieldList& fl, int zero_adjust, int n_out, int k_in,
                 const uint16_t* X, int M, int ldx, uint16_t* Y, int ldy, void* w_scratch, cudaStream_t st);
 

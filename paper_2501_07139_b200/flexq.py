@@ -19,7 +19,8 @@ FQ_DT_BF16 = 1
 FQ_DT_F32 = 2
 FQ_MAX_TOP = 128
 FQ_MAX_VOCAB = 393216
-_I8, _F32, _I32, _IDS = (torch.int8,), (torch.float32,), (torch.int32,), (torch.int32, torch.int64)
+_I8, _F32, _I32, _I64, _IDS = (torch.int8,), (torch.float32,), (torch.int32,), (torch.int64,), (torch.int32, torch.int64)
+_HALF = (torch.float16, torch.bfloat16)
 _TYPES = {torch.float16: FQ_DT_F16, torch.bfloat16: FQ_DT_BF16, torch.float32: FQ_DT_F32}
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -36,7 +37,8 @@ EXPORTS = [
     "fq_export_meta", "fq_storage_bytes", "fq_active_bits", "fq_status", "fq_strerror", "fq_gemv_static", "fq_transition", "fq_save", "fq_load", "fq_search_chain", "fq_prune_chain", "fq_sqdiff",
     "fq_set_wait_limit_ns", "fq_code_bytes", "fq_meta_bytes", "fq_stream_read", "fq_gemm_two_pass", "fq_gemm_plan",
     "fq_host_variant", "fq_transition_swap", "fq_quantize_rows", "fq_gemm_i8", "fq_linear_i8", "fq_token_logprobs", "fq_distill_topk",
-    "fq_distill_topk_grad",
+    "fq_distill_topk_grad", "fq_cache_step", "fq_cache_move", "fq_rotary_table", "fq_rotary", "fq_rotary_cache", "fq_tree_attention_scratch",
+    "fq_tree_attention",
 ]
 
 
@@ -53,6 +55,15 @@ class SwapReport(C.Structure):
 
 class GemmPlan(C.Structure):
     _fields_ = [("two_pass", C.c_int), ("shared", C.c_int), ("blocks", C.c_int), ("tile_tokens", C.c_int), ("tiles", C.c_longlong)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("dev", C.c_void_p), ("token_stride", C.c_longlong), ("head_stride", C.c_longlong), ("heads", C.c_int)]
+
+
+class Cache(C.Structure):
+    _fields_ = [("k_dev", C.c_void_p), ("v_dev", C.c_void_p), ("block_stride", C.c_longlong), ("token_stride", C.c_longlong),
+                ("head_stride", C.c_longlong), ("blocks", C.c_int), ("block_size", C.c_int), ("heads", C.c_int)]
 
 
 class FlexQError(RuntimeError):
@@ -116,6 +127,15 @@ def lib():
     L.fq_token_logprobs.argtypes = [vp, vp, i, i, i, ll, vp, i, fl, vp, vp, i, vp, vp, vp]
     L.fq_distill_topk.argtypes = [vp, vp, i, i, i, ll, vp, i, vp, i, fl, vp, vp, vp, vp, ll, vp]
     L.fq_distill_topk_grad.argtypes = [vp, vp, i, i, i, ll, vp, i, vp, i, fl, vp, vp, vp, ll, vp]
+    hp, cp, db = C.POINTER(Heads), C.POINTER(Cache), C.c_double
+    L.fq_cache_step.argtypes = [vp, i, vp, vp, vp, vp, ll, i, i, vp, i, vp, vp, i, vp, vp, vp, vp, i, vp]
+    L.fq_cache_move.argtypes = [vp, vp, i, cp, i, i, i, vp, ll, i, vp, vp, vp, ll, i, vp, vp, vp]
+    L.fq_rotary_table.argtypes = [i, db, db, i, db, db, vp]
+    L.fq_rotary.argtypes = [vp, hp, hp, i, i, i, i, i, vp, i, vp, i, i, fl, vp]
+    L.fq_rotary_cache.argtypes = [vp, hp, hp, hp, hp, cp, i, i, i, i, vp, i, vp, vp, i, fl, vp]
+    L.fq_tree_attention_scratch.argtypes = [vp, i, i, i, i, i, i]
+    L.fq_tree_attention_scratch.restype = C.c_size_t
+    L.fq_tree_attention.argtypes = [vp, hp, hp, cp, i, i, i, i, vp, vp, vp, ll, i, vp, i, i, fl, vp, vp, C.c_size_t, vp]
     L.fq_strerror.argtypes = [i]
     L.fq_strerror.restype = C.c_char_p
     for name in EXPORTS:
@@ -214,6 +234,16 @@ def fq_quantize_layer(w: torch.Tensor, bits: int, group: int = 128):
         _check(lib().fq_quantize_layer(w.data_ptr(), n, k, bits, group, codes.data_ptr(), scales.data_ptr(),
                                        zeros.data_ptr(), _stream()), "fq_quantize_layer")
     return codes, scales, zeros
+
+
+def fq_rotary_table(rot_dim: int, base: float = 10000.0, factor: float = 1.0, context: int = 0, low: float = 1.0, high: float = 32.0,
+                    device="cuda") -> torch.Tensor:
+    """Angles for fq_rotary and fq_rotary_cache, int64 [rot_dim / 2] on `device`: pair i turns by base^(-2i / rot_dim) radians a position.  For contexts `factor`
+    times as long as the trained one, of `context` tokens: pairs that turn `high` times in it and more stay, those that turn `low` times and
+    less are slowed by `factor`, between them both are mixed; with context 0 all are slowed."""
+    turns = torch.empty(max(rot_dim // 2, 1), dtype=torch.int64)
+    _check(lib().fq_rotary_table(rot_dim, base, factor, context, low, high, turns.data_ptr()), "fq_rotary_table")
+    return turns.to(device)
 
 
 class FlexQ:
@@ -529,3 +559,166 @@ class FlexQ:
                                           teacher.data_ptr(), n_top, temperature, grad_loss.data_ptr(), lse.data_ptr(), grad.data_ptr(), ldg,
                                           _stream_on(self.device)), "fq_distill_topk_grad")
         return grad
+
+    # -- between the linear layers of a block -----------------------------------------------------
+    def _heads(self, t: torch.Tensor, name: str, types, tokens: Optional[int] = None, dim: Optional[int] = None) -> Heads:
+        shape, st = t.shape, t.stride()
+        if len(shape) != 3 or t.dtype not in types or t.get_device() != self._index or (st[2] != 1 and shape[2] > 1):
+            raise ValueError(f"{name}: [tokens][heads][values] of {', '.join(str(d) for d in types)} on {self.device} with dense values are needed, not "
+                             f"{t.dtype} {tuple(shape)} with strides {st} on {t.device}")
+        if (tokens is not None and shape[0] != tokens) or (dim is not None and shape[2] != dim):
+            raise ValueError(f"{name}: {tokens} tokens with heads of {dim} are needed, not {shape[0]} with heads of {shape[2]}")
+        return Heads(t.data_ptr(), st[0], st[1], shape[1])
+
+    def _cache(self, k: torch.Tensor, v: torch.Tensor, types, dim: Optional[int] = None) -> Cache:
+        shape, st = k.shape, k.stride()
+        if len(shape) != 4 or k.dtype not in types or k.get_device() != self._index or (st[3] != 1 and shape[3] > 1) or v.shape != shape or \
+                v.stride() != st or v.dtype != k.dtype or v.get_device() != self._index:
+            raise ValueError(f"caches: two of [blocks][block size][heads][values], {', '.join(str(d) for d in types)} on {self.device} with dense values and the "
+                             f"same strides are needed, not {k.dtype} {tuple(shape)} {st} on {k.device} and {v.dtype} {tuple(v.shape)} {v.stride()} on {v.device}")
+        if dim is not None and shape[3] != dim:
+            raise ValueError(f"caches: heads of {dim} are needed, not of {shape[3]}")
+        return Cache(k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], shape[0], shape[1], shape[2])
+
+    def _table(self, table: torch.Tensor, n_seqs: int):
+        rows, cols, ld = self._matrix(table, "table", _I32)
+        if rows != n_seqs:
+            raise ValueError(f"table: a row for each of {n_seqs} sequences is needed, not {rows}")
+        return cols, max(ld, cols)
+
+    def fq_cache_step(self, lens: torch.Tensor, keep: torch.Tensor, new: torch.Tensor, table: torch.Tensor, free: torch.Tensor, count: torch.Tensor,
+                      block_size: int, tokens: int, parents: Optional[torch.Tensor] = None, words: int = 1):
+        """One step of a batch's paged caches: every sequence is cut back to its first keep[b] tokens, then grows by new[b].  lens [n] and table [n][blocks]
+        (int32), the free list `free` and how many it holds, count [1], are updated in place.  `tokens`: rows of the batch (at least the new tokens).
+        -> (starts int32 [n + 1], slots int64 [tokens], positions int32 [tokens], bits int64 [tokens][words] of drafted trees given by `parents`
+        int32 [tokens], or None).  What does not fit is recorded for fq_status and changes nothing."""
+        n = lens.shape[0] if lens.dim() == 1 else 0
+        for t, name in ((lens, "lens"), (keep, "keep"), (new, "new")):
+            self._dense(t, name, _I32, (n,))
+        blocks, ld = self._table(table, n)
+        self._dense(free, "free", _I32, (free.numel(),))
+        self._dense(count, "count", _I32, (1,))
+        if parents is not None:
+            self._dense(parents, "parents", _I32, (tokens,))
+        width = words if parents is not None else 0
+        if tokens < 1 or width < 0:
+            raise ValueError("tokens and words have to be positive")
+        # one allocation: slots, bits, positions, starts
+        wide = tokens * (1 + width)
+        all4 = torch.empty(wide + (tokens + n + 2) // 2, dtype=torch.int64, device=self.device)
+        narrow = all4.view(torch.int32)
+        slots, positions, starts = all4.as_strided((tokens,), (1,), 0), narrow.as_strided((tokens,), (1,), 2 * wide), narrow.as_strided((n + 1,), (1,), 2 * wide + tokens)
+        mask = all4.as_strided((tokens, width), (width, 1), tokens) if width else None
+        at = all4.data_ptr()
+        _check(lib().fq_cache_step(self._h, n, lens.data_ptr(), keep.data_ptr(), new.data_ptr(), table.data_ptr(), ld, blocks, block_size, free.data_ptr(),
+                                   free.numel(), count.data_ptr(), None if parents is None else parents.data_ptr(), tokens, at + 8 * wide + 4 * tokens, at,
+                                   at + 8 * wide, at + 8 * tokens if width else None, width, _stream_on(self.device)), "fq_cache_step")
+        return starts, slots, positions, mask
+
+    def fq_cache_move(self, caches: Sequence[torch.Tensor], table: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor, kept: torch.Tensor,
+                      n_kept: torch.Tensor):
+        """Moves the accepted branch of every sequence's new tokens together, in all `caches` (keys and values of all layers, [blocks][block size][heads][values] each, of
+        one shape and type): new token kept[b][i] goes to the i-th cell behind what was cached before, i < n_kept[b].  kept int32 [n][most], rising.
+        -> keep int32 [n], what fq_cache_step is to keep."""
+        caches = list(caches)
+        if not caches:
+            raise ValueError("caches: none given")
+        layout = self._cache(caches[0], caches[0], _TYPES)
+        shape, st, dt = caches[0].shape, caches[0].stride(), caches[0].dtype
+        for t in caches:
+            if t.shape != shape or t.stride() != st or t.dtype != dt or t.get_device() != self._index:
+                raise ValueError(f"caches: {dt} {tuple(shape)} with strides {st} on {self.device} for all, not {t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}")
+        n = lens.shape[0] if lens.dim() == 1 else 0
+        self._dense(lens, "lens", _I32, (n,))
+        self._dense(n_kept, "n_kept", _I32, (n,))
+        self._dense(starts, "starts", _I32, (n + 1,))
+        blocks, ld = self._table(table, n)
+        rows, most, ld_kept = self._matrix(kept, "kept", _I32)
+        if rows != n:
+            raise ValueError(f"kept: a row for each of {n} sequences is needed, not {rows}")
+        keep = torch.empty(n, dtype=torch.int32, device=self.device)
+        _check(lib().fq_cache_move(self._h, (C.c_void_p * len(caches))(*[t.data_ptr() for t in caches]), len(caches), C.byref(layout), _TYPES[dt], shape[3], n,
+                                   table.data_ptr(), ld, blocks, starts.data_ptr(), lens.data_ptr(), kept.data_ptr(), max(ld_kept, most), most,
+                                   n_kept.data_ptr(), keep.data_ptr(), _stream_on(self.device)), "fq_cache_move")
+        return keep
+
+    def _positions(self, positions, turns, tokens):
+        self._dense(positions, "positions", _IDS, (tokens,))
+        self._dense(turns, "turns", _I64, (turns.numel(),))
+        return 2 * turns.numel()
+
+    def fq_rotary(self, q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, turns: torch.Tensor, q_out: Optional[torch.Tensor] = None,
+                  k_out: Optional[torch.Tensor] = None, interleaved: bool = False, inverse: bool = False, magnitude: float = 1.0):
+        """Rotary positions of q and k, [tokens][heads][values] (any strides, values dense): the first 2 * len(turns) values of every head are turned in pairs by the
+        angles of fq_rotary_table, values i and i + len(turns), or `interleaved` 2i and 2i + 1.  `inverse` turns back, which is the gradient.  Into q_out and
+        k_out, which may be q and k; new ones where they are not given.  k may be None.  -> (q_out, k_out)"""
+        given = [(q, q_out, "q")] + ([(k, k_out, "k")] if k is not None else [])
+        tokens, _, dim = q.shape if q.dim() == 3 else (0, 0, 0)
+        x, y, outs = (Heads * 2)(), (Heads * 2)(), [None, None]
+        for i, (src, dst, name) in enumerate(given):
+            x[i] = self._heads(src, name, _TYPES if i == 0 else (q.dtype,), tokens, dim)
+            if dst is None:
+                dst = torch.empty(src.shape, dtype=src.dtype, device=self.device)
+            elif dst.shape != src.shape:
+                raise ValueError(f"{name}_out: {tuple(src.shape)} is needed, not {tuple(dst.shape)}")
+            y[i] = self._heads(dst, name + "_out", (q.dtype,), tokens, dim)
+            outs[i] = dst
+        rot = self._positions(positions, turns, tokens)
+        _check(lib().fq_rotary(self._h, x, y, len(given), _TYPES[q.dtype], tokens, dim, rot, positions.data_ptr(), positions.element_size(), turns.data_ptr(),
+                               1 if interleaved else 0, 1 if inverse else 0, magnitude, _stream_on(self.device)), "fq_rotary")
+        return outs[0], outs[1]
+
+    def fq_rotary_cache(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor, turns: torch.Tensor,
+                        k_cache: torch.Tensor, v_cache: torch.Tensor, q_out: Optional[torch.Tensor] = None, interleaved: bool = False, magnitude: float = 1.0):
+        """fq_rotary in a serving step: q goes to q_out (new if it is not given; may be q), k is turned and stored with v in the layer's caches
+        [blocks][block size][heads][values], at slots int64 [tokens] (negative: not stored).  -> q_out"""
+        tokens, _, dim = q.shape if q.dim() == 3 else (0, 0, 0)
+        same = (q.dtype,)
+        hq, hk, hv = self._heads(q, "q", _TYPES), self._heads(k, "k", same, tokens, dim), self._heads(v, "v", same, tokens, dim)
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+        elif q_out.shape != q.shape:
+            raise ValueError(f"q_out: {tuple(q.shape)} is needed, not {tuple(q_out.shape)}")
+        ho = self._heads(q_out, "q_out", same)
+        cache = self._cache(k_cache, v_cache, same, dim)
+        rot = self._positions(positions, turns, tokens)
+        self._dense(slots, "slots", _I64, (tokens,))
+        _check(lib().fq_rotary_cache(self._h, C.byref(hq), C.byref(ho), C.byref(hk), C.byref(hv), C.byref(cache), _TYPES[q.dtype], tokens, dim, rot,
+                                     positions.data_ptr(), positions.element_size(), slots.data_ptr(), turns.data_ptr(), 1 if interleaved else 0, magnitude,
+                                     _stream_on(self.device)), "fq_rotary_cache")
+        return q_out
+
+    def fq_tree_attention(self, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, starts: torch.Tensor,
+                          mask: Optional[torch.Tensor] = None, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                          lse: Optional[torch.Tensor] = None, new: Optional[int] = None):
+        """Attention of every sequence's new tokens over its paged cache, whose last cells they are: q [tokens][heads][values], rows starts[b] .. starts[b + 1] of
+        sequence b, caches [blocks][block size][key heads][values], table int32 [n][blocks], lens int32 [n] (the new tokens counted).  A token sees what was cached
+        before and, of the new tokens, those of its bits in `mask` int64 [tokens][words] (from fq_cache_step), or those up to itself.  `scale`:
+        values^-1/2 if not given.  `new`: how many new tokens a sequence has, about (tokens / n if not given).  Log-sum-exps go to `lse` fp32
+        [tokens][heads] if it is given.  -> out, new if not given; rows behind the last new token are left as they are."""
+        tokens, heads, dim = q.shape if q.dim() == 3 else (0, 0, 0)
+        hq = self._heads(q, "q", _HALF)
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+        elif out.shape != q.shape:
+            raise ValueError(f"out: {tuple(q.shape)} is needed, not {tuple(out.shape)}")
+        ho = self._heads(out, "out", (q.dtype,))
+        cache = self._cache(k_cache, v_cache, (q.dtype,), dim)
+        n = lens.shape[0] if lens.dim() == 1 else 0
+        self._dense(lens, "lens", _I32, (n,))
+        self._dense(starts, "starts", _I32, (n + 1,))
+        blocks, ld = self._table(table, n)
+        words = 0
+        if mask is not None:
+            words = mask.shape[1] if mask.dim() == 2 else 0
+            self._dense(mask, "mask", _I64, (tokens, words))
+        if lse is not None:
+            self._dense(lse, "lse", _F32, (tokens, heads))
+        if new is None:
+            new = -(-tokens // max(n, 1))
+        size = lib().fq_tree_attention_scratch(self._h, n, tokens, heads, cache.heads, dim, new)
+        scratch = torch.empty(max(size, 16), dtype=torch.uint8, device=self.device)
+        _check(lib().fq_tree_attention(self._h, C.byref(hq), C.byref(ho), C.byref(cache), _TYPES[q.dtype], dim, tokens, n, starts.data_ptr(), lens.data_ptr(),
+                                       table.data_ptr(), ld, blocks, None if mask is None else mask.data_ptr(), words, new, dim ** -0.5 if scale is None else scale,
+                                       None if lse is None else lse.data_ptr(), scratch.data_ptr(), size, _stream_on(self.device)), "fq_tree_attention")
+        return out
