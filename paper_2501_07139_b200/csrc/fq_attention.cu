@@ -33,14 +33,6 @@ struct Shape {                                   // DP: head_dim, rounded up to 
     static_assert(kTotal <= 232448, "shared memory over the per-CTA limit");
 };
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 __device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t addr)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -59,24 +51,6 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-template <class T>
-__device__ __forceinline__ uint32_t pack2(float x, float y)
-{
-    if constexpr (std::is_same<T, __half>::value) {
-        const __half2 h = __floats2half2_rn(x, y);
-        return *reinterpret_cast<const uint32_t*>(&h);
-    } else {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-        return *reinterpret_cast<const uint32_t*>(&h);
-    }
-}
-__device__ __forceinline__ float exp2_fast(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 template <class T, int DP>
 __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const __grid_constant__ AttnArgs a)
 {
@@ -138,7 +112,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
             settle();
         }
         f_stage = f_stage + 1 == S::kStages ? 0 : f_stage + 1;
-        copies_done();
+        copies_commit();
     };
     settle();
 #pragma unroll 1
@@ -347,35 +321,37 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
     copies_wait<0>();
 }
 
-// Joins the parts of units that were cut: CTA x takes those of the unit that begins in CTA x of the kernel before, four rows for each y.
+// Joins the parts of units that were cut: CTAs x take those of the unit that begins in CTA x of the kernel before, each y a share of its values.
+//   rows_of_tile : rows of a part;  by_piece : a part lies as [dp / 4][rows][4], else as [rows][dp];  behind that the rows' maxima and sums
+constexpr int kJoinThreads = 256, kJoinPieces = 1024;
 template <class T>
-__global__ void __launch_bounds__(128) attention_join_kernel(const __grid_constant__ AttnArgs a, int rows_of_tile, int dp)
+__global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __grid_constant__ AttnArgs a, int rows_of_tile, int dp, int by_piece)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const AttnJoin j = a.joins[blockIdx.x];
     if (j.others == 0) return;
-    const int s0 = a.starts[j.seq], per_row = dp / 4;
+    const int s0 = a.starts[j.seq], per_row = dp / 4, end = min(rows_of_tile * per_row, ((int)blockIdx.y + 1) * kJoinPieces);
     const long long slot = (long long)rows_of_tile * (dp + 2);
     // the first part is the second slot of its CTA, the others are the first slots of those behind it
     const float* first = a.parts + (blockIdx.x * 2 + 1) * slot;
     const float* rest = a.parts + (blockIdx.x + 1) * 2 * slot;
-    for (int i = threadIdx.x; i < 4 * per_row; i += 128) {
-        const int r = blockIdx.y * 4 + i / per_row, d = i % per_row * 4;
+    for (int i = blockIdx.y * kJoinPieces + threadIdx.x; i < end; i += kJoinThreads) {
+        const int r = by_piece ? i % rows_of_tile : i / per_row, d = (by_piece ? i / rows_of_tile : i % per_row) * 4;
         if (r >= j.rows || d >= a.head_dim) continue;
-        const long long om = rows_of_tile * dp + r, ol = om + rows_of_tile;
+        const long long om = (long long)rows_of_tile * dp + r, ol = om + rows_of_tile;
         float top = __ldcg(first + om);
 #pragma unroll 4
         for (int x = 0; x < j.others; x++) top = fmaxf(top, __ldcg(rest + x * 2 * slot + om));
         const float base = top == -INFINITY ? 0.0f : top;
         float by = exp2_fast(__ldcg(first + om) - base), sum = __ldcg(first + ol) * by;
-        float4 v = __ldcg(reinterpret_cast<const float4*>(first + r * dp + d));
+        float4 v = __ldcg(reinterpret_cast<const float4*>(first) + i);
         v = make_float4(v.x * by, v.y * by, v.z * by, v.w * by);
 #pragma unroll 4
         for (int x = 0; x < j.others; x++) {
             const float* p = rest + x * 2 * slot;
             by = exp2_fast(__ldcg(p + om) - base);
             sum += __ldcg(p + ol) * by;
-            const float4 u = __ldcg(reinterpret_cast<const float4*>(p + r * dp + d));
+            const float4 u = __ldcg(reinterpret_cast<const float4*>(p) + i);
             v.x += u.x * by; v.y += u.y * by; v.z += u.z * by; v.w += u.w * by;
         }
         by = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -397,25 +373,35 @@ int launch_attention(const fq_ctx* ctx, const AttnArgs& a, cudaStream_t st)
         ready[ctx->device].store(true, std::memory_order_release);
     }
     attention_kernel<T, DP><<<ctx->sm_count, S::kThreads, S::kTotal, st>>>(a);
-    if (cudaGetLastError() != cudaSuccess) return FQ_ERR_CUDA;
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)ctx->sm_count, kRows / 4); cfg.blockDim = dim3(128); cfg.stream = st; cfg.attrs = &attr; cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attention_join_kernel<T>, a, kRows, DP) == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
+    return cudaGetLastError() == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
 }
 
 int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
-template <class T>
-int launch_typed(const fq_ctx* ctx, const AttnArgs& a, cudaStream_t st)
+// Query rows of a unit.  Up to 16 rows to a key head go to the kernel of this file, whose work grows with every 16 rows; more to the tensor cores',
+// whose does with every 128, two tiles of them side by side where there are as many.
+int unit_rows(int new_tokens, int share, int dp)
 {
-    switch (padded_dim(a.head_dim)) {
-        case 64: return launch_attention<T, 64>(ctx, a, st);
-        case 128: return launch_attention<T, 128>(ctx, a, st);
-        default: return launch_attention<T, 256>(ctx, a, st);
-    }
+    const long long rows = (long long)new_tokens * share;
+    return rows <= kRows ? kRows : rows <= 128 || dp == 256 ? 128 : 256;
+}
+
+template <class T>
+int launch_typed(const fq_ctx* ctx, const AttnArgs& a, int rows, int dp, cudaStream_t st)
+{
+    int rc;
+    if (rows > kRows) rc = launch_attention_tc(ctx, a, std::is_same<T, __half>::value ? FQ_DT_F16 : FQ_DT_BF16, rows, dp, st);
+    else if (dp == 64) rc = launch_attention<T, 64>(ctx, a, st);
+    else if (dp == 128) rc = launch_attention<T, 128>(ctx, a, st);
+    else rc = launch_attention<T, 256>(ctx, a, st);
+    if (rc != FQ_OK) return rc;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)ctx->sm_count, (unsigned)((rows * dp / 4 + kJoinPieces - 1) / kJoinPieces)); cfg.blockDim = dim3(kJoinThreads);
+    cfg.stream = st; cfg.attrs = &attr; cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, attention_join_kernel<T>, a, rows, dp, rows > kRows ? 1 : 0) == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
 }
 
 bool good_sizes(const fq_ctx* ctx, int n_seqs, int tokens, int q_heads, int cache_heads, int head_dim, int new_tokens)
@@ -436,7 +422,8 @@ extern "C" {
 size_t fq_tree_attention_scratch(const fq_ctx* ctx, int n_seqs, int tokens, int q_heads, int cache_heads, int head_dim, int new_tokens)
 {
     if (!ctx || !good_sizes(ctx, n_seqs, tokens, q_heads, cache_heads, head_dim, new_tokens)) return 0;
-    return join_bytes(ctx) + (size_t)ctx->sm_count * 2 * kRows * (padded_dim(head_dim) + 2) * sizeof(float);
+    const int dp = padded_dim(head_dim), rows = unit_rows(new_tokens, q_heads / cache_heads, dp);
+    return join_bytes(ctx) + (size_t)ctx->sm_count * 2 * rows * (dp + 2) * sizeof(float);
 }
 
 int fq_tree_attention(fq_ctx* ctx, const fq_heads* q, const fq_heads* out, const fq_cache* cache, int dtype, int head_dim, int tokens, int n_seqs,
@@ -476,7 +463,8 @@ int fq_tree_attention(fq_ctx* ctx, const fq_heads* q, const fq_heads* out, const
     a.parts = reinterpret_cast<float*>(static_cast<char*>(scratch_dev) + join_bytes(ctx));
     a.status = ctx->status_dev;
     const cudaStream_t st = (cudaStream_t)stream;
-    return dtype == FQ_DT_F16 ? launch_typed<__half>(ctx, a, st) : launch_typed<__nv_bfloat16>(ctx, a, st);
+    const int dp = padded_dim(head_dim), rows = unit_rows(new_tokens, a.share, dp);
+    return dtype == FQ_DT_F16 ? launch_typed<__half>(ctx, a, rows, dp, st) : launch_typed<__nv_bfloat16>(ctx, a, rows, dp, st);
 }
 
 }  // extern "C"

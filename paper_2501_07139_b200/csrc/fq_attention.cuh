@@ -9,6 +9,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "fq_internal.cuh"
 #include "fq_ptx.cuh"
 
@@ -204,6 +206,32 @@ struct Deal {
     }
 };
 
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+template <class T>
+__device__ __forceinline__ uint32_t pack2(float x, float y)
+{
+    if constexpr (std::is_same<T, __half>::value) {
+        const __half2 h = __floats2half2_rn(x, y);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    } else {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+}
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // Does new token `t` (its row of bits: `row` of the batch) see cell `cell` of its sequence?
 __device__ __forceinline__ bool sees(const AttnArgs& a, const Seq& s, int t, int row, int cell)
 {
@@ -244,5 +272,8 @@ __device__ __noinline__ float unseen_spoils(const AttnArgs& a, const Seq& s, int
     }
     return sum;
 }
+
+// rows: 128 or 256 to a unit; dp: head_dim rounded up to 64, 128 or 256 (128 rows alone)
+int launch_attention_tc(const fq_ctx* ctx, const AttnArgs& a, int dtype, int rows, int dp, cudaStream_t st);
 
 }  // namespace fq
