@@ -55,7 +55,7 @@ template <class T, int DP>
 __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const __grid_constant__ AttnArgs a)
 {
     using S = Shape<DP>;
-    using Work = Deal<kRows, S::kKeys, S::kThreads>;
+    using Work = Deal<kRows, S::kKeys, 3, S::kThreads>;
     constexpr int kUnits = DP / 8;               // 16-byte pieces of a row
     constexpr int kSteps = DP / 16;
     extern __shared__ __align__(1024) char smem[];
@@ -295,7 +295,12 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
             }
             const int n = w.tile * kRows + r, tok = n / a.share;
             if (odd && r < rows && d < a.head_dim)
-                for (int e = 0; e < 8; e++) v[e] += unseen_spoils<T>(a, w.s, w.b, w.head, tok, w.s.row0 + tok, d + e, k0, k1);
+#pragma unroll 1
+                for (int e = 0; e < 8; e++) {
+                    const float more_of = unseen_spoils<T>(a, w.s, w.b, w.head, tok, w.s.row0 + tok, d + e, k0, k1);
+#pragma unroll
+                    for (int x = 0; x < 8; x++) v[x] += x == e ? more_of : 0.0f;
+                }
             if (!whole) {
                 *reinterpret_cast<float4*>(part + r * DP + d) = make_float4(v[0], v[1], v[2], v[3]);
                 *reinterpret_cast<float4*>(part + r * DP + d + 4) = make_float4(v[4], v[5], v[6], v[7]);

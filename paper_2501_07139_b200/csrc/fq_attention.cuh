@@ -77,19 +77,19 @@ __device__ __forceinline__ int key_tiles(const AttnArgs& a, const Seq& s, int ro
 template <int ROWS>
 __device__ __forceinline__ int row_tiles(const AttnArgs& a, const Seq& s) { return (s.fresh * a.share + ROWS - 1) / ROWS; }
 
-// Cost of one key head of a sequence.
-template <int ROWS, int KEYS>
+// Cost of one key head of a sequence.  ENDS: key tiles that a unit's beginning and end take the time of.
+template <int ROWS, int KEYS, int ENDS>
 __device__ __forceinline__ long long head_cost(const AttnArgs& a, const Seq& s)
 {
     const int n = row_tiles<ROWS>(a, s);
-    if (a.mask || n <= 1) return (long long)n * (1 + key_tiles<ROWS, KEYS>(a, s, n - 1));
+    if (a.mask || n <= 1) return (long long)n * (ENDS + key_tiles<ROWS, KEYS>(a, s, n - 1));
     long long c = 0;
-    for (int r = 0; r < n; r++) c += 1 + key_tiles<ROWS, KEYS>(a, s, r);
+    for (int r = 0; r < n; r++) c += ENDS + key_tiles<ROWS, KEYS>(a, s, r);
     return c;
 }
 
 // This CTA's parts of units, one after the other.
-template <int ROWS, int KEYS, int THREADS>
+template <int ROWS, int KEYS, int ENDS, int THREADS>
 struct Deal {
     long long at, end, total;                    // cost position, of the CTA's end, of all work
     int b, head, tile;                           // sequence, key head, row tile
@@ -118,7 +118,7 @@ struct Deal {
                 long long c = 0;
                 if (b0 + tid < a.n_seqs) {
                     const Seq q(a, b0 + tid);
-                    c = q.fresh > 0 ? a.kv_heads * head_cost<ROWS, KEYS>(a, q) : 0;
+                    c = q.fresh > 0 ? a.kv_heads * head_cost<ROWS, KEYS, ENDS>(a, q) : 0;
                 }
                 long long in = c;
 #pragma unroll
@@ -159,27 +159,27 @@ struct Deal {
         b = (int)sums[W];
         s = Seq(a, b);
         unit = sums[W + 1];
-        const long long hc = head_cost<ROWS, KEYS>(a, s);
+        const long long hc = head_cost<ROWS, KEYS, ENDS>(a, s);
         head = (int)((at - unit) / hc);
         unit += head * hc;
         tile = 0;
         tiles = key_tiles<ROWS, KEYS>(a, s, 0);
-        while (at >= unit + 1 + tiles) {
-            unit += 1 + tiles;
+        while (at >= unit + ENDS + tiles) {
+            unit += ENDS + tiles;
             tile++;
             tiles = key_tiles<ROWS, KEYS>(a, s, tile);
         }
         return true;
     }
     // Key tiles [t0, t1) of the unit are this CTA's.  Its outputs are, if `whole`; else a part is left in scratch.
-    __device__ __forceinline__ int t0() const { return (int)max(0ll, at - unit - 1); }
-    __device__ __forceinline__ int t1() const { return (int)max(0ll, min(end - unit, 1ll + tiles) - 1); }
+    __device__ __forceinline__ int t0() const { return (int)max(0ll, at - unit - ENDS); }
+    __device__ __forceinline__ int t1() const { return (int)max(0ll, min(end - unit, (long long)ENDS + tiles) - ENDS); }
     __device__ __forceinline__ bool any() const { return t1() > t0() || (tiles == 0 && at == unit); }
     __device__ __forceinline__ bool whole() const { return t0() == 0 && t1() == tiles; }
     // CTAs behind this one that hold the unit's other parts
     __device__ __forceinline__ int others() const
     {
-        const long long last = unit + tiles;     // the last cost position of the unit
+        const long long last = unit + ENDS + tiles - 1;     // the last cost position of the unit
         // the CTA whose share holds it: share_of(c) <= last < share_of(c + 1)
         long long c = (long long)((unsigned long long)last * ctas(total) / (unsigned long long)total);
         while (share_of(total, (unsigned)c + 1) <= last) c++;
@@ -188,7 +188,7 @@ struct Deal {
     }
     __device__ __forceinline__ bool next(const AttnArgs& a)
     {
-        unit += 1 + tiles;
+        unit += ENDS + tiles;
         at = unit;
         if (at >= end) return false;
         if (++tile >= row_tiles<ROWS>(a, s)) {
@@ -260,7 +260,7 @@ template <> __device__ __forceinline__ bool finite16<__half>(uint32_t v) { retur
 // Infinities and NaNs among the values of new tokens are taken out before the product, where a weight of 0 would spread them to rows that do not
 // see them; this puts them where they belong.  Rare: a unit whose tiles had any comes here.  Returns what is to be added to value d of a row.
 template <class T>
-__device__ __noinline__ float unseen_spoils(const AttnArgs& a, const Seq& s, int b, int head, int t, int row, int d, int cell0, int cell1)
+__device__ __forceinline__ float unseen_spoils(const AttnArgs& a, const Seq& s, int b, int head, int t, int row, int d, int cell0, int cell1)
 {
     float sum = 0.0f;
     for (int cell = max(cell0, s.ctx); cell < min(cell1, s.len); cell++) {

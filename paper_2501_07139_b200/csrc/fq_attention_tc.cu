@@ -30,6 +30,7 @@ struct TcShape {
     static constexpr int kSoftmax = 4 * NQ;                                  // warps
     static constexpr int kWarps = kSoftmax + 4;
     static constexpr int kThreads = kWarps * 32;
+    static constexpr int kEnds = 5;                                          // key tiles' time that a unit's ends take
     static constexpr int kQBytes = 128 * DP * 2;                             // of a query tile
     static constexpr int kSlotBytes = kKeys * DP * 2;
     static constexpr int kSlots = NQ * kQBytes + 6 * kSlotBytes <= 226 * 1024 ? (DP == 64 ? 8 : 6) : 5;
@@ -221,7 +222,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     const __grid_constant__ CUtensorMap q_map, int run)
 {
     using S = TcShape<DP, NQ>;
-    using Work = Deal<S::kRows, S::kKeys, S::kThreads>;
+    using Work = Deal<S::kRows, S::kKeys, S::kEnds, S::kThreads>;
     constexpr int kUnits = DP / 8;               // 16-byte pieces of a row
     extern __shared__ char smem_raw[];
     char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
@@ -397,10 +398,14 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     for (int j = 0; j < 32; j++) v[j] = 0.0f;
                 }
                 if (!real) continue;
-                if (odd)
+                if (odd) {
+#pragma unroll 1
+                    for (int j = 0; j < 32 && c + j < a.head_dim; j++) {
+                        const float more_of = unseen_spoils<T>(a, w.s, w.b, w.head, t, row, c + j, t0 * S::kKeys, w.t1() * S::kKeys);
 #pragma unroll
-                    for (int j = 0; j < 32; j++)
-                        if (c + j < a.head_dim) v[j] += unseen_spoils<T>(a, w.s, w.b, w.head, t, row, c + j, t0 * S::kKeys, w.t1() * S::kKeys);
+                        for (int i = 0; i < 32; i++) v[i] += i == j ? more_of : 0.0f;
+                    }
+                }
                 if (whole) {
 #pragma unroll
                     for (int j = 0; j < 32; j += 8)
