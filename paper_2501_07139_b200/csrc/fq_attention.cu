@@ -1,9 +1,10 @@
 // Attention of a sequence's last tokens over its paged cache, up to 16 query rows a tile (single tokens, small trees): bound by reading keys and values.
 //
-// One CTA an SM, every warp by itself: a tile of keys is 16 cells for each warp, fetched by its own asynchronous copies into its own ring (192 KB an SM, of
-// which two thirds are on their way), so that no warp waits for another until the unit's end.  The online softmax is kept per warp;
-// at the end the warps' maxima, sums and values are joined through shared memory.  Scores and values are formed by mma.m16n8k16: at 16 rows the bytes of
-// a key take ten times as long to arrive as its products take.
+// Every warp is a worker: it has a share of the batch's work of its own, which it fetches by its own asynchronous copies, 16 cells at a time, into its own
+// ring (192 KB an SM, of which two thirds are on their way), so that nobody waits for another before the end of the kernel; there the warps join
+// what they have of the same units.  (With a unit's keys dealt to all warps of a CTA, and their parts joined at its end, a unit's ends took 4 us of the
+// CTA: 48 tokens of a ragged batch, 40 heads, 391 us.)  Scores and values are formed by mma.m16n8k16: at 16 rows the bytes
+// of a key take ten times as long to arrive as its products take.
 #include "fq_attention.cuh"
 
 #include <atomic>
@@ -21,17 +22,18 @@ template <int DP>
 struct Shape {                                   // DP: head_dim, rounded up to 64, 128 or 256
     static constexpr int kWarps = DP == 256 ? 4 : 8;
     static constexpr int kThreads = kWarps * 32;
-    static constexpr int kKeys = kWarps * kChunk;
     static constexpr int kStageBytes = 2 * kChunk * DP * 2;                  // of a warp: keys, then values
     static constexpr int kStages = 196608 / (kWarps * kStageBytes);
-    static constexpr int kSets = kWarps / 2;                                 // sets of values that meet at a unit's end
-    static constexpr int oSets = kWarps * kStages * kStageBytes;
-    static constexpr int oMl = oSets + kSets * kRows * DP * 4;       // float2 [warps][rows]
-    static constexpr int oSums = oMl + kWarps * kRows * 8;                   // long long [warps + 4]
-    static constexpr int oSpoilt = oSums + (kWarps + 4) * 8;
-    static constexpr int kTotal = oSpoilt + 16;
+    static constexpr int kSlot = kRows * (DP + 2);                           // floats of a part: [rows][DP], maxima, sums
+    // A unit's ends (the queries' way here, the results' way out) take the time of two chunks; a worker gets no less than four.
+    using Work = Deal<kRows, kChunk, 2, kThreads, kWarps, 4>;
+    static constexpr int oSums = kWarps * kStages * kStageBytes;             // long long [Work::kSums]
+    static constexpr int oFlags = oSums + Work::kSums * 8;                   // int [warps]
+    static constexpr int kTotal = oFlags + kWarps * 4;
     static_assert(kTotal <= 232448, "shared memory over the per-CTA limit");
 };
+// What a warp leaves: a part of the unit that it continues, whether that ends here, a part of a unit that ends elsewhere.
+enum { kContinues = 1, kEnds = 2, kBegins = 4 };
 
 __device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t addr)
 {
@@ -51,33 +53,82 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// Parts 0 .. n - 1 of row r become one: their values d .. d + 3 (at offset `at`), the row's maximum (at `om`) and sum (at `ol`).  part(x): where part x is.
+struct Joined { float4 v; float top, sum; };
+template <class Part>
+__device__ __forceinline__ Joined join_parts(Part part, int n, int at, int om, int ol)
+{
+    Joined j{make_float4(0.0f, 0.0f, 0.0f, 0.0f), -INFINITY, 0.0f};
+    // (eight at a time: their loads are on their way together)
+    for (int x0 = 0; x0 < n; x0 += 8) {
+        float m[8], l[8];
+        float4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            m[i] = -INFINITY;
+            l[i] = 0.0f;
+            v[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (x0 + i < n) {
+                const float* p = part(x0 + i);
+                m[i] = p[om];
+                l[i] = p[ol];
+                v[i] = *reinterpret_cast<const float4*>(p + at);
+            }
+        }
+        float top = j.top;
+#pragma unroll
+        for (int i = 0; i < 8; i++) top = fmaxf(top, m[i]);
+        const float base = top == -INFINITY ? 0.0f : top;
+        float by = exp2_fast(j.top - base);
+        j.top = top;
+        j.sum *= by;
+        j.v = make_float4(j.v.x * by, j.v.y * by, j.v.z * by, j.v.w * by);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            by = exp2_fast(m[i] - base);
+            j.sum += l[i] * by;
+            j.v.x += v[i].x * by; j.v.y += v[i].y * by; j.v.z += v[i].z * by; j.v.w += v[i].w * by;
+        }
+    }
+    return j;
+}
+// Row r of a unit, values d .. d + 3.
+template <class T>
+__device__ __forceinline__ void write_out(const AttnArgs& a, int row0, int n, int head, int d, const Joined& j)
+{
+    const float by = j.sum == 0.0f ? 0.0f : 1.0f / j.sum;
+    const int t = n / a.share, h = head * a.share + n - t * a.share;
+    const long long at = row0 + t;
+    *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * a.out_token + h * a.out_head + d) =
+        make_uint2(pack2<T>(j.v.x * by, j.v.y * by), pack2<T>(j.v.z * by, j.v.w * by));
+    if (a.lse && d == 0) a.lse[at * (a.kv_heads * a.share) + h] = j.sum == 0.0f ? -INFINITY : (j.top + log2f(j.sum)) * 0.69314718055994531f;
+}
+
 template <class T, int DP>
 __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const __grid_constant__ AttnArgs a)
 {
     using S = Shape<DP>;
-    using Work = Deal<kRows, S::kKeys, 3, S::kThreads>;
+    using Work = typename S::Work;
     constexpr int kUnits = DP / 8;               // 16-byte pieces of a row
     constexpr int kSteps = DP / 16;
     extern __shared__ __align__(1024) char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     const uint32_t ring = smem_u32(smem) + warp * S::kStages * S::kStageBytes;
-    float* sets = reinterpret_cast<float*>(smem + S::oSets);
-    float2* ml = reinterpret_cast<float2*>(smem + S::oMl);
-    volatile int* spoilt = reinterpret_cast<volatile int*>(smem + S::oSpoilt);
+    volatile int* flags = reinterpret_cast<volatile int*>(smem + S::oFlags);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");              // (the joining kernel waits for this one's end)
     if (tid == 0) {
         AttnJoin none{};
         a.joins[blockIdx.x] = none;
-        spoilt[0] = spoilt[1] = 0;
     }
     Work w;
-    if (!w.begin(a, reinterpret_cast<long long*>(smem + S::oSums))) return;
+    const bool some = w.begin(a, reinterpret_cast<long long*>(smem + S::oSums));
     const int pieces = a.head_dim / 8;
+    float* parts = a.parts + (long long)(blockIdx.x * S::kWarps + warp) * 2 * S::kSlot;
 
     // ---- fetching runs ahead of computing, over the ends of units
     Work f = w;
-    int f_tile = f.t0(), f_stage = 0, f_block = -1;
-    bool f_more = true;
+    int f_tile = 0, f_stage = 0, f_block = -1;
+    bool f_more = some;
     const auto settle = [&]() {                  // f at a unit with key tiles, and its next tile's block on the way
         while (f_more && f_tile >= f.t1()) {
             f_more = f.next(a);
@@ -85,13 +136,13 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
         }
         f_block = -1;
         if (f_more) {
-            const int cell = f_tile * S::kKeys + warp * kChunk + (lane & 15);
+            const int cell = f_tile * kChunk + (lane & 15);
             if (cell < f.s.len) f_block = a.table[f.b * a.ld + cell / a.block_size];
         }
     };
     const auto fetch = [&]() {
         if (f_more) {
-            const int cell = f_tile * S::kKeys + warp * kChunk + (lane & 15);
+            const int cell = f_tile * kChunk + (lane & 15);
             long long place = -1;
             if (cell < f.s.len) {
                 if ((unsigned)f_block < (unsigned)a.blocks) place = f_block * a.block_stride + cell % a.block_size * a.cell_stride + f.head * a.head_stride;
@@ -114,14 +165,20 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
         f_stage = f_stage + 1 == S::kStages ? 0 : f_stage + 1;
         copies_commit();
     };
-    settle();
+    if (some) {
+        f_tile = f.t0();
+        settle();
+    }
 #pragma unroll 1
     for (int i = 0; i < S::kStages - 1; i++) fetch();
 
-    int stage = 0, turn = 0;
-    for (bool more = true; more; more = w.next(a)) {
-        if (!w.any()) continue;
-        const int rows = w.s.fresh * a.share - w.tile * kRows;                   // of the unit, from this tile on
+    int stage = 0, flag = 0, lead_rows = 0;
+    for (bool more = some; more;) {
+        if (!w.any()) {
+            more = w.next(a);
+            continue;
+        }
+        const int rows = min(w.s.fresh * a.share - w.tile * kRows, kRows);       // of the unit
         int t[2], row[2];                                                        // this lane's two rows: new token, row of the batch
 #pragma unroll
         for (int h = 0; h < 2; h++) {
@@ -132,7 +189,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             const int r = min(w.tile * kRows + g + 8 * h, w.s.fresh * a.share - 1);
-            const T* q = static_cast<const T*>(a.q) + row[h] * a.q_token + (w.head * a.share + r % a.share) * a.q_head;
+            const T* q = static_cast<const T*>(a.q) + row[h] * a.q_token + (w.head * a.share + r - t[h] * a.share) * a.q_head;
 #pragma unroll
             for (int k = 0; k < kSteps; k++)
 #pragma unroll
@@ -149,15 +206,15 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
         // cells before this one are seen by all rows of the tile
         const int all_see = a.mask ? w.s.ctx : w.s.ctx + w.tile * kRows / a.share + 1;
-        const int t1 = w.t1();
-        for (int tile = w.t0(); tile < t1; tile++) {
+        const int t0 = w.t0(), t1 = w.t1();
+        bool odd = false;                        // infinities or NaNs among values that not all rows see
+        for (int tile = t0; tile < t1; tile++) {
             copies_wait<S::kStages - 2>();
             __syncwarp();
             fetch();
             const uint32_t ks = ring + stage * S::kStageBytes, vs = ks + kChunk * DP * 2;
             stage = stage + 1 == S::kStages ? 0 : stage + 1;
-            const int cell0 = tile * S::kKeys + warp * kChunk;
-            if (cell0 >= w.s.len) continue;
+            const int cell0 = tile * kChunk;
             float sc[2][4];
 #pragma unroll
             for (int n = 0; n < 2; n++)
@@ -182,8 +239,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
                     for (int i = 0; i < 4; i++)
                         if (!sees(a, w.s, t[i >> 1], row[i >> 1], cell0 + n * 8 + 2 * c + (i & 1))) sc[n][i] = -INFINITY;
                 // values that not all rows see: none may be infinite or NaN in the product
-                bool odd = false;
-#pragma unroll
+#pragma unroll 1
                 for (int i = 0; i < kChunk * kUnits / 32; i++) {
                     const uint32_t at = vs + (uint32_t)(i * 32 + lane) * 16;
                     const uint4 v = lds128(at);
@@ -195,7 +251,6 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
                     for (int j = 0; j < 4; j++) out[j] = (finite16<T>(in[j] & 0xffffu) ? in[j] & 0xffffu : 0u) | (finite16<T>(in[j] & 0xffff0000u) ? in[j] & 0xffff0000u : 0u);
                     sts128(at, make_uint4(out[0], out[1], out[2], out[3]));
                 }
-                if (odd) spoilt[turn] = 1;
                 __syncwarp();
             }
             // online softmax: a row is four lanes'
@@ -233,137 +288,123 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
                 mma16816<T>(o[2 * n + 1], pf, b[2], b[3]);
             }
         }
-        // ---- the warps' parts are joined
+        // ---- the unit's end, or this worker's
+        const bool whole = w.whole();
+        // A part that does not end its share goes to scratch, else to this warp's ring, which nobody needs any more.
+        const bool last = !whole && t1 < w.tiles;
+        if (last) {
+            copies_wait<0>();
+            __syncwarp();
+        }
+        float* part = last ? reinterpret_cast<float*>(smem + warp * S::kStages * S::kStageBytes) : parts;
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
             l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-            if (c == 0) ml[warp * kRows + g + 8 * h] = make_float2(m[h], l[h]);
-        }
-        __syncthreads();
+            const int r = g + 8 * h;
+            if (r >= rows) continue;
+            if (whole) {
+                const float by = l[h] == 0.0f ? 0.0f : 1.0f / l[h];
+                const int head = w.head * a.share + w.tile * kRows + r - t[h] * a.share;
+                T* out = static_cast<T*>(a.out) + row[h] * a.out_token + head * a.out_head;
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            float top = -INFINITY;
+                for (int n = 0; n < DP / 8; n++)
+                    if (n < pieces) *reinterpret_cast<uint32_t*>(out + n * 8 + 2 * c) = pack2<T>(o[n][2 * h] * by, o[n][2 * h + 1] * by);
+                if (a.lse && c == 0) a.lse[(long long)row[h] * (a.kv_heads * a.share) + head] = l[h] == 0.0f ? -INFINITY : (m[h] + log2f(l[h])) * 0.69314718055994531f;
+            } else {
 #pragma unroll
-            for (int i = 0; i < S::kWarps; i++) top = fmaxf(top, ml[i * kRows + g + 8 * h].x);
-            const float by = exp2_fast(m[h] - (top == -INFINITY ? 0.0f : top));
-#pragma unroll
-            for (int n = 0; n < DP / 8; n++) { o[n][2 * h] *= by; o[n][2 * h + 1] *= by; }
-        }
-        // (eight values of a row move within it by the row's number, so that the four rows of a half-warp's access lie in different banks)
-        float* mine = sets + ((warp % S::kSets) * kRows + g) * DP + 2 * c;
-        if (warp < S::kSets) {
-#pragma unroll
-            for (int n = 0; n < DP / 8; n++) {
-                *reinterpret_cast<float2*>(mine + (n ^ (g & 3)) * 8) = make_float2(o[n][0], o[n][1]);
-                *reinterpret_cast<float2*>(mine + 8 * DP + (n ^ (g & 3)) * 8) = make_float2(o[n][2], o[n][3]);
+                for (int n = 0; n < DP / 8; n++) *reinterpret_cast<float2*>(part + r * DP + n * 8 + 2 * c) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
+                if (c == 0) {
+                    part[kRows * DP + r] = m[h];
+                    part[kRows * (DP + 1) + r] = l[h];
+                }
             }
         }
-        __syncthreads();
-        if (warp >= S::kSets) {
-#pragma unroll
-            for (int n = 0; n < DP / 8; n++) {
-                float2* x = reinterpret_cast<float2*>(mine + (n ^ (g & 3)) * 8);
-                float2* y = reinterpret_cast<float2*>(mine + 8 * DP + (n ^ (g & 3)) * 8);
-                *x = make_float2(x->x + o[n][0], x->y + o[n][1]);
-                *y = make_float2(y->x + o[n][2], y->y + o[n][3]);
-            }
-        }
-        __syncthreads();
-        const bool whole = w.whole(), odd = spoilt[turn];
-        const int k0 = w.t0() * S::kKeys, k1 = t1 * S::kKeys;
-        float* part = a.parts + (long long)(blockIdx.x * 2 + (w.t0() == 0)) * kRows * (DP + 2);
-        for (int i = tid; i < kRows * kUnits; i += S::kThreads) {
-            const int r = i / kUnits, d = i % kUnits * 8;
-            float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-            for (int j = 0; j < S::kWarps; j++) top = fmaxf(top, ml[j * kRows + r].x);
-#pragma unroll
-            for (int j = 0; j < S::kWarps; j++) {
-                const float2 x = ml[j * kRows + r];
-                sum += x.y * exp2_fast(x.x - (top == -INFINITY ? 0.0f : top));
-            }
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; e++) v[e] = 0.0f;
-#pragma unroll
-            for (int j = 0; j < S::kSets; j++) {
-                const float4* x = reinterpret_cast<const float4*>(sets + (j * kRows + r) * DP + (d ^ (r & 3) * 8));
-                const float4 x0 = x[0], x1 = x[1];
-                v[0] += x0.x; v[1] += x0.y; v[2] += x0.z; v[3] += x0.w;
-                v[4] += x1.x; v[5] += x1.y; v[6] += x1.z; v[7] += x1.w;
-            }
-            const int n = w.tile * kRows + r, tok = n / a.share;
-            if (odd && r < rows && d < a.head_dim)
+        if (__any_sync(0xffffffffu, odd)) {
+            __syncwarp();
 #pragma unroll 1
-                for (int e = 0; e < 8; e++) {
-                    const float more_of = unseen_spoils<T>(a, w.s, w.b, w.head, tok, w.s.row0 + tok, d + e, k0, k1);
-#pragma unroll
-                    for (int x = 0; x < 8; x++) v[x] += x == e ? more_of : 0.0f;
-                }
-            if (!whole) {
-                *reinterpret_cast<float4*>(part + r * DP + d) = make_float4(v[0], v[1], v[2], v[3]);
-                *reinterpret_cast<float4*>(part + r * DP + d + 4) = make_float4(v[4], v[5], v[6], v[7]);
-                if (d == 0) {
-                    part[kRows * DP + r] = top;
-                    part[kRows * DP + kRows + r] = sum;
-                }
-                continue;
+            for (int i = lane; i < rows * a.head_dim; i += 32) {
+                const int r = i / a.head_dim, d = i - r * a.head_dim, n = w.tile * kRows + r, tok = n / a.share;
+                const float x = spoilt_value<T>(a, w.s, w.b, w.head, tok, d, t0 * kChunk, t1 * kChunk);
+                if (x == 0.0f) continue;
+                if (whole) static_cast<T*>(a.out)[(long long)(w.s.row0 + tok) * a.out_token + (w.head * a.share + n - tok * a.share) * a.out_head + d] = (T)x;
+                else part[r * DP + d] = x;
             }
-            if (r >= rows || d >= a.head_dim) continue;
-            const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
-            const int h = w.head * a.share + n % a.share;
-            const long long at = w.s.row0 + tok;
-            *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + at * a.out_token + h * a.out_head + d) =
-                make_uint4(pack2<T>(v[0] * by, v[1] * by), pack2<T>(v[2] * by, v[3] * by), pack2<T>(v[4] * by, v[5] * by), pack2<T>(v[6] * by, v[7] * by));
-            if (a.lse && d == 0) a.lse[at * (a.kv_heads * a.share) + h] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
         }
-        if (tid == 0 && !whole && w.t0() == 0) a.joins[blockIdx.x] = AttnJoin{w.b, w.tile * kRows, w.head, w.others(), min(rows, kRows), {0, 0, 0}};
-        turn ^= 1;
-        if (tid == 0) spoilt[turn] = 0;          // (the next unit's; the last to read it did so before that unit's last barrier)
-        __syncthreads();
+        if (!whole && t0 > 0) {
+            flag |= t1 == w.tiles ? kContinues | kEnds : kContinues;
+            lead_rows = rows;
+        }
+        if (!whole && t0 == 0) {
+            flag |= kBegins;                     // (the share's last unit: w stays at it)
+            break;
+        }
+        more = w.next(a);
     }
     copies_wait<0>();
+
+    // ---- what the warps have of the same units
+    if (lane == 0) flags[warp] = flag;
+    __syncthreads();
+    // Parts of warps `first` .. that are of one unit: all of it, or what goes to scratch for the other kernel.
+    const auto join = [&](int first, int rows, bool begins) {
+        int n = 1;
+        bool ends = !begins && (flags[first] & kEnds);
+        if (ends) return true;                   // (in scratch already)
+        while (!ends && first + n < w.per_cta && (flags[first + n] & kContinues)) {
+            ends = flags[first + n] & kEnds;
+            n++;
+        }
+        const bool out = begins && ends;
+        const float* last = a.parts + (long long)(blockIdx.x * S::kWarps + first + n - 1) * 2 * S::kSlot;
+        const auto part = [&](int x) -> const float* {
+            return ends && x == n - 1 ? last : reinterpret_cast<const float*>(smem + (first + x) * S::kStages * S::kStageBytes);
+        };
+        float* to = parts + (begins ? S::kSlot : 0);
+        for (int i = lane; i < rows * (DP / 4); i += 32) {
+            const int r = i / (DP / 4), d = i % (DP / 4) * 4;
+            if (d >= a.head_dim) continue;
+            const Joined j = join_parts(part, n, r * DP + d, kRows * DP + r, kRows * (DP + 1) + r);
+            if (out) {
+                write_out<T>(a, w.s.row0, w.tile * kRows + r, w.head, d, j);
+                continue;
+            }
+            *reinterpret_cast<float4*>(to + r * DP + d) = j.v;
+            if (d == 0) {
+                to[kRows * DP + r] = j.top;
+                to[kRows * (DP + 1) + r] = j.sum;
+            }
+        }
+        return ends;
+    };
+    if (warp == 0 && (flag & kContinues)) join(0, lead_rows, false);
+    if (flag & kBegins) {
+        const int rows = min(w.s.fresh * a.share - w.tile * kRows, kRows);
+        if (!join(warp, rows, true) && lane == 0)
+            a.joins[blockIdx.x] = AttnJoin{w.s.row0, w.tile * kRows, w.head, w.others(), rows, (int)(blockIdx.x * S::kWarps + warp) * 2 + 1, {0, 0}};
+    }
 }
 
-// Joins the parts of units that were cut: CTAs x take those of the unit that begins in CTA x of the kernel before, each y a share of its values.
+// Joins the parts of units that were cut between CTAs: CTAs x take those of the unit that begins in CTA x of the kernel before, each y a share of its values.
 //   rows_of_tile : rows of a part;  by_piece : a part lies as [dp / 4][rows][4], else as [rows][dp];  behind that the rows' maxima and sums
+//   workers : of a CTA, each with two slots
 constexpr int kJoinThreads = 256, kJoinPieces = 1024;
 template <class T>
-__global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __grid_constant__ AttnArgs a, int rows_of_tile, int dp, int by_piece)
+__global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __grid_constant__ AttnArgs a, int rows_of_tile, int dp, int by_piece, int workers)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const AttnJoin j = a.joins[blockIdx.x];
     if (j.others == 0) return;
-    const int s0 = a.starts[j.seq], per_row = dp / 4, end = min(rows_of_tile * per_row, ((int)blockIdx.y + 1) * kJoinPieces);
+    const int per_row = dp / 4, end = min(rows_of_tile * per_row, ((int)blockIdx.y + 1) * kJoinPieces);
     const long long slot = (long long)rows_of_tile * (dp + 2);
-    // the first part is the second slot of its CTA, the others are the first slots of those behind it
-    const float* first = a.parts + (blockIdx.x * 2 + 1) * slot;
-    const float* rest = a.parts + (blockIdx.x + 1) * 2 * slot;
+    const float* first = a.parts + j.slot * slot;
+    const float* rest = a.parts + (blockIdx.x + 1) * 2 * workers * slot;         // (of what a CTA continues, its first worker has all)
     for (int i = blockIdx.y * kJoinPieces + threadIdx.x; i < end; i += kJoinThreads) {
         const int r = by_piece ? i % rows_of_tile : i / per_row, d = (by_piece ? i / rows_of_tile : i % per_row) * 4;
         if (r >= j.rows || d >= a.head_dim) continue;
-        const long long om = (long long)rows_of_tile * dp + r, ol = om + rows_of_tile;
-        float top = __ldcg(first + om);
-#pragma unroll 4
-        for (int x = 0; x < j.others; x++) top = fmaxf(top, __ldcg(rest + x * 2 * slot + om));
-        const float base = top == -INFINITY ? 0.0f : top;
-        float by = exp2_fast(__ldcg(first + om) - base), sum = __ldcg(first + ol) * by;
-        float4 v = __ldcg(reinterpret_cast<const float4*>(first) + i);
-        v = make_float4(v.x * by, v.y * by, v.z * by, v.w * by);
-#pragma unroll 4
-        for (int x = 0; x < j.others; x++) {
-            const float* p = rest + x * 2 * slot;
-            by = exp2_fast(__ldcg(p + om) - base);
-            sum += __ldcg(p + ol) * by;
-            const float4 u = __ldcg(reinterpret_cast<const float4*>(p) + i);
-            v.x += u.x * by; v.y += u.y * by; v.z += u.z * by; v.w += u.w * by;
-        }
-        by = sum == 0.0f ? 0.0f : 1.0f / sum;
-        const int n = j.row0 + r, h = j.head * a.share + n % a.share;
-        const long long at = s0 + n / a.share;
-        *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * a.out_token + h * a.out_head + d) = make_uint2(pack2<T>(v.x * by, v.y * by), pack2<T>(v.z * by, v.w * by));
-        if (a.lse && d == 0) a.lse[at * (a.kv_heads * a.share) + h] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
+        const int om = rows_of_tile * dp + r;
+        const auto part = [&](int x) { return x == 0 ? first : rest + (x - 1) * 2 * workers * slot; };
+        write_out<T>(a, j.seq_row0, j.row0 + r, j.head, d, join_parts(part, j.others + 1, i * 4, om, om + rows_of_tile));
     }
 }
 
@@ -391,6 +432,10 @@ int unit_rows(int new_tokens, int share, int dp)
     return rows <= kRows ? kRows : rows <= 128 || dp == 256 ? 128 : 256;
 }
 
+// Workers of a CTA: warps of this file's kernel, the CTA of the other.
+int workers_of(int rows, int dp) { return rows > kRows ? 1 : dp == 256 ? Shape<256>::kWarps : Shape<128>::kWarps; }
+static_assert(Shape<64>::kWarps == Shape<128>::kWarps, "workers_of");
+
 template <class T>
 int launch_typed(const fq_ctx* ctx, const AttnArgs& a, int rows, int dp, cudaStream_t st)
 {
@@ -406,7 +451,7 @@ int launch_typed(const fq_ctx* ctx, const AttnArgs& a, int rows, int dp, cudaStr
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)ctx->sm_count, (unsigned)((rows * dp / 4 + kJoinPieces - 1) / kJoinPieces)); cfg.blockDim = dim3(kJoinThreads);
     cfg.stream = st; cfg.attrs = &attr; cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attention_join_kernel<T>, a, rows, dp, rows > kRows ? 1 : 0) == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, attention_join_kernel<T>, a, rows, dp, rows > kRows ? 1 : 0, workers_of(rows, dp)) == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
 }
 
 bool good_sizes(const fq_ctx* ctx, int n_seqs, int tokens, int q_heads, int cache_heads, int head_dim, int new_tokens)
@@ -428,7 +473,7 @@ size_t fq_tree_attention_scratch(const fq_ctx* ctx, int n_seqs, int tokens, int 
 {
     if (!ctx || !good_sizes(ctx, n_seqs, tokens, q_heads, cache_heads, head_dim, new_tokens)) return 0;
     const int dp = padded_dim(head_dim), rows = unit_rows(new_tokens, q_heads / cache_heads, dp);
-    return join_bytes(ctx) + (size_t)ctx->sm_count * 2 * rows * (dp + 2) * sizeof(float);
+    return join_bytes(ctx) + (size_t)ctx->sm_count * workers_of(rows, dp) * 2 * rows * (dp + 2) * sizeof(float);
 }
 
 int fq_tree_attention(fq_ctx* ctx, const fq_heads* q, const fq_heads* out, const fq_cache* cache, int dtype, int head_dim, int tokens, int n_seqs,

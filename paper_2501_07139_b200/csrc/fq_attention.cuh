@@ -1,10 +1,10 @@
-// What the attention kernels share: their arguments, how the work of a batch is dealt to thread blocks, and what a row sees.
+// What the attention kernels share: their arguments, how the work of a batch is dealt, and what a row sees.
 //
 // Work.  A unit is one key head of one sequence and a tile of its query rows: the query heads that share the key head, for all new tokens, are rows
 // r = token * share + head, so that keys and values are read once for all of them.  A unit costs the key tiles that its rows see and
-// one more for its ends.  The host does not know the lengths, so every CTA adds the costs up for itself and takes an equal share of the sum: units of
-// long sequences are cut, and each part leaves (sum, maximum, values) in scratch, which a second small kernel joins.  The parts and
-// their order depend on the lengths alone.
+// some more for its ends.  The host does not know the lengths, so every CTA adds the costs up for itself; a worker (a CTA, or a warp) takes an equal
+// share of the sum.  Units of long sequences are cut: each part leaves (maximum, sum, values) in scratch, and they are joined by the CTA whose
+// warps have them all, or by a second small kernel.  The parts and their order depend on the lengths alone.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -35,16 +35,17 @@ struct AttnArgs {
     int words;
     float scale;                                 // times log2 e
     float* lse;
-    float* parts;                                // two slots a CTA: rows x (head_dim + 2)
+    float* parts;                                // two slots a worker, rows x (head_dim + 2): of the unit it continues, of the one it leaves unfinished
     struct AttnJoin* joins;                      // one a CTA
     int* status;
 };
 
 // A unit that begins in this CTA and ends in another.
 struct AttnJoin {
-    int seq, row0, head, others;                 // others: CTAs behind this one that hold parts (0: nothing to join)
+    int seq_row0, row0, head, others;            // first rows of the sequence in the batch and of the unit in the sequence; others: CTAs behind this one that hold parts (0: nothing to join)
     int rows;                                    // rows of the unit
-    int pad[3];
+    int slot;                                    // where its first part is
+    int pad[2];
 };
 
 struct Seq {
@@ -88,30 +89,52 @@ __device__ __forceinline__ long long head_cost(const AttnArgs& a, const Seq& s)
     return c;
 }
 
-// This CTA's parts of units, one after the other.
-template <int ROWS, int KEYS, int ENDS, int THREADS>
+// A worker's parts of units, one after the other.
+//   WARPS : workers of a CTA: its warps, or 1: the CTA is one;  LEAST : a worker's share, at least, in key tiles
+template <int ROWS, int KEYS, int ENDS, int THREADS, int WARPS = 1, int LEAST = 1>
 struct Deal {
-    long long at, end, total;                    // cost position, of the CTA's end, of all work
+    long long at, end, total;                    // cost position, of the share's end, of all work
     int b, head, tile;                           // sequence, key head, row tile
     Seq s;
     int tiles;                                   // key tiles of the unit
     long long unit;                              // where the unit begins
+    int per_cta;                                 // workers of a CTA that have work: fewer where there is little of it
 
-    // CTAs with work: each has one position at least.  (total < 2^51: cells of a sequence < 2^30, rows of the batch <= 2^30.)
-    static __device__ __forceinline__ unsigned ctas(long long total) { return (unsigned)min((long long)gridDim.x, total); }
-    static __device__ __forceinline__ long long share_of(long long total, unsigned cta)
+    static constexpr int kSums = THREADS / 32 + 3 * WARPS;       // long longs of shared memory that begin() needs
+
+    // (total < 2^51: cells of a sequence < 2^30, rows of the batch <= 2^30.)
+    __device__ __forceinline__ unsigned workers() const { return (unsigned)min((long long)gridDim.x * per_cta, total); }
+    __device__ __forceinline__ long long share_of(unsigned worker) const
     {
-        const unsigned n = ctas(total);
-        return cta >= n ? total : (long long)((unsigned long long)total * cta / n);
+        const unsigned n = workers();
+        if (worker >= n) return total;
+        if (total < 1 << 20) return (unsigned)total * worker / n;                // (n < 2^12; dividing 64 bits takes five times as long)
+        return (long long)((unsigned long long)total * worker / n);
     }
 
-    // All threads of the CTA; `sums` is shared memory of THREADS / 32 + 4 long longs.  False: nothing to do.
+    // All threads of the CTA.  False: nothing to do for this worker.
     __device__ __forceinline__ bool begin(const AttnArgs& a, long long* sums)
     {
         constexpr int W = THREADS / 32;
         const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-        long long base = 0, from = 0;
+        long long base = 0;
         total = 0;
+        per_cta = 1;
+        const auto found = [&](long long excl, long long c, int seq) {           // of the sequence at [excl, excl + c): the workers that begin in it
+            for (int j = 0; j < per_cta; j++) {
+                const long long from = sums[W + 2 * WARPS + j];
+                if (from >= excl && from < excl + c) {
+                    sums[W + 2 * j] = seq;
+                    sums[W + 2 * j + 1] = excl;
+                }
+            }
+        };
+        const auto known = [&](long long all) {
+            total = all;
+            per_cta = (int)min((long long)WARPS, max(1ll, all / ((long long)LEAST * gridDim.x)));
+            if (tid < per_cta) sums[W + 2 * WARPS + tid] = share_of(blockIdx.x * per_cta + tid);
+            __syncthreads();
+        };
         for (int pass = 0; pass < 2; pass++) {
             base = 0;
             for (int b0 = 0; b0 < a.n_seqs; b0 += THREADS) {
@@ -135,30 +158,24 @@ struct Deal {
                     if (w < warp) before += sums[w];
                     all += sums[w];
                 }
-                const long long excl = base + before + in - c;
                 if (a.n_seqs <= THREADS) {       // one look is enough
-                    total = all;
-                    from = share_of(total, blockIdx.x);
+                    known(all);
                     pass = 1;
                 }
-                if (pass == 1 && c > 0 && from >= excl && from < excl + c) {
-                    sums[W] = b0 + tid;
-                    sums[W + 1] = excl;
-                }
+                if (pass == 1 && c > 0) found(base + before + in - c, c, b0 + tid);
                 base += all;
             }
-            if (pass == 0) {
-                total = base;
-                from = share_of(total, blockIdx.x);
-            }
+            if (pass == 0) known(base);
         }
         __syncthreads();
-        at = from;
-        end = share_of(total, blockIdx.x + 1);
+        const int mine = WARPS > 1 ? warp : 0;
+        if (mine >= per_cta) return false;
+        at = sums[W + 2 * WARPS + mine];
+        end = share_of(blockIdx.x * per_cta + mine + 1);
         if (at >= end) return false;
-        b = (int)sums[W];
+        b = (int)sums[W + 2 * mine];
         s = Seq(a, b);
-        unit = sums[W + 1];
+        unit = sums[W + 2 * mine + 1];
         const long long hc = head_cost<ROWS, KEYS, ENDS>(a, s);
         head = (int)((at - unit) / hc);
         unit += head * hc;
@@ -171,7 +188,7 @@ struct Deal {
         }
         return true;
     }
-    // Key tiles [t0, t1) of the unit are this CTA's.  Its outputs are, if `whole`; else a part is left in scratch.
+    // Key tiles [t0, t1) of the unit are this worker's.  Its outputs are, if `whole`; else a part is left in scratch.
     __device__ __forceinline__ int t0() const { return (int)max(0ll, at - unit - ENDS); }
     __device__ __forceinline__ int t1() const { return (int)max(0ll, min(end - unit, (long long)ENDS + tiles) - ENDS); }
     __device__ __forceinline__ bool any() const { return t1() > t0() || (tiles == 0 && at == unit); }
@@ -180,11 +197,11 @@ struct Deal {
     __device__ __forceinline__ int others() const
     {
         const long long last = unit + ENDS + tiles - 1;     // the last cost position of the unit
-        // the CTA whose share holds it: share_of(c) <= last < share_of(c + 1)
-        long long c = (long long)((unsigned long long)last * ctas(total) / (unsigned long long)total);
-        while (share_of(total, (unsigned)c + 1) <= last) c++;
-        while (share_of(total, (unsigned)c) > last) c--;
-        return (int)c - (int)blockIdx.x;
+        // the worker whose share holds it: share_of(c) <= last < share_of(c + 1)
+        long long c = (long long)((double)last * workers() / (double)total);
+        while (share_of((unsigned)c + 1) <= last) c++;
+        while (share_of((unsigned)c) > last) c--;
+        return (int)c / per_cta - (int)blockIdx.x;
     }
     __device__ __forceinline__ bool next(const AttnArgs& a)
     {
@@ -258,13 +275,14 @@ template <> __device__ __forceinline__ bool finite16<__nv_bfloat16>(uint32_t v) 
 template <> __device__ __forceinline__ bool finite16<__half>(uint32_t v) { return (v & 0x7c00u) != 0x7c00u && (v & 0x7c000000u) != 0x7c000000u; }
 
 // Infinities and NaNs among the values of new tokens are taken out before the product, where a weight of 0 would spread them to rows that do not
-// see them; this puts them where they belong.  Rare: a unit whose tiles had any comes here.  Returns what is to be added to value d of a row.
+// see them; this says what value d of a row becomes by those that it does see (0: nothing), cells [cell0, cell1).  Units that had any come here, once their
+// values are written.
 template <class T>
-__device__ __forceinline__ float unseen_spoils(const AttnArgs& a, const Seq& s, int b, int head, int t, int row, int d, int cell0, int cell1)
+__device__ __forceinline__ float spoilt_value(const AttnArgs& a, const Seq& s, int b, int head, int t, int d, int cell0, int cell1)
 {
     float sum = 0.0f;
     for (int cell = max(cell0, s.ctx); cell < min(cell1, s.len); cell++) {
-        if (!sees(a, s, t, row, cell)) continue;
+        if (!sees(a, s, t, s.row0 + t, cell)) continue;
         const long long place = cell_place(a, b, cell);
         if (place < 0) continue;
         const float v = (float)static_cast<const T*>(a.v)[place + head * a.head_stride + d];

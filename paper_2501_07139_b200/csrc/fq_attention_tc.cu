@@ -39,7 +39,7 @@ struct TcShape {
     // full[slots] empty[slots] raw[slots] q_full q_empty s_full[2] p_full[2] pv_done[2] unit_begun
     static constexpr int kBars = 3 * kSlots + 9;
     static constexpr int oSums = oBars + kBars * 8;
-    static constexpr int oMisc = oSums + (kWarps + 4) * 8;                   // TMEM address, abort flag, spoilt[8]
+    static constexpr int oMisc = oSums + (kWarps + 3) * 8;                   // TMEM address, abort flag, spoilt[8]
     static constexpr int kTotal = oMisc + 48 + 1024;                         // (tiles start at a multiple of 1024)
     static constexpr int kTmemS = 0;                                         // two tiles of scores, then NQ of values
     static constexpr int kTmemO = 2 * kKeys;
@@ -398,14 +398,6 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     for (int j = 0; j < 32; j++) v[j] = 0.0f;
                 }
                 if (!real) continue;
-                if (odd) {
-#pragma unroll 1
-                    for (int j = 0; j < 32 && c + j < a.head_dim; j++) {
-                        const float more_of = unseen_spoils<T>(a, w.s, w.b, w.head, t, row, c + j, t0 * S::kKeys, w.t1() * S::kKeys);
-#pragma unroll
-                        for (int i = 0; i < 32; i++) v[i] += i == j ? more_of : 0.0f;
-                    }
-                }
                 if (whole) {
 #pragma unroll
                     for (int j = 0; j < 32; j += 8)
@@ -418,6 +410,15 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                         *reinterpret_cast<float4*>(part + ((c + j) / 4 * S::kRows + q * 128 + r) * 4) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
                 }
             }
+            if (odd && real) {
+#pragma unroll 1
+                for (int d = 0; d < a.head_dim; d++) {
+                    const float x = spoilt_value<T>(a, w.s, w.b, w.head, t, d, t0 * S::kKeys, w.t1() * S::kKeys);
+                    if (x == 0.0f) continue;
+                    if (whole) out[d] = (T)x;
+                    else part[(d / 4 * S::kRows + q * 128 + r) * 4 + d % 4] = x;
+                }
+            }
             const float top = m * a.scale;       // (-inf stays)
             if (!whole) {
                 part[S::kRows * DP + q * 128 + r] = top;
@@ -426,7 +427,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 a.lse[(long long)row * (a.kv_heads * a.share) + h] = l == 0.0f ? -INFINITY : (top + log2f(l)) * 0.69314718055994531f;
             }
             if (tid == 0 && !whole && t0 == 0)
-                a.joins[blockIdx.x] = AttnJoin{w.b, w.tile * S::kRows, w.head, w.others(), min(rows - w.tile * S::kRows, S::kRows), {0, 0, 0}};
+                a.joins[blockIdx.x] = AttnJoin{w.s.row0, w.tile * S::kRows, w.head, w.others(), min(rows - w.tile * S::kRows, S::kRows), (int)blockIdx.x * 2 + 1, {0, 0}};
             if (w.t1() > t0) unit++;
             // nobody is two units ahead of another (the flags of units that hold infinities have eight places)
             tc_before();
