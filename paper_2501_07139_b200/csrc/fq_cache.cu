@@ -2,7 +2,9 @@
 // drafted tree, the bits of what it sees; and the accepted branch of a tree is moved together.
 //
 // fq_cache_step is a chain of short phases that depend on one another through exclusive sums over the sequences, so its time is latency.  One cluster does
-// it: every CTA forms the sums for itself, each phase's writes are dealt to all of them, and a cluster barrier stands between phases.
+// it: every CTA forms the sums for itself, each phase's writes are dealt to all of them, and a cluster barrier stands between phases.  The rows of
+// a large batch, which depend on nothing but the new tables, are a kernel of their own over all SMs (150 thousand rows, 300 sequences: 41 us by the
+// cluster).
 #include <atomic>
 
 #include "fq_cluster.cuh"
@@ -34,6 +36,7 @@ struct StepArgs {
     uint64_t* mask;
     int words;
     int n_cta;
+    int rows_here;                               // the cluster writes the rows too
     int* status;
 };
 
@@ -74,6 +77,46 @@ __device__ __forceinline__ void phase_end(int n_cta)
     }
 }
 
+// Row t of the batch: slot, position, and in a drafted tree what it sees.  starts[n_seqs]: first rows of the sequences;  rows: of all new tokens.
+__device__ __forceinline__ void token_row(const StepArgs& a, const int* starts, int t, int rows)
+{
+    uint64_t* bits = a.parents ? a.mask + (long long)t * a.words : nullptr;
+    if (t >= rows) {
+        a.slots[t] = -1;
+        a.positions[t] = 0;
+        if (bits)
+            for (int w = 0; w < a.words; w++) bits[w] = 0;
+        return;
+    }
+    int lo = 0, hi = a.n_seqs - 1;               // the last sequence that starts at or before this row
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (starts[mid] <= t) lo = mid;
+        else hi = mid - 1;
+    }
+    const int keep = a.keep[lo], i = t - starts[lo], cell = keep + i, block = cell / a.block_size;
+    a.slots[t] = (long long)__ldcg(a.table + lo * a.ld + block) * a.block_size + (cell - block * a.block_size);
+    if (!bits) {
+        a.positions[t] = cell;
+        return;
+    }
+    // up the branch: token numbers fall, so the words are finished one after the other
+    const int* parents = a.parents + starts[lo];
+    int at = i, above = 0, word = a.words - 1;
+    uint64_t w = 0;
+    for (;;) {
+        for (; word > at / 64; word--, w = 0) bits[word] = w;
+        w |= 1ull << (at & 63);
+        const int p = parents[at];
+        if (p >= at || p < -1) atomicCAS(a.status, 0, FQ_ERR_INDEX);
+        if (p >= at || p < 0) break;
+        at = p;
+        above++;
+    }
+    for (; word >= 0; word--, w = 0) bits[word] = w;
+    a.positions[t] = keep + above;
+}
+
 __global__ void __launch_bounds__(kThreads) cache_step_kernel(const StepArgs a)
 {
     extern __shared__ int sums[];                // [3][n_seqs]: returned blocks, taken blocks, rows of the sequences before
@@ -82,6 +125,7 @@ __global__ void __launch_bounds__(kThreads) cache_step_kernel(const StepArgs a)
     int* s_rows = sums + 2 * a.n_seqs;
     __shared__ Three warp_sums[kWarps];
     __shared__ int bad;                          // the call is refused, and why
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");              // (the rows' kernel waits for this one's end)
     const int tid = threadIdx.x, cta = a.n_cta > 1 ? (int)cluster_rank() : 0;
     const int worker = cta * kThreads + tid, workers = a.n_cta * kThreads;
     if (tid == 0) bad = 0;
@@ -121,11 +165,8 @@ __global__ void __launch_bounds__(kThreads) cache_step_kernel(const StepArgs a)
     if (bad) {
         if (worker == 0) atomicCAS(a.status, 0, bad);
         for (int b = worker; b <= a.n_seqs; b += workers) a.starts[b] = 0;
-        for (int t = worker; t < a.tokens; t += workers) {
-            a.slots[t] = -1;
-            a.positions[t] = 0;
-            for (int w = 0; w < (a.parents ? a.words : 0); w++) a.mask[(long long)t * a.words + w] = 0;
-        }
+        if (a.rows_here)
+            for (int t = worker; t < a.tokens; t += workers) token_row(a, s_rows, t, 0);
         return;
     }
     const int lane = tid & 31, warps = workers / 32;
@@ -153,44 +194,20 @@ __global__ void __launch_bounds__(kThreads) cache_step_kernel(const StepArgs a)
         a.starts[a.n_seqs] = (int)rows;
         *a.free_count = end - (int)take;
     }
+    if (!a.rows_here) return;
     phase_end(a.n_cta);
-    for (int t = worker; t < a.tokens; t += workers) {
-        uint64_t* bits = a.parents ? a.mask + (long long)t * a.words : nullptr;
-        if (t >= rows) {
-            a.slots[t] = -1;
-            a.positions[t] = 0;
-            if (bits)
-                for (int w = 0; w < a.words; w++) bits[w] = 0;
-            continue;
-        }
-        int lo = 0, hi = a.n_seqs - 1;           // the last sequence that starts at or before this row
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) / 2;
-            if (s_rows[mid] <= t) lo = mid;
-            else hi = mid - 1;
-        }
-        const int keep = a.keep[lo], i = t - s_rows[lo], cell = keep + i, block = cell / a.block_size;
-        a.slots[t] = (long long)__ldcg(a.table + lo * a.ld + block) * a.block_size + (cell - block * a.block_size);
-        if (!bits) {
-            a.positions[t] = cell;
-            continue;
-        }
-        // up the branch: token numbers fall, so the words are finished one after the other
-        const int* parents = a.parents + s_rows[lo];
-        int at = i, above = 0, word = a.words - 1;
-        uint64_t w = 0;
-        for (;;) {
-            for (; word > at / 64; word--, w = 0) bits[word] = w;
-            w |= 1ull << (at & 63);
-            const int p = parents[at];
-            if (p >= at || p < -1) atomicCAS(a.status, 0, FQ_ERR_INDEX);
-            if (p >= at || p < 0) break;
-            at = p;
-            above++;
-        }
-        for (; word >= 0; word--, w = 0) bits[word] = w;
-        a.positions[t] = keep + above;
-    }
+    for (int t = worker; t < a.tokens; t += workers) token_row(a, s_rows, t, (int)rows);
+}
+
+// The rows of a large batch, by all SMs, from what the kernel before left.
+__global__ void __launch_bounds__(kThreads) cache_rows_kernel(const StepArgs a)
+{
+    extern __shared__ int starts[];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int b = threadIdx.x; b < a.n_seqs; b += kThreads) starts[b] = a.starts[b];
+    const int rows = a.starts[a.n_seqs];
+    __syncthreads();
+    for (int t = blockIdx.x * kThreads + threadIdx.x; t < a.tokens; t += gridDim.x * kThreads) token_row(a, starts, t, rows);
 }
 
 // ------------------------------------------------------------------------------------------------ the accepted branch
@@ -218,7 +235,8 @@ struct MoveArgs {
 };
 
 // A thread owns one piece of a cell in one cache and moves it for token after token: cell before + i only ever takes from cells at or behind it, so what a
-// thread has yet to read is never what it has written.  Eight loads at a time.
+// thread has yet to read is never what it has written.  Eight loads at a time.  90 sequences, 64 caches, 8 heads of 128, 105 MB moved: 46 us (HBM floor 33; several
+// pieces a thread, so that a CTA looks its cells up once for them: 51).
 __global__ void __launch_bounds__(kMoveThreads) cache_move_kernel(const __grid_constant__ MoveArgs a)
 {
     __shared__ long long from[kMaxKept], to[kMaxKept];
@@ -256,9 +274,9 @@ __global__ void __launch_bounds__(kMoveThreads) cache_move_kernel(const __grid_c
     if (bad && tid == 0) atomicCAS(a.status, 0, FQ_ERR_INDEX);
     if (tid == 0 && a.keep && blockIdx.x == 0) a.keep[b] = before + (bad ? 0 : n);
     if (bad) return;
-    const long long p = (long long)blockIdx.x * kMoveThreads + tid;
-    if (p >= (long long)a.n_caches * a.pieces) return;
-    const int c = (int)(p / a.pieces), piece = (int)(p - (long long)c * a.pieces), head = piece / a.per_head;
+    const int p = blockIdx.x * kMoveThreads + tid;
+    if (p >= a.n_caches * a.pieces) return;
+    const int c = p / a.pieces, piece = p - c * a.pieces, head = piece / a.per_head;
     char* base = static_cast<char*>(a.cache[c]) + head * a.head_bytes + (piece - head * a.per_head) * 16;
     for (int i0 = 0; i0 < n; i0 += 8) {
         uint4 v[8];
@@ -303,12 +321,13 @@ int fq_cache_step(fq_ctx* ctx, int n_seqs, int* lens_dev, const int* keep_dev, c
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
     StepArgs a{n_seqs, max_blocks, block_size, lens_dev, keep_dev, new_dev, table_dev, ld, free_dev, free_room, free_count_dev, parents_dev, tokens,
-               starts_dev, slots_dev, positions_dev, mask_dev, words, 1, ctx->status_dev};
+               starts_dev, slots_dev, positions_dev, mask_dev, words, 1, tokens <= 4096, ctx->status_dev};
     if (n_seqs > 64 || tokens > 512) a.n_cta = kMaxCluster;
     const size_t smem = 3 * sizeof(int) * (size_t)n_seqs;
     if (smem > 48 * 1024) {
         // (a setting of the kernel on this device; asking for it again costs a microsecond, and only very large batches do)
-        if (cudaFuncSetAttribute(cache_step_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * (int)sizeof(int) * FQ_MAX_SEQS) != cudaSuccess)
+        if (cudaFuncSetAttribute(cache_step_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * (int)sizeof(int) * FQ_MAX_SEQS) != cudaSuccess ||
+            cudaFuncSetAttribute(cache_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(int) * FQ_MAX_SEQS) != cudaSuccess)
             return FQ_ERR_CUDA;
     }
     cudaLaunchAttribute attr{};
@@ -317,7 +336,15 @@ int fq_cache_step(fq_ctx* ctx, int n_seqs, int* lens_dev, const int* keep_dev, c
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)a.n_cta); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = (cudaStream_t)stream;
     if (a.n_cta > 1) { cfg.attrs = &attr; cfg.numAttrs = 1; }
-    return cudaLaunchKernelEx(&cfg, cache_step_kernel, a) == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, cache_step_kernel, a) != cudaSuccess) return FQ_ERR_CUDA;
+    if (a.rows_here) return FQ_OK;
+    const int ctas = (tokens + kThreads - 1) / kThreads, most = 4 * ctx->sm_count;
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)(ctas < most ? ctas : most)); cfg.dynamicSmemBytes = sizeof(int) * (size_t)n_seqs;
+    cfg.attrs = &early; cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, cache_rows_kernel, a) == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
 }
 
 int fq_cache_move(fq_ctx* ctx, void* const* caches_host, int n_caches, const fq_cache* layout, int dtype, int head_dim, int n_seqs, const int* table_dev,
@@ -351,8 +378,8 @@ int fq_cache_move(fq_ctx* ctx, void* const* caches_host, int n_caches, const fq_
         a.n_caches = n_caches - c0 < kMoveCaches ? n_caches - c0 : kMoveCaches;
         for (int i = 0; i < a.n_caches; i++) a.cache[i] = caches_host[c0 + i];
         a.keep = c0 == 0 ? keep_dev : nullptr;
-        const long long threads = (long long)a.n_caches * a.pieces;
-        const dim3 grid((unsigned)((threads + kMoveThreads - 1) / kMoveThreads), (unsigned)n_seqs);
+        // (at most 128 caches x 1024 heads x 256 pieces)
+        const dim3 grid((unsigned)((a.n_caches * a.pieces + kMoveThreads - 1) / kMoveThreads), (unsigned)n_seqs);
         cache_move_kernel<<<grid, kMoveThreads, 0, (cudaStream_t)stream>>>(a);
         if (cudaGetLastError() != cudaSuccess) return FQ_ERR_CUDA;
     }

@@ -43,37 +43,33 @@ struct RotaryArgs {
     int* status;
 };
 
-// N values of a row in registers, as fp32.
+// N values of a row in registers, as they lie in memory: one access.
 template <class T, int N>
 struct Piece {
     static constexpr int kBytes = N * (int)sizeof(T);
     static_assert(kBytes == 16 || kBytes == 8 || N == 1, "one access");
-    float v[N];
+    alignas(16) T raw[N];
     __device__ __forceinline__ void load(const T* p)
     {
-        alignas(16) T raw[N];
         if constexpr (kBytes == 16) *reinterpret_cast<uint4*>(raw) = *reinterpret_cast<const uint4*>(p);
         else if constexpr (kBytes == 8) *reinterpret_cast<uint2*>(raw) = *reinterpret_cast<const uint2*>(p);
         else raw[0] = p[0];
-#pragma unroll
-        for (int i = 0; i < N; i++) v[i] = Group<T>::to_f(raw[i]);
     }
     __device__ __forceinline__ void store(T* p) const
     {
-        alignas(16) T raw[N];
-#pragma unroll
-        for (int i = 0; i < N; i++) raw[i] = Group<T>::from_f(v[i]);
         if constexpr (kBytes == 16) *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(raw);
         else if constexpr (kBytes == 8) *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(raw);
         else p[0] = raw[0];
     }
+    __device__ __forceinline__ float at(int i) const { return Group<T>::to_f(raw[i]); }
+    __device__ __forceinline__ void set(int i, float v) { raw[i] = Group<T>::from_f(v); }
 };
 
 // A CTA has up to U items a thread of one token.  Its loads go out before the angles are formed.
 //   N : values of a piece.  A turned item is a piece of the lower and one of the upper half, or with INTERLEAVED one piece of pairs (two single values
 //       where N is 1)
 template <class T, int N, bool INTERLEAVED, int U>
-__global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant__ RotaryArgs a)
+__global__ void __launch_bounds__(kThreads, 4) rotary_kernel(const __grid_constant__ RotaryArgs a)
 {
     __shared__ float2 angle[kMaxRot / 2];        // (cos, sin) * magnitude
     __shared__ long long place;                  // offset of the token's cell in the cache, or -1
@@ -138,18 +134,18 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant_
 #pragma unroll
             for (int i = 0; i < N; i += 2) {
                 const float2 w = angle[pair[u] + i / 2];
-                const float x0 = lo[u].v[i], x1 = lo[u].v[i + 1];
-                lo[u].v[i] = fmaf(x0, w.x, -(x1 * w.y));         // (written out: the same roundings in every variant)
-                lo[u].v[i + 1] = fmaf(x0, w.y, x1 * w.x);
+                const float x0 = lo[u].at(i), x1 = lo[u].at(i + 1);
+                lo[u].set(i, fmaf(x0, w.x, -(x1 * w.y)));        // (written out: the same roundings in every variant)
+                lo[u].set(i + 1, fmaf(x0, w.y, x1 * w.x));
             }
             lo[u].store(y);
         } else {
 #pragma unroll
             for (int i = 0; i < N; i++) {
                 const float2 w = angle[pair[u] + i];
-                const float x0 = lo[u].v[i], x1 = hi[u].v[i];
-                lo[u].v[i] = fmaf(x0, w.x, -(x1 * w.y));
-                hi[u].v[i] = fmaf(x0, w.y, x1 * w.x);
+                const float x0 = lo[u].at(i), x1 = hi[u].at(i);
+                lo[u].set(i, fmaf(x0, w.x, -(x1 * w.y)));
+                hi[u].set(i, fmaf(x0, w.y, x1 * w.x));
             }
             lo[u].store(y);
             hi[u].store(y + (apart[u] & 0xffff));
@@ -170,7 +166,7 @@ int launch_pieces(RotaryArgs& a, int tokens, int rot, int sm_count, cudaStream_t
     }
     // Few tokens: a piece a thread over as many CTAs as that takes; else up to four, so that a token's angles are formed by fewer.
     const int one = (a.items + kThreads - 1) / kThreads;
-    const bool few = (long long)tokens * one <= 4ll * sm_count;
+    const bool few = (long long)tokens * one <= 32ll * sm_count;
     const int u = few ? 1 : one >= 4 ? 4 : one >= 2 ? 2 : 1;
     const int ctas = (one + u - 1) / u;
     a.per_cta = (a.items + ctas - 1) / ctas;

@@ -7,6 +7,8 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
+from operator import attrgetter
 from typing import List, Optional, Sequence
 
 import torch
@@ -20,6 +22,7 @@ FQ_DT_F32 = 2
 FQ_MAX_TOP = 128
 FQ_MAX_VOCAB = 393216
 _I8, _F32, _I32, _I64, _IDS = (torch.int8,), (torch.float32,), (torch.int32,), (torch.int64,), (torch.int32, torch.int64)
+_dtype_of = attrgetter("dtype")
 _HALF = (torch.float16, torch.bfloat16)
 _TYPES = {torch.float16: FQ_DT_F16, torch.bfloat16: FQ_DT_BF16, torch.float32: FQ_DT_F32}
 
@@ -127,7 +130,7 @@ def lib():
     L.fq_token_logprobs.argtypes = [vp, vp, i, i, i, ll, vp, i, fl, vp, vp, i, vp, vp, vp]
     L.fq_distill_topk.argtypes = [vp, vp, i, i, i, ll, vp, i, vp, i, fl, vp, vp, vp, vp, ll, vp]
     L.fq_distill_topk_grad.argtypes = [vp, vp, i, i, i, ll, vp, i, vp, i, fl, vp, vp, vp, ll, vp]
-    hp, cp, db = C.POINTER(Heads), C.POINTER(Cache), C.c_double
+    hp, cp, db = vp, vp, C.c_double
     L.fq_cache_step.argtypes = [vp, i, vp, vp, vp, vp, ll, i, i, vp, i, vp, vp, i, vp, vp, vp, vp, i, vp]
     L.fq_cache_move.argtypes = [vp, vp, i, cp, i, i, i, vp, ll, i, vp, vp, vp, ll, i, vp, vp, vp]
     L.fq_rotary_table.argtypes = [i, db, db, i, db, db, vp]
@@ -563,22 +566,24 @@ class FlexQ:
     # -- between the linear layers of a block -----------------------------------------------------
     def _heads(self, t: torch.Tensor, name: str, types, tokens: Optional[int] = None, dim: Optional[int] = None) -> Heads:
         shape, st = t.shape, t.stride()
-        if len(shape) != 3 or t.dtype not in types or t.get_device() != self._index or (st[2] != 1 and shape[2] > 1):
-            raise ValueError(f"{name}: [tokens][heads][values] of {', '.join(str(d) for d in types)} on {self.device} with dense values are needed, not "
-                             f"{t.dtype} {tuple(shape)} with strides {st} on {t.device}")
-        if (tokens is not None and shape[0] != tokens) or (dim is not None and shape[2] != dim):
-            raise ValueError(f"{name}: {tokens} tokens with heads of {dim} are needed, not {shape[0]} with heads of {shape[2]}")
-        return Heads(t.data_ptr(), st[0], st[1], shape[1])
+        if len(shape) == 3:
+            n, heads, d = shape
+            if t.dtype in types and t.get_device() == self._index and (st[2] == 1 or d < 2) and (tokens is None or (n == tokens and d == dim)):
+                return Heads(t.data_ptr(), st[0], st[1], heads)
+        wanted = "[tokens][heads][values]" if tokens is None else f"[{tokens}][heads][{dim}]"
+        raise ValueError(f"{name}: {wanted} of {', '.join(str(d) for d in types)} on {self.device} with dense values are needed, not "
+                         f"{t.dtype} {tuple(shape)} with strides {st} on {t.device}")
 
     def _cache(self, k: torch.Tensor, v: torch.Tensor, types, dim: Optional[int] = None) -> Cache:
-        shape, st = k.shape, k.stride()
-        if len(shape) != 4 or k.dtype not in types or k.get_device() != self._index or (st[3] != 1 and shape[3] > 1) or v.shape != shape or \
-                v.stride() != st or v.dtype != k.dtype or v.get_device() != self._index:
-            raise ValueError(f"caches: two of [blocks][block size][heads][values], {', '.join(str(d) for d in types)} on {self.device} with dense values and the "
-                             f"same strides are needed, not {k.dtype} {tuple(shape)} {st} on {k.device} and {v.dtype} {tuple(v.shape)} {v.stride()} on {v.device}")
-        if dim is not None and shape[3] != dim:
-            raise ValueError(f"caches: heads of {dim} are needed, not of {shape[3]}")
-        return Cache(k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], shape[0], shape[1], shape[2])
+        shape, st, dt = k.shape, k.stride(), k.dtype
+        if len(shape) == 4 and dt in types and k.get_device() == self._index and (st[3] == 1 or shape[3] < 2) and (
+                k is v or (v.shape == shape and v.stride() == st and v.dtype is dt and v.get_device() == self._index)):
+            blocks, block, heads, d = shape
+            if dim is not None and d != dim:
+                raise ValueError(f"caches: heads of {dim} are needed, not of {d}")
+            return Cache(k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], blocks, block, heads)
+        raise ValueError(f"caches: two of [blocks][block size][heads][values], {', '.join(str(d) for d in types)} on {self.device} with dense values and the "
+                         f"same strides are needed, not {dt} {tuple(shape)} {st} on {k.device} and {v.dtype} {tuple(v.shape)} {v.stride()} on {v.device}")
 
     def _table(self, table: torch.Tensor, n_seqs: int):
         rows, cols, ld = self._matrix(table, "table", _I32)
@@ -623,11 +628,13 @@ class FlexQ:
         caches = list(caches)
         if not caches:
             raise ValueError("caches: none given")
-        layout = self._cache(caches[0], caches[0], _TYPES)
+        layout, count = self._cache(caches[0], caches[0], _TYPES), len(caches)
         shape, st, dt = caches[0].shape, caches[0].stride(), caches[0].dtype
-        for t in caches:
-            if t.shape != shape or t.stride() != st or t.dtype != dt or t.get_device() != self._index:
-                raise ValueError(f"caches: {dt} {tuple(shape)} with strides {st} on {self.device} for all, not {t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}")
+        # (a tensor's properties for all of them at once: there are two caches a layer)
+        if list(map(torch.Tensor.size, caches)).count(shape) != count or list(map(torch.Tensor.stride, caches)).count(st) != count or \
+                list(map(_dtype_of, caches)).count(dt) != count or list(map(torch.Tensor.get_device, caches)).count(self._index) != count:
+            raise ValueError(f"caches: {dt} {tuple(shape)} with strides {st} on {self.device} are needed for all")
+        pointers = array("Q", map(torch.Tensor.data_ptr, caches))
         n = lens.shape[0] if lens.dim() == 1 else 0
         self._dense(lens, "lens", _I32, (n,))
         self._dense(n_kept, "n_kept", _I32, (n,))
@@ -637,7 +644,7 @@ class FlexQ:
         if rows != n:
             raise ValueError(f"kept: a row for each of {n} sequences is needed, not {rows}")
         keep = torch.empty(n, dtype=torch.int32, device=self.device)
-        _check(lib().fq_cache_move(self._h, (C.c_void_p * len(caches))(*[t.data_ptr() for t in caches]), len(caches), C.byref(layout), _TYPES[dt], shape[3], n,
+        _check(lib().fq_cache_move(self._h, pointers.buffer_info()[0], count, C.byref(layout), _TYPES[dt], shape[3], n,
                                    table.data_ptr(), ld, blocks, starts.data_ptr(), lens.data_ptr(), kept.data_ptr(), max(ld_kept, most), most,
                                    n_kept.data_ptr(), keep.data_ptr(), _stream_on(self.device)), "fq_cache_move")
         return keep
