@@ -65,51 +65,47 @@ struct Piece {
     __device__ __forceinline__ void set(int i, float v) { raw[i] = Group<T>::from_f(v); }
 };
 
-// A CTA has up to U items a thread of one token.  Its loads go out before the angles are formed.
+// A CTA has an item a thread of one token: with several (fewer CTAs form a token's angles then) 777 tokens of 64 heads took 10.5 us instead of 8.5, and
+// 8192 of 80 as long.  The loads go out before the angles are formed.  8192 tokens, 80 heads of 128 in fp32, 671 MB: 123 us (HBM floor 104).
 //   N : values of a piece.  A turned item is a piece of the lower and one of the upper half, or with INTERLEAVED one piece of pairs (two single values
 //       where N is 1)
-template <class T, int N, bool INTERLEAVED, int U>
+template <class T, int N, bool INTERLEAVED>
 __global__ void __launch_bounds__(kThreads, 4) rotary_kernel(const __grid_constant__ RotaryArgs a)
 {
     __shared__ float2 angle[kMaxRot / 2];        // (cos, sin) * magnitude
     __shared__ long long place;                  // offset of the token's cell in the cache, or -1
-    const int token = blockIdx.x, first = blockIdx.y * a.per_cta, end = min(a.items, first + a.per_cta);
+    const int token = blockIdx.x;
     constexpr int kStep = INTERLEAVED && N == 1 ? 2 : N;        // values of a row that a turned item's first piece stands for
-    Piece<T, N> lo[U], hi[U];
-    T* out[U];
-    int pair[U], apart[U];                       // first pair (-1: copied), distance of the second piece
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-        int i = first + u * kThreads + (int)threadIdx.x;
-        out[u] = nullptr;
-        if (i >= end) continue;
+    constexpr bool kTwo = !(INTERLEAVED && N > 1);
+    Piece<T, N> lo, hi;
+    T* out = nullptr;
+    int pair = -1, apart = 0;                    // first pair (-1: copied), distance of the second piece
+    bool stored = false;                         // goes to the cache
+    int i = blockIdx.y * kThreads + (int)threadIdx.x;
+    if (i < a.items) {
         int which = 0;
         while (i >= a.t[which].heads * a.t[which].pieces) i -= a.t[which].heads * a.t[which].pieces, which++;
         const Tensor& t = a.t[which];
         const int head = i / t.pieces, piece = i - head * t.pieces;
         const int turned = INTERLEAVED ? t.rot / kStep : t.rot / 2 / N;
-        int at;
+        int at = t.rot + (piece - turned) * N;
         if (piece < turned) {
             at = piece * kStep;
-            pair[u] = INTERLEAVED ? at / 2 : at;
-            apart[u] = INTERLEAVED ? 1 : t.rot / 2;
-        } else {
-            at = t.rot + (piece - turned) * N;
-            pair[u] = -1;
-            apart[u] = 0;
+            pair = INTERLEAVED ? at / 2 : at;
+            apart = INTERLEAVED ? 1 : t.rot / 2;
         }
         const T* src = static_cast<const T*>(t.src) + token * t.src_token + head * t.src_head + at;
-        out[u] = (t.dst ? static_cast<T*>(t.dst) + token * t.dst_token : static_cast<T*>(a.cache[which == 2])) + head * t.dst_head + at;
-        if (!t.dst) apart[u] |= 1 << 30;         // goes to the cache
-        lo[u].load(src);
-        if (pair[u] >= 0 && !(INTERLEAVED && N > 1)) hi[u].load(src + (apart[u] & 0xffff));
+        stored = !t.dst;
+        out = (stored ? static_cast<T*>(a.cache[which == 2]) : static_cast<T*>(t.dst) + token * t.dst_token) + head * t.dst_head + at;
+        lo.load(src);
+        if (kTwo && pair >= 0) hi.load(src + apart);
     }
     const long long position = a.wide_positions ? static_cast<const long long*>(a.positions)[token] : static_cast<const int*>(a.positions)[token];
-    for (int i = threadIdx.x; i < a.half; i += kThreads) {
-        const uint64_t turn = (uint64_t)position * a.turns[i];
+    for (int p = threadIdx.x; p < a.half; p += kThreads) {
+        const uint64_t turn = (uint64_t)position * a.turns[p];
         float s, c;
         sincospif((float)(int)(turn >> 32) * 0x1p-31f, &s, &c);
-        angle[i] = make_float2(c * a.magnitude, s * a.magnitude * a.side);
+        angle[p] = make_float2(c * a.magnitude, s * a.magnitude * a.side);
     }
     if (threadIdx.x == 0 && a.slots) {
         const long long slot = a.slots[token];
@@ -118,43 +114,36 @@ __global__ void __launch_bounds__(kThreads, 4) rotary_kernel(const __grid_consta
         else if (slot >= 0) place = slot / a.block_size * a.block_stride + slot % a.block_size * a.token_stride;
     }
     __syncthreads();
+    if (!out || (stored && place < 0)) return;
+    T* y = stored ? out + place : out;
+    if (pair < 0) {
+        lo.store(y);
+        return;
+    }
+    if constexpr (!kTwo) {
 #pragma unroll
-    for (int u = 0; u < U; u++) {
-        if (!out[u]) continue;
-        T* y = out[u];
-        if (apart[u] >> 30) {
-            if (place < 0) continue;
-            y += place;
+        for (int e = 0; e < N; e += 2) {
+            const float2 w = angle[pair + e / 2];
+            const float x0 = lo.at(e), x1 = lo.at(e + 1);
+            lo.set(e, fmaf(x0, w.x, -(x1 * w.y)));               // (written out: the same roundings in every variant)
+            lo.set(e + 1, fmaf(x0, w.y, x1 * w.x));
         }
-        if (pair[u] < 0) {
-            lo[u].store(y);
-            continue;
-        }
-        if constexpr (INTERLEAVED && N > 1) {
+        lo.store(y);
+    } else {
 #pragma unroll
-            for (int i = 0; i < N; i += 2) {
-                const float2 w = angle[pair[u] + i / 2];
-                const float x0 = lo[u].at(i), x1 = lo[u].at(i + 1);
-                lo[u].set(i, fmaf(x0, w.x, -(x1 * w.y)));        // (written out: the same roundings in every variant)
-                lo[u].set(i + 1, fmaf(x0, w.y, x1 * w.x));
-            }
-            lo[u].store(y);
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; i++) {
-                const float2 w = angle[pair[u] + i];
-                const float x0 = lo[u].at(i), x1 = hi[u].at(i);
-                lo[u].set(i, fmaf(x0, w.x, -(x1 * w.y)));
-                hi[u].set(i, fmaf(x0, w.y, x1 * w.x));
-            }
-            lo[u].store(y);
-            hi[u].store(y + (apart[u] & 0xffff));
+        for (int e = 0; e < N; e++) {
+            const float2 w = angle[pair + e];
+            const float x0 = lo.at(e), x1 = hi.at(e);
+            lo.set(e, fmaf(x0, w.x, -(x1 * w.y)));
+            hi.set(e, fmaf(x0, w.y, x1 * w.x));
         }
+        lo.store(y);
+        hi.store(y + apart);
     }
 }
 
 template <class T, int N, bool INTERLEAVED>
-int launch_pieces(RotaryArgs& a, int tokens, int rot, int sm_count, cudaStream_t st)
+int launch_pieces(RotaryArgs& a, int tokens, cudaStream_t st)
 {
     constexpr int kStep = INTERLEAVED && N == 1 ? 2 : N;
     a.items = 0;
@@ -164,31 +153,22 @@ int launch_pieces(RotaryArgs& a, int tokens, int rot, int sm_count, cudaStream_t
         t.pieces = turned + (t.dst == t.src ? 0 : (a.head_dim - t.rot) / N);
         a.items += t.heads * t.pieces;
     }
-    // Few tokens: a piece a thread over as many CTAs as that takes; else up to four, so that a token's angles are formed by fewer.
-    const int one = (a.items + kThreads - 1) / kThreads;
-    const bool few = (long long)tokens * one <= 32ll * sm_count;
-    const int u = few ? 1 : one >= 4 ? 4 : one >= 2 ? 2 : 1;
-    const int ctas = (one + u - 1) / u;
-    a.per_cta = (a.items + ctas - 1) / ctas;
-    const dim3 grid((unsigned)tokens, (unsigned)ctas);
-    if (u == 1) rotary_kernel<T, N, INTERLEAVED, 1><<<grid, kThreads, 0, st>>>(a);
-    else if (u == 2) rotary_kernel<T, N, INTERLEAVED, 2><<<grid, kThreads, 0, st>>>(a);
-    else rotary_kernel<T, N, INTERLEAVED, 4><<<grid, kThreads, 0, st>>>(a);
+    rotary_kernel<T, N, INTERLEAVED><<<dim3((unsigned)tokens, (unsigned)((a.items + kThreads - 1) / kThreads)), kThreads, 0, st>>>(a);
     return cudaGetLastError() == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
 }
 
 template <class T>
-int launch_typed(RotaryArgs& a, int tokens, int rot, int interleaved, size_t align, int sm_count, cudaStream_t st)
+int launch_typed(RotaryArgs& a, int tokens, int interleaved, size_t align, cudaStream_t st)
 {
     constexpr int kFull = 16 / (int)sizeof(T), kHalf = 8 / (int)sizeof(T);
     if (interleaved) {
-        if (align >= 16) return launch_pieces<T, kFull, true>(a, tokens, rot, sm_count, st);
-        if (align >= 8) return launch_pieces<T, kHalf, true>(a, tokens, rot, sm_count, st);
-        return launch_pieces<T, 1, true>(a, tokens, rot, sm_count, st);
+        if (align >= 16) return launch_pieces<T, kFull, true>(a, tokens, st);
+        if (align >= 8) return launch_pieces<T, kHalf, true>(a, tokens, st);
+        return launch_pieces<T, 1, true>(a, tokens, st);
     }
-    if (align >= 16) return launch_pieces<T, kFull, false>(a, tokens, rot, sm_count, st);
-    if (align >= 8) return launch_pieces<T, kHalf, false>(a, tokens, rot, sm_count, st);
-    return launch_pieces<T, 1, false>(a, tokens, rot, sm_count, st);
+    if (align >= 16) return launch_pieces<T, kFull, false>(a, tokens, st);
+    if (align >= 8) return launch_pieces<T, kHalf, false>(a, tokens, st);
+    return launch_pieces<T, 1, false>(a, tokens, st);
 }
 
 // The largest power of two, up to 16, that divides every address and distance (in bytes).
@@ -215,9 +195,9 @@ int launch_rotary(const fq_ctx* ctx, RotaryArgs& a, int dtype, int tokens, int r
     }                                    // (a cache's cells are 16-byte aligned)
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
-    if (dtype == FQ_DT_F32) return launch_typed<float>(a, tokens, rot, interleaved, c.bytes(), ctx->sm_count, st);
-    if (dtype == FQ_DT_F16) return launch_typed<__half>(a, tokens, rot, interleaved, c.bytes(), ctx->sm_count, st);
-    return launch_typed<__nv_bfloat16>(a, tokens, rot, interleaved, c.bytes(), ctx->sm_count, st);
+    if (dtype == FQ_DT_F32) return launch_typed<float>(a, tokens, interleaved, c.bytes(), st);
+    if (dtype == FQ_DT_F16) return launch_typed<__half>(a, tokens, interleaved, c.bytes(), st);
+    return launch_typed<__nv_bfloat16>(a, tokens, interleaved, c.bytes(), st);
 }
 
 int check_rotary(const fq_ctx* ctx, int dtype, int tokens, int head_dim, int rot_dim, const void* positions, int id_bytes, const uint64_t* turns,
