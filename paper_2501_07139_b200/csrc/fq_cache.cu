@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(kThreads) cache_step_kernel(const StepArgs a)
     int* s_rows = sums + 2 * a.n_seqs;
     __shared__ Three warp_sums[kWarps];
     __shared__ int bad;                          // the call is refused, and why
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");              // (the rows' kernel waits for this one's end)
+    if (!a.rows_here) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");        // (the rows' kernel waits for this one's end)
     const int tid = threadIdx.x, cta = a.n_cta > 1 ? (int)cluster_rank() : 0;
     const int worker = cta * kThreads + tid, workers = a.n_cta * kThreads;
     if (tid == 0) bad = 0;
