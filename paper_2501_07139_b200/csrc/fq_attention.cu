@@ -1,4 +1,5 @@
-// Attention of a sequence's last tokens over its paged cache, up to 16 query rows a tile (single tokens, small trees): bound by reading keys and values.
+// Attention of a sequence's last tokens over its paged cache, up to 16 query rows to a key head (single tokens, small trees) and heads of up to 128: bound by
+// reading keys and values.
 //
 // Every warp is a worker: it has a share of the batch's work of its own, which it fetches by its own asynchronous copies, 16 cells at a time, into its own
 // ring (192 KB an SM, of which two thirds are on their way), so that nobody waits for another before the end of the kernel; there the warps join
@@ -18,9 +19,10 @@ namespace {
 constexpr int kRows = 16;
 constexpr int kChunk = 16;                       // cells of a warp's share of a key tile
 
+constexpr int kWorkers = 8;                      // warps of a CTA
 template <int DP>
-struct Shape {                                   // DP: head_dim, rounded up to 64, 128 or 256
-    static constexpr int kWarps = DP == 256 ? 4 : 8;
+struct Shape {                                   // DP: head_dim, rounded up to 64 or 128
+    static constexpr int kWarps = kWorkers;
     static constexpr int kThreads = kWarps * 32;
     static constexpr int kStageBytes = 2 * kChunk * DP * 2;                  // of a warp: keys, then values
     static constexpr int kStages = 196608 / (kWarps * kStageBytes);
@@ -424,17 +426,19 @@ int launch_attention(const fq_ctx* ctx, const AttnArgs& a, cudaStream_t st)
 
 int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
-// Query rows of a unit.  Up to 16 rows to a key head go to the kernel of this file, whose work grows with every 16 rows; more to the tensor cores',
-// whose does with every 128, two tiles of them side by side where there are as many.
+// Query rows of a unit, by how many a key head has.  (Measured, us; "warps" is this file's kernel.)
+//   Up to 16, heads of up to 128: warps.  48 sequences of 4096, 40 heads, 1 row: 316, tensor cores 371; 64 of 1000, 8 heads, 8 rows: 37 and 56, 16 rows 47 and 56; one
+//   of 4000, 32 heads, 1 row: 20.5 and 26.7.  Larger heads: tensor cores (16 sequences of 4000, 8 heads of 256, 1 row: 77, warps 82; 8 rows of 32 x 2000: 74 and 94).
+//   Up to 384: one tile of 128 query rows at a time.  16 sequences of 16000, 8 heads, 32 rows: 106, warps 144; 5 of 40000, 240 rows: 144, two tiles 145;
+//   300 rows of 2 x 8000 cells, 32 heads: 101 and 116.  More: two tiles side by side, which read keys once.  480 rows of 5 x 40000: 227, one tile 245; 8000 of
+//   one prompt: 617 and 704.
 int unit_rows(int new_tokens, int share, int dp)
 {
     const long long rows = (long long)new_tokens * share;
-    return rows <= kRows ? kRows : rows <= 128 || dp == 256 ? 128 : 256;
+    if (dp == 256) return 128;
+    return rows <= kRows ? kRows : rows <= 384 ? 128 : 256;
 }
-
-// Workers of a CTA: warps of this file's kernel, the CTA of the other.
-int workers_of(int rows, int dp) { return rows > kRows ? 1 : dp == 256 ? Shape<256>::kWarps : Shape<128>::kWarps; }
-static_assert(Shape<64>::kWarps == Shape<128>::kWarps, "workers_of");
+int workers_of(int rows) { return rows > kRows ? 1 : kWorkers; }
 
 template <class T>
 int launch_typed(const fq_ctx* ctx, const AttnArgs& a, int rows, int dp, cudaStream_t st)
@@ -442,8 +446,7 @@ int launch_typed(const fq_ctx* ctx, const AttnArgs& a, int rows, int dp, cudaStr
     int rc;
     if (rows > kRows) rc = launch_attention_tc(ctx, a, std::is_same<T, __half>::value ? FQ_DT_F16 : FQ_DT_BF16, rows, dp, st);
     else if (dp == 64) rc = launch_attention<T, 64>(ctx, a, st);
-    else if (dp == 128) rc = launch_attention<T, 128>(ctx, a, st);
-    else rc = launch_attention<T, 256>(ctx, a, st);
+    else rc = launch_attention<T, 128>(ctx, a, st);
     if (rc != FQ_OK) return rc;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -451,7 +454,7 @@ int launch_typed(const fq_ctx* ctx, const AttnArgs& a, int rows, int dp, cudaStr
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)ctx->sm_count, (unsigned)((rows * dp / 4 + kJoinPieces - 1) / kJoinPieces)); cfg.blockDim = dim3(kJoinThreads);
     cfg.stream = st; cfg.attrs = &attr; cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attention_join_kernel<T>, a, rows, dp, rows > kRows ? 1 : 0, workers_of(rows, dp)) == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, attention_join_kernel<T>, a, rows, dp, rows > kRows ? 1 : 0, workers_of(rows)) == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
 }
 
 bool good_sizes(const fq_ctx* ctx, int n_seqs, int tokens, int q_heads, int cache_heads, int head_dim, int new_tokens)
@@ -473,7 +476,7 @@ size_t fq_tree_attention_scratch(const fq_ctx* ctx, int n_seqs, int tokens, int 
 {
     if (!ctx || !good_sizes(ctx, n_seqs, tokens, q_heads, cache_heads, head_dim, new_tokens)) return 0;
     const int dp = padded_dim(head_dim), rows = unit_rows(new_tokens, q_heads / cache_heads, dp);
-    return join_bytes(ctx) + (size_t)ctx->sm_count * workers_of(rows, dp) * 2 * rows * (dp + 2) * sizeof(float);
+    return join_bytes(ctx) + (size_t)ctx->sm_count * workers_of(rows) * 2 * rows * (dp + 2) * sizeof(float);
 }
 
 int fq_tree_attention(fq_ctx* ctx, const fq_heads* q, const fq_heads* out, const fq_cache* cache, int dtype, int head_dim, int tokens, int n_seqs,

@@ -27,23 +27,23 @@ template <int DP, int NQ>
 struct TcShape {
     static constexpr int kRows = 128 * NQ;
     static constexpr int kKeys = DP == 256 ? 64 : 128;
+    static constexpr int kBufs = NQ == 1 ? 2 : 1;                            // tiles of scores of a query tile: they share 512 columns with the values
     static constexpr int kSoftmax = 4 * NQ;                                  // warps
     static constexpr int kWarps = kSoftmax + 4;
     static constexpr int kThreads = kWarps * 32;
-    static constexpr int kEnds = 5;                                          // key tiles' time that a unit's ends take
+    static constexpr int kEnds = 640 / kKeys;                                // key tiles' time that a unit's ends take
     static constexpr int kQBytes = 128 * DP * 2;                             // of a query tile
     static constexpr int kSlotBytes = kKeys * DP * 2;
-    static constexpr int kSlots = NQ * kQBytes + 6 * kSlotBytes <= 226 * 1024 ? (DP == 64 ? 8 : 6) : 5;
+    static constexpr int kSlots = (224 * 1024 - NQ * kQBytes) / kSlotBytes < 10 ? (224 * 1024 - NQ * kQBytes) / kSlotBytes : 10;
     static constexpr int oRing = NQ * kQBytes;
     static constexpr int oBars = oRing + kSlots * kSlotBytes;
-    // full[slots] empty[slots] raw[slots] q_full q_empty s_full[2] p_full[2] pv_done[2] unit_begun
-    static constexpr int kBars = 3 * kSlots + 9;
+    // full[slots] empty[slots] raw[slots] q_full q_empty s_full[4] p_full[4] pv_done[2] unit_begun
+    static constexpr int kBars = 3 * kSlots + 13;
     static constexpr int oSums = oBars + kBars * 8;
     static constexpr int oMisc = oSums + (kWarps + 3) * 8;                   // TMEM address, abort flag, spoilt[8]
     static constexpr int kTotal = oMisc + 48 + 1024;                         // (tiles start at a multiple of 1024)
-    static constexpr int kTmemS = 0;                                         // two tiles of scores, then NQ of values
-    static constexpr int kTmemO = 2 * kKeys;
-    static_assert(NQ == 1 || kThreads == 384, "the split of registers");
+    static constexpr int kTmemS = 0;                                         // scores of the query tiles, then their values
+    static constexpr int kTmemO = kBufs * NQ * kKeys;
     static_assert(kTmemO + NQ * DP <= 512, "TMEM columns");
     static_assert(kTotal <= 232448, "shared memory over the per-CTA limit");
 };
@@ -231,7 +231,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     const auto full = [&](int slot) { return bars + slot * 8; };
     const auto empty = [&](int slot) { return bars + (S::kSlots + slot) * 8; };
     const auto raw = [&](int slot) { return bars + (2 * S::kSlots + slot) * 8; };
-    const uint32_t q_full = bars + 3 * S::kSlots * 8, q_empty = q_full + 8, s_full = q_full + 16, p_full = q_full + 32, pv_done = q_full + 48, unit_begun = q_full + 64;
+    const uint32_t q_full = bars + 3 * S::kSlots * 8, q_empty = q_full + 8, s_full = q_full + 16, p_full = q_full + 48, pv_done = q_full + 80, unit_begun = q_full + 96;
     uint32_t* tmem_at = reinterpret_cast<uint32_t*>(smem + S::oMisc);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::oMisc + 4);
     volatile int* spoilt = reinterpret_cast<volatile int*>(smem + S::oMisc + 8);
@@ -249,11 +249,11 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
         mbar_init(unit_begun, S::kSoftmax);
-        for (int i = 0; i < 2; i++) {
+        for (int i = 0; i < 4; i++) {
             mbar_init(s_full + 8 * i, 1);
             mbar_init(p_full + 8 * i, 4);
-            mbar_init(pv_done + 8 * i, 1);
         }
+        for (int i = 0; i < 2; i++) mbar_init(pv_done + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == S::kWarps - 1) {
@@ -282,6 +282,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     // With two query tiles a softmax thread holds 128 scores and needs more registers than the 168 that all got; the last four warps give theirs
     // up: 8 x 32 x 208 + 4 x 32 x 88 = 12 x 32 x 168.
     if constexpr (NQ == 2) {
+        static_assert(S::kThreads == 384, "the split of registers");
         if (warp < S::kSoftmax) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     }
@@ -306,7 +307,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             const int all_see = a.mask ? w.s.ctx : w.s.ctx + (w.tile * S::kRows + q * 128) / a.share + 1;
             float m = -INFINITY, l = 0.0f;                                       // m: of the raw scores
             for (int tile = t0; tile < t1; tile++, n_tiles++) {
-                const uint32_t buf = NQ == 1 ? n_tiles & 1 : (uint32_t)q, phase = NQ == 1 ? n_tiles >> 1 & 1 : n_tiles & 1;
+                const uint32_t buf = S::kBufs == 2 ? n_tiles & 1 : (uint32_t)q, phase = (S::kBufs == 2 ? n_tiles >> 1 : n_tiles) & 1;
                 if (!wait(s_full + 8 * buf, phase)) break;
                 tc_after();
                 const uint32_t s_at = lanes + S::kTmemS + buf * S::kKeys;
@@ -577,34 +578,26 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         v_at.next();
         unsigned n_tiles[2] = {0, 0};
         int unit = 0;
+        // (All that follows one wait is issued by one lane in one go: entering and leaving such a stretch takes some 300 cycles, whatever it issues.)
         const auto scores = [&](int q, uint32_t buf) {
             const uint32_t k_tile = ring + k_at.slot * S::kSlotBytes, q_tile = base + q * S::kQBytes;
-            if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < DP / 16; k++) {
-                    const uint32_t in = (k & 3) * 32;                            // bytes within a 128-byte row
-                    mma_ss(tmem + S::kTmemS + buf * S::kKeys, umma_desc_sw128(q_tile + (k >> 2) * (128 * 128) + in),
-                           umma_desc_sw128(k_tile + (k >> 2) * (S::kKeys * 128) + in), id_s, k > 0);
-                }
-                umma_commit(s_full + 8 * buf);
+            for (int k = 0; k < DP / 16; k++) {
+                const uint32_t in = (k & 3) * 32;                                // bytes within a 128-byte row
+                mma_ss(tmem + S::kTmemS + buf * S::kKeys, umma_desc_sw128(q_tile + (k >> 2) * (128 * 128) + in),
+                       umma_desc_sw128(k_tile + (k >> 2) * (S::kKeys * 128) + in), id_s, k > 0);
             }
-            __syncwarp();
+            umma_commit(s_full + 8 * buf);
         };
         const auto values = [&](int q, uint32_t buf, bool accumulate) {
             const uint32_t v_tile = ring + v_at.slot * S::kSlotBytes;
-            if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < S::kKeys / 16; k++)
-                    mma_ts(tmem + S::kTmemO + q * DP, tmem + S::kTmemS + buf * S::kKeys + k * 8, desc_values(v_tile + k * 2048, S::kKeys * 128), id_o,
-                           accumulate || k > 0);
-                umma_commit(pv_done + 8 * q);
-            }
-            __syncwarp();
+            for (int k = 0; k < S::kKeys / 16; k++)
+                mma_ts(tmem + S::kTmemO + q * DP, tmem + S::kTmemS + buf * S::kKeys + k * 8, desc_values(v_tile + k * 2048, S::kKeys * 128), id_o,
+                       accumulate || k > 0);
+            umma_commit(pv_done + 8 * q);
         };
-        const auto release = [&](uint32_t bar) {
-            if (elect_one()) umma_commit(bar);
-            __syncwarp();
-        };
+        const auto buffer = [](int q, unsigned n) { return S::kBufs == 2 ? n & 1 : (uint32_t)q; };
         const auto two_on = [](Place<S::kSlots>& p) { p.next(); p.next(); };
         for (bool more = true; more && ok; more = w.next(a)) {
             if (!w.any() || w.t1() <= w.t0()) continue;
@@ -614,42 +607,52 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             for (int q = 0; q < NQ; q++) end[q] = tiles_end<NQ, S::kKeys>(a, w, q);
             if (!wait(full(k_at.slot), k_at.phase) || !wait(q_full, unit & 1)) break;
             tc_after();
+            if (elect_one()) {
 #pragma unroll
-            for (int q = 0; q < NQ; q++)
-                if (end[q] > t0) scores(q, NQ == 1 ? n_tiles[0] & 1 : q);
-            release(empty(k_at.slot));
-            if (t1 - t0 == 1) release(q_empty);
+                for (int q = 0; q < NQ; q++)
+                    if (end[q] > t0) scores(q, buffer(q, n_tiles[q]));
+                umma_commit(empty(k_at.slot));
+                if (t1 - t0 == 1) umma_commit(q_empty);
+            }
+            __syncwarp();
             two_on(k_at);
             for (int tile = t0; tile < t1 && ok; tile++) {
                 const bool ahead = tile + 1 < t1;
                 if (ahead && !wait(full(k_at.slot), k_at.phase)) break;
-                if constexpr (NQ == 1) {
-                    tc_after();
-                    if (ahead) {
-                        scores(0, (n_tiles[0] + 1) & 1);
-                        release(empty(k_at.slot));
-                        if (tile + 2 == t1) release(q_empty);
-                        two_on(k_at);
+                if constexpr (S::kBufs == 2) {
+                    if (ahead) {                 // the next scores, into the buffer whose weights have had their product issued
+                        tc_after();
+                        if (elect_one()) {
+                            scores(0, buffer(0, n_tiles[0] + 1));
+                            umma_commit(empty(k_at.slot));
+                            if (tile + 2 == t1) umma_commit(q_empty);
+                        }
+                        __syncwarp();
                     }
                 }
                 if (!wait(full(v_at.slot), v_at.phase)) break;
 #pragma unroll
                 for (int q = 0; q < NQ; q++) {
-                    if (tile >= end[q]) continue;
-                    const uint32_t buf = NQ == 1 ? n_tiles[q] & 1 : (uint32_t)q, phase = NQ == 1 ? n_tiles[q] >> 1 & 1 : n_tiles[q] & 1;
-                    if (!wait(p_full + 8 * buf, phase)) break;
+                    const bool mine = tile < end[q], last = q == NQ - 1;
+                    const uint32_t buf = buffer(q, n_tiles[q]), phase = (S::kBufs == 2 ? n_tiles[q] >> 1 : n_tiles[q]) & 1;
+                    if (mine && !wait(p_full + 8 * buf, phase)) break;
                     tc_after();
-                    values(q, buf, tile > t0);
-                    n_tiles[q]++;
-                    if (NQ > 1 && tile + 1 < end[q]) scores(q, q);
+                    if (elect_one()) {
+                        if (mine) values(q, buf, tile > t0);
+                        if (S::kBufs == 1 && tile + 1 < end[q]) scores(q, buf);  // (behind the product that reads the weights there)
+                        if (last) {
+                            umma_commit(empty(v_at.slot));
+                            if (S::kBufs == 1 && ahead) {
+                                umma_commit(empty(k_at.slot));
+                                if (tile + 2 == t1) umma_commit(q_empty);
+                            }
+                        }
+                    }
+                    __syncwarp();
+                    n_tiles[q] += mine;
                 }
-                release(empty(v_at.slot));
                 two_on(v_at);
-                if (NQ > 1 && ahead) {
-                    release(empty(k_at.slot));
-                    if (tile + 2 == t1) release(q_empty);
-                    two_on(k_at);
-                }
+                if (ahead) two_on(k_at);
             }
             unit++;
         }

@@ -40,6 +40,8 @@ def test_far_blocks(fq, new, heads, dt):
     big = [store.as_strided(size, (1 << 20, kv * dim, dim, 1), offset) for offset in (0, 1 << 19)]
     table_far, table_near = dev([[2199, 3, 2100, 2150, 2049, 2198, 7, 2047, 2048]]), dev([list(range(9))])
     small = [torch.zeros((9, block, kv, dim), dtype=dt, device="cuda") for _ in range(2)]
+    for t in big:
+        t[table_far[0].long()] = 0               # (what no token is stored in is compared too)
     lens = dev([130 if new < 100 else 140])
     starts = dev([0, new])
     before = int(lens) - new
