@@ -369,7 +369,7 @@ int fq_distill_topk_grad(fq_ctx* ctx, const void* logits_dev, int dtype, int row
 /* A sequence's keys and values lie in blocks of `block_size` tokens that may be anywhere in a layer's cache; its row of a block table names them in order,
  * the same for all layers.  Cell p of a sequence is token p % block_size of block table[p / block_size]; a slot is block * block_size + that.
  * What these calls read from device memory is checked there: a number that cannot be (a block outside the cache, a negative length) is never
- * followed; it is recorded for fq_status, and each call says what its outputs are then. */
+ * followed; it is recorded for fq_status, and each call says what its outputs are then.  Their many arguments come in a structure each, which is read during the call. */
 
 #define FQ_MAX_SEQS 16384       /* sequences of one call */
 #define FQ_MAX_TREE_WORDS 16    /* 64-bit words of a row of tree bits */
@@ -409,9 +409,22 @@ typedef struct fq_cache {
  * and slots all -1.  A parent that is not a smaller number counts as -1 (FQ_ERR_INDEX).
  * 1 <= n_seqs <= FQ_MAX_SEQS, 1 <= tokens <= FQ_MAX_ROWS, 1 <= max_blocks <= 2^20, 1 <= block_size <= 2^16, max_blocks * block_size < 2^30.
  * Calls that share any of the updated arrays have to be ordered. */
-int fq_cache_step(fq_ctx* ctx, int n_seqs, int* lens_dev, const int* keep_dev, const int* new_dev, int* table_dev, long long ld, int max_blocks,
-                  int block_size, int* free_dev, int free_room, int* free_count_dev, const int* parents_dev, int tokens, int* starts_dev,
-                  long long* slots_dev, int* positions_dev, uint64_t* mask_dev, int words, void* stream);
+typedef struct fq_cache_step_args {
+    int* lens_dev;
+    const int* keep_dev;
+    const int* new_dev;
+    int* table_dev;
+    long long ld;
+    int* free_dev;
+    int* free_count_dev;
+    const int* parents_dev;
+    int* starts_dev;
+    long long* slots_dev;
+    int* positions_dev;
+    uint64_t* mask_dev;
+    int n_seqs, max_blocks, block_size, free_room, tokens, words;
+} fq_cache_step_args;
+int fq_cache_step(fq_ctx* ctx, const fq_cache_step_args* args, void* stream);
 
 /* The accepted branch of every sequence's drafted tokens is moved together, in n_caches caches (keys or values of a layer each): the key or value of new token
  * kept[b][i] goes to cell before + i, where `before` = lens[b] less the sequence's new tokens, for i < n_kept[b].  kept[b][0 .. n_kept) rises
@@ -419,9 +432,20 @@ int fq_cache_step(fq_ctx* ctx, int n_seqs, int* lens_dev, const int* keep_dev, c
  *   caches_host   host array of n_caches device pointers, each a cache as in fq_cache (dtype, strides and sizes are those of all)
  *   kept_dev      int [n_seqs][ld_kept >= max_kept], n_kept_dev int [n_seqs];  1 <= max_kept <= 1024
  *   keep_dev      int [n_seqs]                before + n_kept: what fq_cache_step is to keep next (written) */
-int fq_cache_move(fq_ctx* ctx, void* const* caches_host, int n_caches, const fq_cache* layout, int dtype, int head_dim, int n_seqs, const int* table_dev,
-                  long long ld, int max_blocks, const int* starts_dev, const int* lens_dev, const int* kept_dev, long long ld_kept,
-                  int max_kept, const int* n_kept_dev, int* keep_dev, void* stream);
+typedef struct fq_cache_move_args {
+    void* const* caches_host;
+    fq_cache layout;            /* k_dev and v_dev are not looked at */
+    const int* table_dev;
+    long long ld;
+    const int* starts_dev;
+    const int* lens_dev;
+    const int* kept_dev;
+    long long ld_kept;
+    const int* n_kept_dev;
+    int* keep_dev;
+    int n_caches, dtype, head_dim, n_seqs, max_blocks, max_kept;
+} fq_cache_move_args;
+int fq_cache_move(fq_ctx* ctx, const fq_cache_move_args* args, void* stream);
 
 /* Angles of rotary positions: pair i of rot_dim / 2 turns by f_i radians a position, f_i = base^(-2i / rot_dim), in a longer context than the trained one
  * scaled by parts:  r = context * f_i / (2 pi) turns within the original context,  g = (r - low) / (high - low) kept within [0, 1],
@@ -433,18 +457,31 @@ int fq_rotary_table(int rot_dim, double base, double factor, int context, double
 /* Rotary positions.  Of every head the first rot_dim values are turned in pairs (x_i, x_{i + rot_dim/2}), or (x_2i, x_{2i+1}) if `interleaved`:
  *   y = magnitude (x cos a - x' sin a),   y' = magnitude (x sin a + x' cos a),   a = angle of pair i at the token's position;
  * the others are copied.  `inverse` turns the other way, which with the same magnitude is the gradient.  fp32 arithmetic, one rounding.
- *   x, y          n (1 .. 4) tensors and where they go; y[i] may be x[i] itself, with the same strides
+ *   x, y          n (1 or 2) tensors and where they go; y[i] may be x[i] itself, with the same strides
  *   positions_dev int32 or int64 [tokens] (id_bytes 4 or 8)
  *   turns_dev     uint64 [rot_dim / 2], 8-byte aligned, from fq_rotary_table
  * rot_dim even, 2 <= rot_dim <= head_dim <= 1024; 1 <= tokens <= FQ_MAX_ROWS; up to 1024 heads; any alignment to the type. */
-int fq_rotary(fq_ctx* ctx, const fq_heads* x, const fq_heads* y, int n, int dtype, int tokens, int head_dim, int rot_dim, const void* positions_dev,
-              int id_bytes, const uint64_t* turns_dev, int interleaved, int inverse, float magnitude, void* stream);
+typedef struct fq_rotary_args {
+    fq_heads x[2], y[2];
+    const void* positions_dev;
+    const uint64_t* turns_dev;
+    int n, dtype, tokens, head_dim, rot_dim, id_bytes, interleaved, inverse;
+    float magnitude;
+} fq_rotary_args;
+int fq_rotary(fq_ctx* ctx, const fq_rotary_args* args, void* stream);
 
 /* The same in a serving step: q is turned into q_out (may be q), k is turned and stored with v in the layer's cache, at slots_dev int64 [tokens].  Tokens with a
  * negative slot are not stored; nor are those with a slot outside the cache (FQ_ERR_INDEX).  No two tokens may have the same slot. */
-int fq_rotary_cache(fq_ctx* ctx, const fq_heads* q, const fq_heads* q_out, const fq_heads* k, const fq_heads* v, const fq_cache* cache, int dtype,
-                    int tokens, int head_dim, int rot_dim, const void* positions_dev, int id_bytes, const long long* slots_dev,
-                    const uint64_t* turns_dev, int interleaved, float magnitude, void* stream);
+typedef struct fq_rotary_cache_args {
+    fq_heads q, q_out, k, v;
+    fq_cache cache;
+    const void* positions_dev;
+    const long long* slots_dev;
+    const uint64_t* turns_dev;
+    int dtype, tokens, head_dim, rot_dim, id_bytes, interleaved;
+    float magnitude;
+} fq_rotary_cache_args;
+int fq_rotary_cache(fq_ctx* ctx, const fq_rotary_cache_args* args, void* stream);
 
 /* Attention of every sequence's new tokens, which are the last ones in its cache, over all that is cached and those of the new ones that they see:
  *   out = sum_j p_j v_j,   p = softmax(scale q . k_j) over the cells j that the token sees;   lse = log sum exp(scale q . k_j)
@@ -462,10 +499,22 @@ int fq_rotary_cache(fq_ctx* ctx, const fq_heads* q, const fq_heads* q_out, const
  * head_dim a multiple of 8, up to 256; up to 1024 heads; sizes as in fq_cache_step.  Scores and sums in fp32, p rounded to dtype for the product with v, out rounded
  * once.  The result does not depend on what else is in the batch beyond the order in which fp32 sums are formed; the same call gives the same bits.
  * Cells in a block outside the cache count as zeros, and a sequence with fewer cells than new tokens as one whose rows see nothing (FQ_ERR_INDEX). */
+typedef struct fq_attention_args {
+    fq_heads q, out;
+    fq_cache cache;
+    const int* starts_dev;
+    const int* lens_dev;
+    const int* table_dev;
+    long long ld;
+    const uint64_t* mask_dev;
+    float* lse_dev;
+    void* scratch_dev;
+    size_t scratch_bytes;
+    int dtype, head_dim, tokens, n_seqs, max_blocks, words, new_tokens;
+    float scale;
+} fq_attention_args;
 size_t fq_tree_attention_scratch(const fq_ctx* ctx, int n_seqs, int tokens, int q_heads, int cache_heads, int head_dim, int new_tokens);
-int fq_tree_attention(fq_ctx* ctx, const fq_heads* q, const fq_heads* out, const fq_cache* cache, int dtype, int head_dim, int tokens, int n_seqs,
-                      const int* starts_dev, const int* lens_dev, const int* table_dev, long long ld, int max_blocks, const uint64_t* mask_dev, int words,
-                      int new_tokens, float scale, float* lse_dev, void* scratch_dev, size_t scratch_bytes, void* stream);
+int fq_tree_attention(fq_ctx* ctx, const fq_attention_args* args, void* stream);
 
 /* Test / reporting support ------------------------------------------------------------ */
 

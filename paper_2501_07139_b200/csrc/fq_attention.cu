@@ -457,7 +457,7 @@ int launch_typed(const fq_ctx* ctx, const AttnArgs& a, int rows, int dp, cudaStr
     return cudaLaunchKernelEx(&cfg, attention_join_kernel<T>, a, rows, dp, rows > kRows ? 1 : 0, workers_of(rows)) == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
 }
 
-bool good_sizes(const fq_ctx* ctx, int n_seqs, int tokens, int q_heads, int cache_heads, int head_dim, int new_tokens)
+bool good_sizes(int n_seqs, int tokens, int q_heads, int cache_heads, int head_dim, int new_tokens)
 {
     return n_seqs >= 1 && n_seqs <= FQ_MAX_SEQS && tokens >= 1 && tokens <= FQ_MAX_ROWS && cache_heads >= 1 && q_heads >= cache_heads && q_heads <= 1024 &&
            q_heads % cache_heads == 0 && head_dim >= 8 && head_dim <= 256 && head_dim % 8 == 0 && new_tokens >= 1;
@@ -474,50 +474,52 @@ extern "C" {
 
 size_t fq_tree_attention_scratch(const fq_ctx* ctx, int n_seqs, int tokens, int q_heads, int cache_heads, int head_dim, int new_tokens)
 {
-    if (!ctx || !good_sizes(ctx, n_seqs, tokens, q_heads, cache_heads, head_dim, new_tokens)) return 0;
+    if (!ctx || !good_sizes(n_seqs, tokens, q_heads, cache_heads, head_dim, new_tokens)) return 0;
     const int dp = padded_dim(head_dim), rows = unit_rows(new_tokens, q_heads / cache_heads, dp);
     return join_bytes(ctx) + (size_t)ctx->sm_count * workers_of(rows) * 2 * rows * (dp + 2) * sizeof(float);
 }
 
-int fq_tree_attention(fq_ctx* ctx, const fq_heads* q, const fq_heads* out, const fq_cache* cache, int dtype, int head_dim, int tokens, int n_seqs,
-                      const int* starts_dev, const int* lens_dev, const int* table_dev, long long ld, int max_blocks, const uint64_t* mask_dev, int words,
-                      int new_tokens, float scale, float* lse_dev, void* scratch_dev, size_t scratch_bytes, void* stream)
+int fq_tree_attention(fq_ctx* ctx, const fq_attention_args* args, void* stream)
 {
-    if (!ctx || !q || !out || !cache || !q->dev || !out->dev || !starts_dev || !lens_dev || !scratch_dev) return FQ_ERR_ARG;
-    if ((dtype != FQ_DT_F16 && dtype != FQ_DT_BF16) || !(scale > 0.0f) || !std::isfinite(scale)) return FQ_ERR_ARG;
-    if (!good_sizes(ctx, n_seqs, tokens, q->heads, cache->heads, head_dim, new_tokens) || out->heads != q->heads) return FQ_ERR_SHAPE;
-    if (mask_dev && (words < 1 || words > FQ_MAX_TREE_WORDS)) return FQ_ERR_SHAPE;
-    int rc = check_heads(out, dtype, tokens, head_dim);
-    if (rc == FQ_OK) rc = check_cache(cache, dtype, head_dim);
-    if (rc == FQ_OK) rc = check_table(table_dev, ld, n_seqs, max_blocks, cache->block_size);
+    if (!ctx || !args) return FQ_ERR_ARG;
+    const fq_attention_args& x = *args;
+    const fq_heads &q = x.q, &out = x.out;
+    const fq_cache& cache = x.cache;
+    if (!q.dev || !out.dev || !x.starts_dev || !x.lens_dev || !x.scratch_dev) return FQ_ERR_ARG;
+    if ((x.dtype != FQ_DT_F16 && x.dtype != FQ_DT_BF16) || !(x.scale > 0.0f) || !std::isfinite(x.scale)) return FQ_ERR_ARG;
+    if (!good_sizes(x.n_seqs, x.tokens, q.heads, cache.heads, x.head_dim, x.new_tokens) || out.heads != q.heads) return FQ_ERR_SHAPE;
+    if (x.mask_dev && (x.words < 1 || x.words > FQ_MAX_TREE_WORDS)) return FQ_ERR_SHAPE;
+    int rc = check_heads(&out, x.dtype, x.tokens, x.head_dim);
+    if (rc == FQ_OK) rc = check_cache(&cache, x.dtype, x.head_dim);
+    if (rc == FQ_OK) rc = check_table(x.table_dev, x.ld, x.n_seqs, x.max_blocks, cache.block_size);
     if (rc != FQ_OK) return rc;
-    if (q->head_stride < 0 || q->token_stride < 0) return FQ_ERR_SHAPE;
-    const bool many = tokens > 1, wide = q->heads > 1;
-    if (!aligned(q->dev, 16) || !aligned(out->dev, 16) || !aligned(scratch_dev, 16) || !aligned(starts_dev, 4) || !aligned(lens_dev, 4) ||
-        !aligned(mask_dev, 8) || !aligned(lse_dev, 4) || (many && (q->token_stride % 8 || out->token_stride % 8)) ||
-        (wide && (q->head_stride % 8 || out->head_stride % 8)))
+    if (q.head_stride < 0 || q.token_stride < 0) return FQ_ERR_SHAPE;
+    const bool many = x.tokens > 1, wide = q.heads > 1;
+    if (!aligned(q.dev, 16) || !aligned(out.dev, 16) || !aligned(x.scratch_dev, 16) || !aligned(x.starts_dev, 4) || !aligned(x.lens_dev, 4) ||
+        !aligned(x.mask_dev, 8) || !aligned(x.lse_dev, 4) || (many && (q.token_stride % 8 || out.token_stride % 8)) ||
+        (wide && (q.head_stride % 8 || out.head_stride % 8)))
         return FQ_ERR_ALIGN;
-    if (scratch_bytes < fq_tree_attention_scratch(ctx, n_seqs, tokens, q->heads, cache->heads, head_dim, new_tokens)) return FQ_ERR_SCRATCH;
+    if (x.scratch_bytes < fq_tree_attention_scratch(ctx, x.n_seqs, x.tokens, q.heads, cache.heads, x.head_dim, x.new_tokens)) return FQ_ERR_SCRATCH;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
     AttnArgs a{};
-    a.q = q->dev; a.out = out->dev;
-    a.q_token = many ? q->token_stride : 0; a.q_head = wide ? q->head_stride : 0;
-    a.out_token = many ? out->token_stride : 0; a.out_head = wide ? out->head_stride : 0;
-    a.k = cache->k_dev; a.v = cache->v_dev;
-    a.block_stride = cache->blocks > 1 ? cache->block_stride : 0; a.cell_stride = cache->block_size > 1 ? cache->token_stride : 0;
-    a.head_stride = cache->heads > 1 ? cache->head_stride : 0;
-    a.blocks = cache->blocks; a.block_size = cache->block_size;
-    a.tokens = tokens; a.n_seqs = n_seqs; a.kv_heads = cache->heads; a.share = q->heads / cache->heads; a.head_dim = head_dim;
-    a.starts = starts_dev; a.lens = lens_dev; a.table = table_dev; a.ld = ld; a.max_blocks = max_blocks; a.mask = mask_dev; a.words = words;
-    a.scale = (float)((double)scale * 1.4426950408889634);
-    a.lse = lse_dev;
-    a.joins = static_cast<AttnJoin*>(scratch_dev);
-    a.parts = reinterpret_cast<float*>(static_cast<char*>(scratch_dev) + join_bytes(ctx));
+    a.q = q.dev; a.out = out.dev;
+    a.q_token = many ? q.token_stride : 0; a.q_head = wide ? q.head_stride : 0;
+    a.out_token = many ? out.token_stride : 0; a.out_head = wide ? out.head_stride : 0;
+    a.k = cache.k_dev; a.v = cache.v_dev;
+    a.block_stride = cache.blocks > 1 ? cache.block_stride : 0; a.cell_stride = cache.block_size > 1 ? cache.token_stride : 0;
+    a.head_stride = cache.heads > 1 ? cache.head_stride : 0;
+    a.blocks = cache.blocks; a.block_size = cache.block_size;
+    a.tokens = x.tokens; a.n_seqs = x.n_seqs; a.kv_heads = cache.heads; a.share = q.heads / cache.heads; a.head_dim = x.head_dim;
+    a.starts = x.starts_dev; a.lens = x.lens_dev; a.table = x.table_dev; a.ld = x.ld; a.max_blocks = x.max_blocks; a.mask = x.mask_dev; a.words = x.words;
+    a.scale = (float)((double)x.scale * 1.4426950408889634);
+    a.lse = x.lse_dev;
+    a.joins = static_cast<AttnJoin*>(x.scratch_dev);
+    a.parts = reinterpret_cast<float*>(static_cast<char*>(x.scratch_dev) + join_bytes(ctx));
     a.status = ctx->status_dev;
     const cudaStream_t st = (cudaStream_t)stream;
-    const int dp = padded_dim(head_dim), rows = unit_rows(new_tokens, a.share, dp);
-    return dtype == FQ_DT_F16 ? launch_typed<__half>(ctx, a, rows, dp, st) : launch_typed<__nv_bfloat16>(ctx, a, rows, dp, st);
+    const int dp = padded_dim(x.head_dim), rows = unit_rows(x.new_tokens, a.share, dp);
+    return x.dtype == FQ_DT_F16 ? launch_typed<__half>(ctx, a, rows, dp, st) : launch_typed<__nv_bfloat16>(ctx, a, rows, dp, st);
 }
 
 }  // extern "C"

@@ -306,22 +306,23 @@ using namespace fq;
 
 extern "C" {
 
-int fq_cache_step(fq_ctx* ctx, int n_seqs, int* lens_dev, const int* keep_dev, const int* new_dev, int* table_dev, long long ld, int max_blocks,
-                  int block_size, int* free_dev, int free_room, int* free_count_dev, const int* parents_dev, int tokens, int* starts_dev,
-                  long long* slots_dev, int* positions_dev, uint64_t* mask_dev, int words, void* stream)
+int fq_cache_step(fq_ctx* ctx, const fq_cache_step_args* args, void* stream)
 {
-    if (!ctx || !lens_dev || !keep_dev || !new_dev || !free_dev || !free_count_dev || !starts_dev || !slots_dev || !positions_dev) return FQ_ERR_ARG;
-    if (parents_dev && !mask_dev) return FQ_ERR_ARG;
-    const int rc = check_table(table_dev, ld, n_seqs, max_blocks, block_size);
+    if (!ctx || !args) return FQ_ERR_ARG;
+    const fq_cache_step_args& x = *args;
+    if (!x.lens_dev || !x.keep_dev || !x.new_dev || !x.free_dev || !x.free_count_dev || !x.starts_dev || !x.slots_dev || !x.positions_dev) return FQ_ERR_ARG;
+    if (x.parents_dev && !x.mask_dev) return FQ_ERR_ARG;
+    const int rc = check_table(x.table_dev, x.ld, x.n_seqs, x.max_blocks, x.block_size);
     if (rc != FQ_OK) return rc;
-    if (tokens < 1 || tokens > FQ_MAX_ROWS || free_room < 1 || (parents_dev && (words < 1 || words > FQ_MAX_TREE_WORDS))) return FQ_ERR_SHAPE;
-    if (!aligned(lens_dev, 4) || !aligned(keep_dev, 4) || !aligned(new_dev, 4) || !aligned(free_dev, 4) || !aligned(free_count_dev, 4) ||
-        !aligned(parents_dev, 4) || !aligned(starts_dev, 4) || !aligned(slots_dev, 8) || !aligned(positions_dev, 4) || !aligned(mask_dev, 8))
+    if (x.tokens < 1 || x.tokens > FQ_MAX_ROWS || x.free_room < 1 || (x.parents_dev && (x.words < 1 || x.words > FQ_MAX_TREE_WORDS))) return FQ_ERR_SHAPE;
+    if (!aligned(x.lens_dev, 4) || !aligned(x.keep_dev, 4) || !aligned(x.new_dev, 4) || !aligned(x.free_dev, 4) || !aligned(x.free_count_dev, 4) ||
+        !aligned(x.parents_dev, 4) || !aligned(x.starts_dev, 4) || !aligned(x.slots_dev, 8) || !aligned(x.positions_dev, 4) || !aligned(x.mask_dev, 8))
         return FQ_ERR_ALIGN;
+    const int n_seqs = x.n_seqs, tokens = x.tokens;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
-    StepArgs a{n_seqs, max_blocks, block_size, lens_dev, keep_dev, new_dev, table_dev, ld, free_dev, free_room, free_count_dev, parents_dev, tokens,
-               starts_dev, slots_dev, positions_dev, mask_dev, words, 1, tokens <= 4096, ctx->status_dev};
+    StepArgs a{n_seqs, x.max_blocks, x.block_size, x.lens_dev, x.keep_dev, x.new_dev, x.table_dev, x.ld, x.free_dev, x.free_room, x.free_count_dev,
+               x.parents_dev, tokens, x.starts_dev, x.slots_dev, x.positions_dev, x.mask_dev, x.words, 1, tokens <= 4096, ctx->status_dev};
     if (n_seqs > 64 || tokens > 512) a.n_cta = kMaxCluster;
     const size_t smem = 3 * sizeof(int) * (size_t)n_seqs;
     if (smem > 48 * 1024) {
@@ -347,23 +348,24 @@ int fq_cache_step(fq_ctx* ctx, int n_seqs, int* lens_dev, const int* keep_dev, c
     return cudaLaunchKernelEx(&cfg, cache_rows_kernel, a) == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
 }
 
-int fq_cache_move(fq_ctx* ctx, void* const* caches_host, int n_caches, const fq_cache* layout, int dtype, int head_dim, int n_seqs, const int* table_dev,
-                  long long ld, int max_blocks, const int* starts_dev, const int* lens_dev, const int* kept_dev, long long ld_kept,
-                  int max_kept, const int* n_kept_dev, int* keep_dev, void* stream)
+int fq_cache_move(fq_ctx* ctx, const fq_cache_move_args* args, void* stream)
 {
-    const int size = type_size(dtype);
-    if (!ctx || !caches_host || !layout || !starts_dev || !lens_dev || !kept_dev || !n_kept_dev || !keep_dev || !size) return FQ_ERR_ARG;
-    if (n_caches < 1 || n_caches > (1 << 16) || head_dim < 1 || head_dim > 1024 || max_kept < 1 ||
-        max_kept > kMaxKept || ld_kept < max_kept)
+    if (!ctx || !args) return FQ_ERR_ARG;
+    const fq_cache_move_args& x = *args;
+    const int size = type_size(x.dtype), n_caches = x.n_caches;
+    if (!x.caches_host || !x.starts_dev || !x.lens_dev || !x.kept_dev || !x.n_kept_dev || !x.keep_dev || !size) return FQ_ERR_ARG;
+    if (n_caches < 1 || n_caches > (1 << 16) || x.head_dim < 1 || x.head_dim > 1024 || x.max_kept < 1 || x.max_kept > kMaxKept || x.ld_kept < x.max_kept)
         return FQ_ERR_SHAPE;
-    int rc = check_table(table_dev, ld, n_seqs, max_blocks, layout->block_size);
+    int rc = check_table(x.table_dev, x.ld, x.n_seqs, x.max_blocks, x.layout.block_size);
     for (int i = 0; i < n_caches && rc == FQ_OK; i++) {
-        fq_cache c = *layout;
-        c.k_dev = c.v_dev = caches_host[i];
-        rc = check_cache(&c, dtype, head_dim);
+        fq_cache c = x.layout;
+        c.k_dev = c.v_dev = x.caches_host[i];
+        rc = check_cache(&c, x.dtype, x.head_dim);
     }
     if (rc != FQ_OK) return rc;
-    if (!aligned(starts_dev, 4) || !aligned(lens_dev, 4) || !aligned(kept_dev, 4) || !aligned(n_kept_dev, 4) || !aligned(keep_dev, 4)) return FQ_ERR_ALIGN;
+    if (!aligned(x.starts_dev, 4) || !aligned(x.lens_dev, 4) || !aligned(x.kept_dev, 4) || !aligned(x.n_kept_dev, 4) || !aligned(x.keep_dev, 4))
+        return FQ_ERR_ALIGN;
+    const fq_cache* layout = &x.layout;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;
     MoveArgs a{};
@@ -371,15 +373,15 @@ int fq_cache_move(fq_ctx* ctx, void* const* caches_host, int n_caches, const fq_
     a.token_bytes = layout->block_size > 1 ? layout->token_stride * size : 0;
     a.head_bytes = layout->heads > 1 ? layout->head_stride * size : 0;
     a.blocks = layout->blocks; a.block_size = layout->block_size;
-    a.per_head = head_dim * size / 16; a.pieces = a.per_head * layout->heads;
-    a.n_seqs = n_seqs; a.max_blocks = max_blocks; a.table = table_dev; a.ld = ld; a.starts = starts_dev; a.lens = lens_dev;
-    a.kept = kept_dev; a.ld_kept = ld_kept; a.max_kept = max_kept; a.n_kept = n_kept_dev; a.status = ctx->status_dev;
+    a.per_head = x.head_dim * size / 16; a.pieces = a.per_head * layout->heads;
+    a.n_seqs = x.n_seqs; a.max_blocks = x.max_blocks; a.table = x.table_dev; a.ld = x.ld; a.starts = x.starts_dev; a.lens = x.lens_dev;
+    a.kept = x.kept_dev; a.ld_kept = x.ld_kept; a.max_kept = x.max_kept; a.n_kept = x.n_kept_dev; a.status = ctx->status_dev;
     for (int c0 = 0; c0 < n_caches; c0 += kMoveCaches) {
         a.n_caches = n_caches - c0 < kMoveCaches ? n_caches - c0 : kMoveCaches;
-        for (int i = 0; i < a.n_caches; i++) a.cache[i] = caches_host[c0 + i];
-        a.keep = c0 == 0 ? keep_dev : nullptr;
+        for (int i = 0; i < a.n_caches; i++) a.cache[i] = x.caches_host[c0 + i];
+        a.keep = c0 == 0 ? x.keep_dev : nullptr;
         // (at most 128 caches x 1024 heads x 256 pieces)
-        const dim3 grid((unsigned)((a.n_caches * a.pieces + kMoveThreads - 1) / kMoveThreads), (unsigned)n_seqs);
+        const dim3 grid((unsigned)((a.n_caches * a.pieces + kMoveThreads - 1) / kMoveThreads), (unsigned)x.n_seqs);
         cache_move_kernel<<<grid, kMoveThreads, 0, (cudaStream_t)stream>>>(a);
         if (cudaGetLastError() != cudaSuccess) return FQ_ERR_CUDA;
     }

@@ -14,7 +14,7 @@
 namespace fq {
 namespace {
 
-constexpr int kMaxTensors = 4;
+constexpr int kMaxTensors = 3;
 constexpr int kThreads = 256;
 constexpr int kMaxRot = 1024;
 
@@ -298,49 +298,49 @@ int fq_rotary_table(int rot_dim, double base, double factor, int context, double
     return FQ_OK;
 }
 
-int fq_rotary(fq_ctx* ctx, const fq_heads* x, const fq_heads* y, int n, int dtype, int tokens, int head_dim, int rot_dim, const void* positions_dev,
-              int id_bytes, const uint64_t* turns_dev, int interleaved, int inverse, float magnitude, void* stream)
+int fq_rotary(fq_ctx* ctx, const fq_rotary_args* args, void* stream)
 {
-    int rc = check_rotary(ctx, dtype, tokens, head_dim, rot_dim, positions_dev, id_bytes, turns_dev, magnitude);
+    if (!args) return FQ_ERR_ARG;
+    const fq_rotary_args& x = *args;
+    int rc = check_rotary(ctx, x.dtype, x.tokens, x.head_dim, x.rot_dim, x.positions_dev, x.id_bytes, x.turns_dev, x.magnitude);
     if (rc != FQ_OK) return rc;
-    if (!x || !y) return FQ_ERR_ARG;
-    if (n < 1 || n > kMaxTensors) return FQ_ERR_SHAPE;
+    if (x.n < 1 || x.n > 2) return FQ_ERR_SHAPE;
     RotaryArgs a{};
-    for (int i = 0; i < n; i++) {
-        rc = check_pair(x + i, y + i, dtype, tokens, head_dim);
+    for (int i = 0; i < x.n; i++) {
+        rc = check_pair(x.x + i, x.y + i, x.dtype, x.tokens, x.head_dim);
         if (rc != FQ_OK) return rc;
-        a.t[i] = tensor(x + i, y + i, tokens, rot_dim);
+        a.t[i] = tensor(x.x + i, x.y + i, x.tokens, x.rot_dim);
     }
-    a.n = n; a.head_dim = head_dim; a.half = rot_dim / 2;
-    a.positions = positions_dev; a.wide_positions = id_bytes == 8; a.turns = turns_dev;
-    a.magnitude = magnitude; a.side = inverse ? -1.0f : 1.0f; a.status = ctx->status_dev;
-    return launch_rotary(ctx, a, dtype, tokens, rot_dim, interleaved, (cudaStream_t)stream);
+    a.n = x.n; a.head_dim = x.head_dim; a.half = x.rot_dim / 2;
+    a.positions = x.positions_dev; a.wide_positions = x.id_bytes == 8; a.turns = x.turns_dev;
+    a.magnitude = x.magnitude; a.side = x.inverse ? -1.0f : 1.0f; a.status = ctx->status_dev;
+    return launch_rotary(ctx, a, x.dtype, x.tokens, x.rot_dim, x.interleaved, (cudaStream_t)stream);
 }
 
-int fq_rotary_cache(fq_ctx* ctx, const fq_heads* q, const fq_heads* q_out, const fq_heads* k, const fq_heads* v, const fq_cache* cache, int dtype,
-                    int tokens, int head_dim, int rot_dim, const void* positions_dev, int id_bytes, const long long* slots_dev,
-                    const uint64_t* turns_dev, int interleaved, float magnitude, void* stream)
+int fq_rotary_cache(fq_ctx* ctx, const fq_rotary_cache_args* args, void* stream)
 {
-    int rc = check_rotary(ctx, dtype, tokens, head_dim, rot_dim, positions_dev, id_bytes, turns_dev, magnitude);
-    if (rc == FQ_OK) rc = check_pair(q, q_out, dtype, tokens, head_dim);
-    if (rc == FQ_OK) rc = check_source(k, dtype);
-    if (rc == FQ_OK) rc = check_source(v, dtype);
-    if (rc == FQ_OK) rc = check_cache(cache, dtype, head_dim);
+    if (!args) return FQ_ERR_ARG;
+    const fq_rotary_cache_args& x = *args;
+    int rc = check_rotary(ctx, x.dtype, x.tokens, x.head_dim, x.rot_dim, x.positions_dev, x.id_bytes, x.turns_dev, x.magnitude);
+    if (rc == FQ_OK) rc = check_pair(&x.q, &x.q_out, x.dtype, x.tokens, x.head_dim);
+    if (rc == FQ_OK) rc = check_source(&x.k, x.dtype);
+    if (rc == FQ_OK) rc = check_source(&x.v, x.dtype);
+    if (rc == FQ_OK) rc = check_cache(&x.cache, x.dtype, x.head_dim);
     if (rc != FQ_OK) return rc;
-    if (!slots_dev) return FQ_ERR_ARG;
-    if (k->heads != cache->heads || v->heads != cache->heads) return FQ_ERR_SHAPE;
-    if (!aligned(slots_dev, 8)) return FQ_ERR_ALIGN;
+    if (!x.slots_dev) return FQ_ERR_ARG;
+    if (x.k.heads != x.cache.heads || x.v.heads != x.cache.heads) return FQ_ERR_SHAPE;
+    if (!aligned(x.slots_dev, 8)) return FQ_ERR_ALIGN;
     RotaryArgs a{};
-    a.t[0] = tensor(q, q_out, tokens, rot_dim);
-    a.t[1] = to_cache(k, cache, tokens, rot_dim);
-    a.t[2] = to_cache(v, cache, tokens, 0);
-    a.n = 3; a.head_dim = head_dim; a.half = rot_dim / 2;
-    a.positions = positions_dev; a.wide_positions = id_bytes == 8; a.turns = turns_dev;
-    a.magnitude = magnitude; a.side = 1.0f; a.status = ctx->status_dev;
-    a.slots = slots_dev; a.cache[0] = cache->k_dev; a.cache[1] = cache->v_dev;
-    a.block_stride = cache->block_stride; a.token_stride = cache->token_stride; a.block_size = cache->block_size;
-    a.n_slots = (long long)cache->blocks * cache->block_size;
-    return launch_rotary(ctx, a, dtype, tokens, rot_dim, interleaved, (cudaStream_t)stream);
+    a.t[0] = tensor(&x.q, &x.q_out, x.tokens, x.rot_dim);
+    a.t[1] = to_cache(&x.k, &x.cache, x.tokens, x.rot_dim);
+    a.t[2] = to_cache(&x.v, &x.cache, x.tokens, 0);
+    a.n = 3; a.head_dim = x.head_dim; a.half = x.rot_dim / 2;
+    a.positions = x.positions_dev; a.wide_positions = x.id_bytes == 8; a.turns = x.turns_dev;
+    a.magnitude = x.magnitude; a.side = 1.0f; a.status = ctx->status_dev;
+    a.slots = x.slots_dev; a.cache[0] = x.cache.k_dev; a.cache[1] = x.cache.v_dev;
+    a.block_stride = x.cache.block_stride; a.token_stride = x.cache.token_stride; a.block_size = x.cache.block_size;
+    a.n_slots = (long long)x.cache.blocks * x.cache.block_size;
+    return launch_rotary(ctx, a, x.dtype, x.tokens, x.rot_dim, x.interleaved, (cudaStream_t)stream);
 }
 
 }  // extern "C"

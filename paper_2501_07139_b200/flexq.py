@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from array import array
 from operator import attrgetter
 from typing import List, Optional, Sequence
@@ -60,13 +61,14 @@ class GemmPlan(C.Structure):
     _fields_ = [("two_pass", C.c_int), ("shared", C.c_int), ("blocks", C.c_int), ("tile_tokens", C.c_int), ("tiles", C.c_longlong)]
 
 
-class Heads(C.Structure):
-    _fields_ = [("dev", C.c_void_p), ("token_stride", C.c_longlong), ("head_stride", C.c_longlong), ("heads", C.c_int)]
-
-
-class Cache(C.Structure):
-    _fields_ = [("k_dev", C.c_void_p), ("v_dev", C.c_void_p), ("block_stride", C.c_longlong), ("token_stride", C.c_longlong),
-                ("head_stride", C.c_longlong), ("blocks", C.c_int), ("block_size", C.c_int), ("heads", C.c_int)]
+# The structures that the calls between the linear layers take, packed as C lays them out: an address, then strides, then counts.
+_HEADS, _CACHE = "qqqi4x", "qqqqqiii4x"
+_STEP_ARGS = struct.Struct("qqqqqqqqqqqqiiiiii")
+_MOVE_ARGS = struct.Struct("q" + _CACHE + "qqqqqqqqiiiiii")
+_ROTARY_ARGS = struct.Struct(4 * _HEADS + "qqiiiiiiiif4x")
+_ROTARY_CACHE_ARGS = struct.Struct(4 * _HEADS + _CACHE + "qqqiiiiiif4x")
+_ATTENTION_ARGS = struct.Struct(2 * _HEADS + _CACHE + "qqqqqqqqiiiiiiif")
+_NO_HEADS = (0, 0, 0, 0)
 
 
 class FlexQError(RuntimeError):
@@ -130,15 +132,12 @@ def lib():
     L.fq_token_logprobs.argtypes = [vp, vp, i, i, i, ll, vp, i, fl, vp, vp, i, vp, vp, vp]
     L.fq_distill_topk.argtypes = [vp, vp, i, i, i, ll, vp, i, vp, i, fl, vp, vp, vp, vp, ll, vp]
     L.fq_distill_topk_grad.argtypes = [vp, vp, i, i, i, ll, vp, i, vp, i, fl, vp, vp, vp, ll, vp]
-    hp, cp, db = vp, vp, C.c_double
-    L.fq_cache_step.argtypes = [vp, i, vp, vp, vp, vp, ll, i, i, vp, i, vp, vp, i, vp, vp, vp, vp, i, vp]
-    L.fq_cache_move.argtypes = [vp, vp, i, cp, i, i, i, vp, ll, i, vp, vp, vp, ll, i, vp, vp, vp]
+    db = C.c_double
+    for name in ("fq_cache_step", "fq_cache_move", "fq_rotary", "fq_rotary_cache", "fq_tree_attention"):
+        getattr(L, name).argtypes = [vp, vp, vp]
     L.fq_rotary_table.argtypes = [i, db, db, i, db, db, vp]
-    L.fq_rotary.argtypes = [vp, hp, hp, i, i, i, i, i, vp, i, vp, i, i, fl, vp]
-    L.fq_rotary_cache.argtypes = [vp, hp, hp, hp, hp, cp, i, i, i, i, vp, i, vp, vp, i, fl, vp]
     L.fq_tree_attention_scratch.argtypes = [vp, i, i, i, i, i, i]
     L.fq_tree_attention_scratch.restype = C.c_size_t
-    L.fq_tree_attention.argtypes = [vp, hp, hp, cp, i, i, i, i, vp, vp, vp, ll, i, vp, i, i, fl, vp, vp, C.c_size_t, vp]
     L.fq_strerror.argtypes = [i]
     L.fq_strerror.restype = C.c_char_p
     for name in EXPORTS:
@@ -260,6 +259,7 @@ class FlexQ:
         self.n_layers = n_layers
         self._keep = {}          # (layer, bits) -> stored variant retained by the context
         self._stack_keep = None
+        self._scratch = {}       # sizes of an attention call -> bytes of scratch
 
     # -- lifetime -----------------------------------------------------------------
     def fq_destroy(self):
@@ -564,24 +564,24 @@ class FlexQ:
         return grad
 
     # -- between the linear layers of a block -----------------------------------------------------
-    def _heads(self, t: torch.Tensor, name: str, types, tokens: Optional[int] = None, dim: Optional[int] = None) -> Heads:
+    def _heads(self, t: torch.Tensor, name: str, types, tokens: Optional[int] = None, dim: Optional[int] = None) -> tuple:
         shape, st = t.shape, t.stride()
         if len(shape) == 3:
             n, heads, d = shape
             if t.dtype in types and t.get_device() == self._index and (st[2] == 1 or d < 2) and (tokens is None or (n == tokens and d == dim)):
-                return Heads(t.data_ptr(), st[0], st[1], heads)
+                return t.data_ptr(), st[0], st[1], heads
         wanted = "[tokens][heads][values]" if tokens is None else f"[{tokens}][heads][{dim}]"
         raise ValueError(f"{name}: {wanted} of {', '.join(str(d) for d in types)} on {self.device} with dense values are needed, not "
                          f"{t.dtype} {tuple(shape)} with strides {st} on {t.device}")
 
-    def _cache(self, k: torch.Tensor, v: torch.Tensor, types, dim: Optional[int] = None) -> Cache:
+    def _cache(self, k: torch.Tensor, v: torch.Tensor, types, dim: Optional[int] = None) -> tuple:
         shape, st, dt = k.shape, k.stride(), k.dtype
         if len(shape) == 4 and dt in types and k.get_device() == self._index and (st[3] == 1 or shape[3] < 2) and (
                 k is v or (v.shape == shape and v.stride() == st and v.dtype is dt and v.get_device() == self._index)):
             blocks, block, heads, d = shape
             if dim is not None and d != dim:
                 raise ValueError(f"caches: heads of {dim} are needed, not of {d}")
-            return Cache(k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], blocks, block, heads)
+            return k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], blocks, block, heads
         raise ValueError(f"caches: two of [blocks][block size][heads][values], {', '.join(str(d) for d in types)} on {self.device} with dense values and the "
                          f"same strides are needed, not {dt} {tuple(shape)} {st} on {k.device} and {v.dtype} {tuple(v.shape)} {v.stride()} on {v.device}")
 
@@ -615,9 +615,10 @@ class FlexQ:
         slots, positions, starts = all4.as_strided((tokens,), (1,), 0), narrow.as_strided((tokens,), (1,), 2 * wide), narrow.as_strided((n + 1,), (1,), 2 * wide + tokens)
         mask = all4.as_strided((tokens, width), (width, 1), tokens) if width else None
         at = all4.data_ptr()
-        _check(lib().fq_cache_step(self._h, n, lens.data_ptr(), keep.data_ptr(), new.data_ptr(), table.data_ptr(), ld, blocks, block_size, free.data_ptr(),
-                                   free.numel(), count.data_ptr(), None if parents is None else parents.data_ptr(), tokens, at + 8 * wide + 4 * tokens, at,
-                                   at + 8 * wide, at + 8 * tokens if width else None, width, _stream_on(self.device)), "fq_cache_step")
+        args = _STEP_ARGS.pack(lens.data_ptr(), keep.data_ptr(), new.data_ptr(), table.data_ptr(), ld, free.data_ptr(), count.data_ptr(),
+                               0 if parents is None else parents.data_ptr(), at + 8 * wide + 4 * tokens, at, at + 8 * wide, at + 8 * tokens if width else 0, n,
+                               blocks, block_size, free.numel(), tokens, width)
+        _check(lib().fq_cache_step(self._h, args, _stream_on(self.device)), "fq_cache_step")
         return starts, slots, positions, mask
 
     def fq_cache_move(self, caches: Sequence[torch.Tensor], table: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor, kept: torch.Tensor,
@@ -631,7 +632,8 @@ class FlexQ:
         layout, count = self._cache(caches[0], caches[0], _TYPES), len(caches)
         shape, st, dt = caches[0].shape, caches[0].stride(), caches[0].dtype
         # (a tensor's properties for all of them at once: there are two caches a layer)
-        if list(map(torch.Tensor.size, caches)).count(shape) != count or list(map(torch.Tensor.stride, caches)).count(st) != count or \
+        alike = all(map(torch.Tensor.is_contiguous, caches)) if caches[0].is_contiguous() else list(map(torch.Tensor.stride, caches)).count(st) == count
+        if not alike or list(map(torch.Tensor.size, caches)).count(shape) != count or \
                 list(map(_dtype_of, caches)).count(dt) != count or list(map(torch.Tensor.get_device, caches)).count(self._index) != count:
             raise ValueError(f"caches: {dt} {tuple(shape)} with strides {st} on {self.device} are needed for all")
         pointers = array("Q", map(torch.Tensor.data_ptr, caches))
@@ -644,9 +646,9 @@ class FlexQ:
         if rows != n:
             raise ValueError(f"kept: a row for each of {n} sequences is needed, not {rows}")
         keep = torch.empty(n, dtype=torch.int32, device=self.device)
-        _check(lib().fq_cache_move(self._h, pointers.buffer_info()[0], count, C.byref(layout), _TYPES[dt], shape[3], n,
-                                   table.data_ptr(), ld, blocks, starts.data_ptr(), lens.data_ptr(), kept.data_ptr(), max(ld_kept, most), most,
-                                   n_kept.data_ptr(), keep.data_ptr(), _stream_on(self.device)), "fq_cache_move")
+        args = _MOVE_ARGS.pack(pointers.buffer_info()[0], *layout, table.data_ptr(), ld, starts.data_ptr(), lens.data_ptr(), kept.data_ptr(), max(ld_kept, most),
+                               n_kept.data_ptr(), keep.data_ptr(), count, _TYPES[dt], shape[3], n, blocks, most)
+        _check(lib().fq_cache_move(self._h, args, _stream_on(self.device)), "fq_cache_move")
         return keep
 
     def _positions(self, positions, turns, tokens):
@@ -659,21 +661,28 @@ class FlexQ:
         """Rotary positions of q and k, [tokens][heads][values] (any strides, values dense): the first 2 * len(turns) values of every head are turned in pairs by the
         angles of fq_rotary_table, values i and i + len(turns), or `interleaved` 2i and 2i + 1.  `inverse` turns back, which is the gradient.  Into q_out and
         k_out, which may be q and k; new ones where they are not given.  k may be None.  -> (q_out, k_out)"""
-        given = [(q, q_out, "q")] + ([(k, k_out, "k")] if k is not None else [])
         tokens, _, dim = q.shape if q.dim() == 3 else (0, 0, 0)
-        x, y, outs = (Heads * 2)(), (Heads * 2)(), [None, None]
-        for i, (src, dst, name) in enumerate(given):
-            x[i] = self._heads(src, name, _TYPES if i == 0 else (q.dtype,), tokens, dim)
-            if dst is None:
-                dst = torch.empty(src.shape, dtype=src.dtype, device=self.device)
-            elif dst.shape != src.shape:
-                raise ValueError(f"{name}_out: {tuple(src.shape)} is needed, not {tuple(dst.shape)}")
-            y[i] = self._heads(dst, name + "_out", (q.dtype,), tokens, dim)
-            outs[i] = dst
+        same = (q.dtype,)
+        hq, hk, hk_out = self._heads(q, "q", _TYPES), _NO_HEADS, _NO_HEADS
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+        elif q_out.shape != q.shape:
+            raise ValueError(f"q_out: {tuple(q.shape)} is needed, not {tuple(q_out.shape)}")
+        hq_out = self._heads(q_out, "q_out", same)
+        if k is not None:
+            hk = self._heads(k, "k", same, tokens, dim)
+            if k_out is None:
+                k_out = torch.empty(k.shape, dtype=k.dtype, device=self.device)
+            elif k_out.shape != k.shape:
+                raise ValueError(f"k_out: {tuple(k.shape)} is needed, not {tuple(k_out.shape)}")
+            hk_out = self._heads(k_out, "k_out", same)
+        elif k_out is not None:
+            raise ValueError("k_out without k")
         rot = self._positions(positions, turns, tokens)
-        _check(lib().fq_rotary(self._h, x, y, len(given), _TYPES[q.dtype], tokens, dim, rot, positions.data_ptr(), positions.element_size(), turns.data_ptr(),
-                               1 if interleaved else 0, 1 if inverse else 0, magnitude, _stream_on(self.device)), "fq_rotary")
-        return outs[0], outs[1]
+        args = _ROTARY_ARGS.pack(*hq, *hk, *hq_out, *hk_out, positions.data_ptr(), turns.data_ptr(), 1 if k is None else 2, _TYPES[q.dtype], tokens, dim, rot,
+                                 positions.element_size(), 1 if interleaved else 0, 1 if inverse else 0, magnitude)
+        _check(lib().fq_rotary(self._h, args, _stream_on(self.device)), "fq_rotary")
+        return q_out, k_out
 
     def fq_rotary_cache(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor, turns: torch.Tensor,
                         k_cache: torch.Tensor, v_cache: torch.Tensor, q_out: Optional[torch.Tensor] = None, interleaved: bool = False, magnitude: float = 1.0):
@@ -690,9 +699,9 @@ class FlexQ:
         cache = self._cache(k_cache, v_cache, same, dim)
         rot = self._positions(positions, turns, tokens)
         self._dense(slots, "slots", _I64, (tokens,))
-        _check(lib().fq_rotary_cache(self._h, C.byref(hq), C.byref(ho), C.byref(hk), C.byref(hv), C.byref(cache), _TYPES[q.dtype], tokens, dim, rot,
-                                     positions.data_ptr(), positions.element_size(), slots.data_ptr(), turns.data_ptr(), 1 if interleaved else 0, magnitude,
-                                     _stream_on(self.device)), "fq_rotary_cache")
+        args = _ROTARY_CACHE_ARGS.pack(*hq, *ho, *hk, *hv, *cache, positions.data_ptr(), slots.data_ptr(), turns.data_ptr(), _TYPES[q.dtype], tokens, dim, rot,
+                                       positions.element_size(), 1 if interleaved else 0, magnitude)
+        _check(lib().fq_rotary_cache(self._h, args, _stream_on(self.device)), "fq_rotary_cache")
         return q_out
 
     def fq_tree_attention(self, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, starts: torch.Tensor,
@@ -723,9 +732,15 @@ class FlexQ:
             self._dense(lse, "lse", _F32, (tokens, heads))
         if new is None:
             new = -(-tokens // max(n, 1))
-        size = lib().fq_tree_attention_scratch(self._h, n, tokens, heads, cache.heads, dim, new)
+        sizes = (n, tokens, heads, cache[7], dim, new)
+        size = self._scratch.get(sizes)
+        if size is None:
+            if len(self._scratch) >= 1024:
+                self._scratch.clear()
+            size = self._scratch[sizes] = lib().fq_tree_attention_scratch(self._h, *sizes)
         scratch = torch.empty(max(size, 16), dtype=torch.uint8, device=self.device)
-        _check(lib().fq_tree_attention(self._h, C.byref(hq), C.byref(ho), C.byref(cache), _TYPES[q.dtype], dim, tokens, n, starts.data_ptr(), lens.data_ptr(),
-                                       table.data_ptr(), ld, blocks, None if mask is None else mask.data_ptr(), words, new, dim ** -0.5 if scale is None else scale,
-                                       None if lse is None else lse.data_ptr(), scratch.data_ptr(), size, _stream_on(self.device)), "fq_tree_attention")
+        args = _ATTENTION_ARGS.pack(*hq, *ho, *cache, starts.data_ptr(), lens.data_ptr(), table.data_ptr(), ld, 0 if mask is None else mask.data_ptr(),
+                                    0 if lse is None else lse.data_ptr(), scratch.data_ptr(), size, _TYPES[q.dtype], dim, tokens, n, blocks, words, new,
+                                    dim ** -0.5 if scale is None else scale)
+        _check(lib().fq_tree_attention(self._h, args, _stream_on(self.device)), "fq_tree_attention")
         return out

@@ -100,17 +100,17 @@ def test_many_caches_and_tokens(fq):
 
 
 def test_scratch_that_is_too_small(fq):
-    import ctypes as C
     import paper_2501_07139_b200 as P
+    from paper_2501_07139_b200 import flexq as F
     q, cache = torch.zeros((1, 4, 64), device="cuda").half(), torch.zeros((2, 2, 16, 4, 64), device="cuda").half()
     h, c = fq._heads(q, "q", (q.dtype,)), fq._cache(cache[0], cache[1], (q.dtype,))
     size = P.lib().fq_tree_attention_scratch(fq._h, 1, 1, 4, 4, 64, 1)
-    i32 = dev([0, 0])
-    out = fq._heads(torch.zeros_like(q), "out", (q.dtype,))
+    i32, result = dev([0, 0]), torch.zeros_like(q)
     for given, code in ((size - 1, -9), (0, -9), (size, 0)):
         scratch = torch.empty(size, dtype=torch.uint8, device="cuda")
-        assert P.lib().fq_tree_attention(fq._h, C.byref(h), C.byref(out), C.byref(c), 0, 64, 1, 1, i32.data_ptr(), i32.data_ptr(), i32.data_ptr(), 2, 2, None, 0, 1, 1.0, None,
-                                         scratch.data_ptr(), given, None) == code
+        args = F._ATTENTION_ARGS.pack(*h, *fq._heads(result, "out", (q.dtype,)), *c, i32.data_ptr(), i32.data_ptr(), i32.data_ptr(), 2, 0, 0, scratch.data_ptr(), given,
+                                      F.FQ_DT_F16, 64, 1, 1, 2, 0, 1, 1.0)
+        assert P.lib().fq_tree_attention(fq._h, args, None) == code
     assert size > 0 and fq.fq_status() == 0
 
 
