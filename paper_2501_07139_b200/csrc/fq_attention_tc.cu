@@ -300,7 +300,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             __syncwarp();
             if (lane == 0) mbar_arrive(unit_begun);
             const int n = w.tile * S::kRows + q * 128 + r, rows = w.s.fresh * a.share;
-            const bool real = n < rows;
+            const bool real = n < rows, idle = n - lane >= rows;                 // idle: the warp has no row at all
             const int t = min(n, rows - 1) / a.share, row = w.s.row0 + t;
             const int t0 = w.t0(), t1 = tiles_end<NQ, S::kKeys>(a, w, q);
             // cells before this one are seen by all rows of the tile
@@ -309,6 +309,11 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             for (int tile = t0; tile < t1; tile++, n_tiles++) {
                 const uint32_t buf = S::kBufs == 2 ? n_tiles & 1 : (uint32_t)q, phase = (S::kBufs == 2 ? n_tiles >> 1 : n_tiles) & 1;
                 if (!wait(s_full + 8 * buf, phase)) break;
+                if (idle) {                      // (whatever stands for weights there: no row has anything from another)
+                    if (tile > t0 && !wait(pv_done + 8 * q, (n_tiles - 1) & 1)) break;
+                    if (lane == 0) mbar_arrive(p_full + 8 * buf);
+                    continue;
+                }
                 tc_after();
                 const uint32_t s_at = lanes + S::kTmemS + buf * S::kKeys;
                 const int cell0 = tile * S::kKeys;
@@ -390,7 +395,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             T* out = static_cast<T*>(a.out) + row * a.out_token + h * a.out_head;
             float* part = a.parts + (long long)(blockIdx.x * 2 + (t0 == 0)) * S::kRows * (DP + 2);
 #pragma unroll 1
-            for (int c = 0; c < DP; c += 32) {
+            for (int c = 0; c < (idle ? 0 : DP); c += 32) {
                 float v[32];
                 if (t1 > t0) {
                     tmem_ld32(o_at + c, v);
@@ -398,18 +403,18 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 #pragma unroll
                     for (int j = 0; j < 32; j++) v[j] = 0.0f;
                 }
-                if (!real) continue;
-                if (whole) {
+                if (real && whole) {
 #pragma unroll
                     for (int j = 0; j < 32; j += 8)
                         if (c + j < a.head_dim)
                             *reinterpret_cast<uint4*>(out + c + j) = make_uint4(pack2<T>(v[j] * by, v[j + 1] * by), pack2<T>(v[j + 2] * by, v[j + 3] * by),
                                                                                 pack2<T>(v[j + 4] * by, v[j + 5] * by), pack2<T>(v[j + 6] * by, v[j + 7] * by));
-                } else {
+                } else if (real) {
 #pragma unroll
                     for (int j = 0; j < 32; j += 4)
                         *reinterpret_cast<float4*>(part + ((c + j) / 4 * S::kRows + q * 128 + r) * 4) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
                 }
+                __syncwarp();                    // (the next load is the whole warp's)
             }
             if (odd && real) {
 #pragma unroll 1
