@@ -429,14 +429,14 @@ int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 12
 // Query rows of a unit, by how many a key head has.  (Measured, us; "warps" is this file's kernel.)
 //   Up to 16, heads of up to 128: warps.  48 sequences of 4096, 40 heads, 1 row: 316, tensor cores 371; 64 of 1000, 8 heads, 8 rows: 37 and 56, 16 rows 47 and 56; one
 //   of 4000, 32 heads, 1 row: 20.5 and 26.7.  Larger heads: tensor cores (16 sequences of 4000, 8 heads of 256, 1 row: 77, warps 82; 8 rows of 32 x 2000: 74 and 94).
-//   Up to 384: one tile of 128 query rows at a time.  16 sequences of 16000, 8 heads, 32 rows: 106, warps 144; 5 of 40000, 240 rows: 144, two tiles 145;
-//   300 rows of 2 x 8000 cells, 32 heads: 101 and 116.  More: two tiles side by side, which read keys once.  480 rows of 5 x 40000: 227, one tile 245; 8000 of
-//   one prompt: 617 and 704.
+//   Up to 256: one tile of 128 query rows at a time.  16 sequences of 16000, 8 heads, 32 rows: 106, warps 144; 5 of 40000, 240 rows: 156, two tiles 156.  More:
+//   two tiles side by side, which read keys once for both.  480 rows of 5 x 40000: 230, one tile at a time 308; 320 rows: 218 and 237; four prompts of up to 2048:
+//   144 and 155; 300 rows of 2 x 8000 cells, 32 heads: 108 and 110.
 int unit_rows(int new_tokens, int share, int dp)
 {
     const long long rows = (long long)new_tokens * share;
     if (dp == 256) return 128;
-    return rows <= kRows ? kRows : rows <= 384 ? 128 : 256;
+    return rows <= kRows ? kRows : rows <= 256 ? 128 : 256;
 }
 int workers_of(int rows) { return rows > kRows ? 1 : kWorkers; }
 
