@@ -394,8 +394,8 @@ typedef struct fq_cache {
  * less: drafted tokens were refused; 0: another request takes its place.  Blocks that are no longer needed go to the end of the free list, in the order of sequences
  * and cells; then the needed ones come from its end.
  *   lens_dev      int [n_seqs]                tokens in the cache before (read) and after (written: keep + new)
- *   keep_dev, new_dev int [n_seqs]            0 <= keep <= lens, new >= 0
- *   table_dev     int [n_seqs][ld >= max_blocks]   block numbers (updated; entries that no token uses any more become -1)
+ *   keep_dev, new_dev int [n_seqs]            0 <= keep <= lens, new >= 0; keep_dev may be lens_dev itself (all go on)
+ *   table_dev     int [n_seqs][ld >= max_blocks]   block numbers (updated; entries that no token uses any more become -1); a block is one sequence's
  *   free_dev      int [free_room], free_count_dev int [1]   the free list and how many it holds (updated)
  *   parents_dev   int [tokens] or NULL        drafted trees: for every new token the number (within its sequence's new tokens) of the one before it in
  *                                             its branch, always a smaller number; -1: it follows what is cached
@@ -487,7 +487,7 @@ int fq_rotary_cache(fq_ctx* ctx, const fq_rotary_cache_args* args, void* stream)
  *   out = sum_j p_j v_j,   p = softmax(scale q . k_j) over the cells j that the token sees;   lse = log sum exp(scale q . k_j)
  * Query heads share key heads in groups: head h uses key head h / (q heads / cache heads).  A token sees all cells before the new ones and, of the new ones,
  * those of its bits in mask_dev; with mask_dev NULL those up to itself (single tokens, drafted chains, prompts).  A row that sees nothing: out 0,
- * lse -inf.  What a row does not see does not touch it, an infinity or a NaN in it neither; one that it sees makes its values infinite or NaN.
+ * lse -inf; a score of -inf counts as a cell that it does not see.  What a row does not see does not touch it, an infinity or a NaN in it neither; one that it sees makes its values infinite or NaN.
  *   q, out        dtype fp16 or bf16, [tokens][q heads][head_dim]; 16-byte aligned, strides multiples of 8; out may not overlap q
  *   cache         of the same dtype
  *   starts_dev    int [n_seqs + 1]: rows of the sequences' new tokens (may be none); rows behind the last are left as they are

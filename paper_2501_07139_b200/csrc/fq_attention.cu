@@ -506,6 +506,7 @@ int fq_tree_attention(fq_ctx* ctx, const fq_attention_args* args, void* stream)
     a.q = q.dev; a.out = out.dev;
     a.q_token = many ? q.token_stride : 0; a.q_head = wide ? q.head_stride : 0;
     a.out_token = many ? out.token_stride : 0; a.out_head = wide ? out.head_stride : 0;
+    a.rows_by_tma = 128 % (q.heads / cache.heads) == 0 && (!many || q.token_stride > 0) && (!wide || q.head_stride > 0);
     a.k = cache.k_dev; a.v = cache.v_dev;
     a.block_stride = cache.blocks > 1 ? cache.block_stride : 0; a.cell_stride = cache.block_size > 1 ? cache.token_stride : 0;
     a.head_stride = cache.heads > 1 ? cache.head_stride : 0;

@@ -20,6 +20,7 @@ struct AttnArgs {
     const void* q;
     void* out;
     long long q_token, q_head, out_token, out_head;
+    bool rows_by_tma;                            // a tile of 128 query rows is a whole number of tokens, and no stride is 0
     const void* k;
     const void* v;
     long long block_stride, cell_stride, head_stride;
@@ -42,7 +43,8 @@ struct AttnArgs {
 
 // A unit that begins in this CTA and ends in another.
 struct AttnJoin {
-    int seq_row0, row0, head, others;            // first rows of the sequence in the batch and of the unit in the sequence; others: CTAs behind this one that hold parts (0: nothing to join)
+    int seq_row0, row0, head;                    // first rows of the sequence in the batch and of the unit in the sequence
+    int others;                                  // CTAs behind this one that hold parts (0: nothing to join)
     int rows;                                    // rows of the unit
     int slot;                                    // where its first part is
     int pad[2];

@@ -215,7 +215,7 @@ __device__ __forceinline__ void tma_cells(uint32_t dst, const CUtensorMap* map, 
                  ::"r"(dst), "l"(map), "r"(value), "r"(cell), "r"(head), "r"(block), "r"(bar) : "memory");
 }
 
-//   run : cells of a TMA box;  q_map: query rows of [token][key head][head of its group][value], used where the group's size divides 128
+//   run : cells of a TMA box;  q_map: query rows of [token][key head][head of its group][value], if rows_by_tma
 template <class T, int DP, int NQ>
 __global__ void __launch_bounds__(TcShape<DP, NQ>::kThreads, 1)
 attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
@@ -450,7 +450,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             if (t1 <= t0) continue;
             // once the unit before has formed its last scores
             if (!wait(q_empty, (unit & 1) ^ 1)) break;
-            if (128 % a.share == 0) {
+            if (a.rows_by_tma) {
                 if (lane == 0) mbar_expect_tx(q_full, NQ * S::kQBytes);
                 __syncwarp();
                 const int token = w.s.row0 + w.tile * (S::kRows / a.share);      // (rows of other sequences, or none, behind the last token: nobody uses them)
@@ -709,7 +709,7 @@ int launch(const fq_ctx* ctx, const AttnArgs& a, cudaStream_t st)
     }
     const int run = std::gcd(a.block_size, S::kKeys);
     CUtensorMap k_map, v_map, q_map{};
-    if (128 % a.share == 0 && rows_map(&q_map, a) != FQ_OK) return FQ_ERR_CUDA;
+    if (a.rows_by_tma && rows_map(&q_map, a) != FQ_OK) return FQ_ERR_CUDA;
     if (cells_map(&k_map, a.k, a, run) != FQ_OK || cells_map(&v_map, a.v, a, run) != FQ_OK) return FQ_ERR_CUDA;
     attention_tc_kernel<T, DP, NQ><<<ctx->sm_count, S::kThreads, S::kTotal, st>>>(a, k_map, v_map, q_map, run);
     return cudaGetLastError() == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;

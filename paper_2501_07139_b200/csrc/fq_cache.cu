@@ -77,7 +77,8 @@ __device__ __forceinline__ void phase_end(int n_cta)
     }
 }
 
-// Row t of the batch: slot, position, and in a drafted tree what it sees.  starts[n_seqs]: first rows of the sequences;  rows: of all new tokens.
+// Row t of the batch: slot, position, and in a drafted tree what it sees.  starts[n_seqs]: first rows of the sequences;  rows: of all new tokens.  What
+// was kept of a sequence is told from its new length: `keep` may be the array of the lengths, which has these by now.
 __device__ __forceinline__ void token_row(const StepArgs& a, const int* starts, int t, int rows)
 {
     uint64_t* bits = a.parents ? a.mask + (long long)t * a.words : nullptr;
@@ -94,7 +95,8 @@ __device__ __forceinline__ void token_row(const StepArgs& a, const int* starts, 
         if (starts[mid] <= t) lo = mid;
         else hi = mid - 1;
     }
-    const int keep = a.keep[lo], i = t - starts[lo], cell = keep + i, block = cell / a.block_size;
+    const int keep = __ldcg(a.lens + lo) - ((lo + 1 < a.n_seqs ? starts[lo + 1] : rows) - starts[lo]);
+    const int i = t - starts[lo], cell = keep + i, block = cell / a.block_size;
     a.slots[t] = (long long)__ldcg(a.table + lo * a.ld + block) * a.block_size + (cell - block * a.block_size);
     if (!bits) {
         a.positions[t] = cell;
@@ -185,6 +187,7 @@ __global__ void __launch_bounds__(kThreads) cache_step_kernel(const StepArgs a)
         const int gone = upto(s_back, back, b) - s_back[b], n = upto(s_take, take, b) - s_take[b];
         const int keep = a.keep[b], left = (keep + a.block_size - 1) / a.block_size;
         for (int j = lane; j < max(gone, n); j += 32) a.table[b * a.ld + left + j] = j < n ? __ldcg(a.free_blocks + end - 1 - s_take[b] - j) : -1;
+        __syncwarp();                            // (`keep` may be the lengths themselves)
         if (lane == 0) {
             a.lens[b] = keep + upto(s_rows, rows, b) - s_rows[b];
             a.starts[b] = s_rows[b];

@@ -128,7 +128,30 @@ def test_many_sequences(fq):
     n = 700
     ctx, new = torch.randint(0, 90, (n,), generator=g).tolist(), torch.randint(0, 4, (n,), generator=g).tolist()
     s = make(ctx, new, 4, 2, 64, 16, torch.float16, True)
-    check(s, *call(fq, s))
+    for hint in (1, 40, 500):
+        check(s, *call(fq, s, new=hint))
+    assert fq.fq_status() == 0
+
+
+@pytest.mark.parametrize("heads,kv,new", [(200, 1, 3), (96, 2, 5), (128, 1, 2), (24, 8, 100)])
+def test_large_and_odd_groups(fq, heads, kv, new):
+    """Query heads to a key head: more than a tile of rows, sizes that do not divide it."""
+    s = make([150, 0], [new, new], heads, kv, 64, 16, torch.bfloat16, True, words=2)
+    for hint in (1, 40, 500):
+        check(s, *call(fq, s, new=hint))
+    assert fq.fq_status() == 0
+
+
+def test_queries_that_are_repeated(fq):
+    """One token's queries, or one head's, for all: strides of 0."""
+    s = make([100, 30], [20, 33], 8, 2, 128, 16, torch.float16)
+    for q in (s["q"][:1].expand(53, 8, 128), s["q"][:, :1].expand(53, 8, 128)):
+        want, lse = call(fq, {**s, "q": q.contiguous()})
+        for hint in (1, 20, 500):
+            got, lse2 = call(fq, {**s, "q": q}, new=hint)
+            check({**s, "q": q.contiguous()}, got, lse2)
+            same, lse3 = call(fq, {**s, "q": q.contiguous()}, new=hint)
+            assert torch.equal(got, same) and torch.equal(lse2, lse3)
     assert fq.fq_status() == 0
 
 

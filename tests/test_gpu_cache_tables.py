@@ -80,6 +80,21 @@ def test_a_run_of_steps(fq):
     assert fq.fq_status() == 0
 
 
+@pytest.mark.parametrize("n,tokens", [(3, 40), (400, 9000)])
+def test_all_go_on(fq, n, tokens):
+    """The lengths themselves as what is kept."""
+    g = torch.Generator().manual_seed(n)
+    lens, new = torch.randint(0, 50, (n,), generator=g).tolist(), torch.randint(0, tokens // n, (n,), generator=g).tolist()
+    blocks = sum(O.ceil_div(a + b, 8) for a, b in zip(lens, new)) + 2
+    table, rest = O.make_table(lens, 8, 30, blocks, g)
+    free, rows, count = rest + [0] * (blocks - len(rest)), table.tolist(), len(rest)
+    d, t, f, c = dev(lens), table.cuda(), dev(free), dev([count])
+    got = fq.fq_cache_step(d, d, dev(new), t, f, c, 8, tokens)
+    starts, slots, positions, _, count = O.step(lens, list(lens), new, rows, free, count, 8, tokens)
+    assert fq.fq_status() == 0 and d.tolist() == lens and t.tolist() == rows and c.tolist() == [count]
+    assert got[0].tolist() == starts and got[1].tolist() == slots and got[2].tolist() == positions
+
+
 BAD = {
     "blocks": (dict(count=[1]), -13), "width": (dict(new=[3, 200, 0]), -13), "rows": (dict(new=[30, 30, 30]), -13), "keep": (dict(keep=[3, 41, 0]), -14),
     "negative new": (dict(new=[1, -1, 1]), -14), "negative length": (dict(lens=[-1, 40, 5]), -14), "long": (dict(lens=[3, 4000, 5]), -14),
