@@ -34,7 +34,7 @@ def build_library(force: bool = False, verbose: bool = False, checked: bool = Fa
     """Compiles every .cu under csrc/ into libflexq.so next to this file (if stale).  checked=True builds
     libflexq_checked.so instead: the decode kernels, the fused GEMM and the batch kernel verify every global-memory index they
     compute against the size of the buffer it falls in, skip an access that would be outside and report FQ_ERR_BOUNDS through fq_status
-    (fq_gemm_i8.cu, fq_gemv_i8.cu, fq_quant_rows.cu and fq_logits.cu have no such checks)."""
+    (fq_gemm_i8.cu, fq_gemv_i8.cu, fq_quant_rows.cu, fq_logits.cu, fq_cache.cu, fq_rotary.cu, fq_attention.cu and fq_attention_tc.cu have no such checks)."""
     lib = LIB_CHECKED if checked else LIB
     if not force and not _stale(lib):
         return lib
