@@ -30,12 +30,15 @@ struct Shape {                                   // DP: head_dim, rounded up to 
     // A unit's ends (the queries' way here, the results' way out) take the time of two chunks; a worker gets no less than four.
     using Work = Deal<kRows, kChunk, 2, kThreads, kWarps, 4>;
     static constexpr int oSums = kWarps * kStages * kStageBytes;             // long long [Work::kSums]
-    static constexpr int oFlags = oSums + Work::kSums * 8;                   // int [warps]
-    static constexpr int kTotal = oFlags + kWarps * 4;
+    static constexpr int oLeft = oSums + Work::kSums * 8;                    // Left [warps]
+    static constexpr int kTotal = oLeft + kWarps * 32;
     static_assert(kTotal <= 232448, "shared memory over the per-CTA limit");
 };
-// What a warp leaves: a part of the unit that it continues, whether that ends here, a part of a unit that ends elsewhere.
+// What a warp leaves: a part of the unit that it continues, whether that ends here, a part of a unit that ends elsewhere; rows of the first, and the
+// second: its rows, first row of its sequence in the batch, row tile, key head.
 enum { kContinues = 1, kEnds = 2, kBegins = 4 };
+struct Left { int flag, lead_rows, rows, seq_row0, tile, head, pad[2]; };
+static_assert(sizeof(Left) == 32, "Shape::oLeft");
 
 __device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t addr)
 {
@@ -116,7 +119,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
     extern __shared__ __align__(1024) char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     const uint32_t ring = smem_u32(smem) + warp * S::kStages * S::kStageBytes;
-    volatile int* flags = reinterpret_cast<volatile int*>(smem + S::oFlags);
+    volatile Left* left = reinterpret_cast<volatile Left*>(smem + S::oLeft);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");              // (the joining kernel waits for this one's end)
     if (tid == 0) {
         AttnJoin none{};
@@ -345,30 +348,40 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
     }
     copies_wait<0>();
 
-    // ---- what the warps have of the same units
-    if (lane == 0) flags[warp] = flag;
+    // ---- what the warps have of the same units, joined by all of them
+    const bool begins = flag & kBegins;
+    if (lane == 0) {
+        left[warp].flag = flag;
+        left[warp].lead_rows = lead_rows;
+        if (begins) {
+            left[warp].rows = min(w.s.fresh * a.share - w.tile * kRows, kRows);
+            left[warp].seq_row0 = w.s.row0; left[warp].tile = w.tile; left[warp].head = w.head;
+        }
+    }
     __syncthreads();
-    // Parts of warps `first` .. that are of one unit: all of it, or what goes to scratch for the other kernel.
-    const auto join = [&](int first, int rows, bool begins) {
+    // Unit by unit: the one that this CTA continues (f = -1), then those that begin in a warp and end elsewhere.
+    for (int f = -1; f < w.per_cta; f++) {
+        const int first = max(f, 0);
+        if (f < 0 ? (left[0].flag & (kContinues | kEnds)) != kContinues : !(left[f].flag & kBegins)) continue;   // (one that ends in the first warp is in scratch already)
         int n = 1;
-        bool ends = !begins && (flags[first] & kEnds);
-        if (ends) return true;                   // (in scratch already)
-        while (!ends && first + n < w.per_cta && (flags[first + n] & kContinues)) {
-            ends = flags[first + n] & kEnds;
+        bool ends = false;
+        while (!ends && first + n < w.per_cta && (left[first + n].flag & kContinues)) {
+            ends = left[first + n].flag & kEnds;
             n++;
         }
-        const bool out = begins && ends;
+        const bool out = f >= 0 && ends;         // all of the unit is here; else it goes to scratch for the other kernel
+        const int rows = f < 0 ? left[0].lead_rows : left[f].rows;
         const float* last = a.parts + (long long)(blockIdx.x * S::kWarps + first + n - 1) * 2 * S::kSlot;
         const auto part = [&](int x) -> const float* {
             return ends && x == n - 1 ? last : reinterpret_cast<const float*>(smem + (first + x) * S::kStages * S::kStageBytes);
         };
-        float* to = parts + (begins ? S::kSlot : 0);
-        for (int i = lane; i < rows * (DP / 4); i += 32) {
+        float* to = a.parts + ((long long)(blockIdx.x * S::kWarps + first) * 2 + (f >= 0)) * S::kSlot;
+        for (int i = tid; i < rows * (DP / 4); i += S::kThreads) {
             const int r = i / (DP / 4), d = i % (DP / 4) * 4;
             if (d >= a.head_dim) continue;
             const Joined j = join_parts(part, n, r * DP + d, kRows * DP + r, kRows * (DP + 1) + r);
             if (out) {
-                write_out<T>(a, w.s.row0, w.tile * kRows + r, w.head, d, j);
+                write_out<T>(a, left[f].seq_row0, left[f].tile * kRows + r, left[f].head, d, j);
                 continue;
             }
             *reinterpret_cast<float4*>(to + r * DP + d) = j.v;
@@ -377,13 +390,8 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
                 to[kRows * (DP + 1) + r] = j.sum;
             }
         }
-        return ends;
-    };
-    if (warp == 0 && (flag & kContinues)) join(0, lead_rows, false);
-    if (flag & kBegins) {
-        const int rows = min(w.s.fresh * a.share - w.tile * kRows, kRows);
-        if (!join(warp, rows, true) && lane == 0)
-            a.joins[blockIdx.x] = AttnJoin{w.s.row0, w.tile * kRows, w.head, w.others(), rows, (int)(blockIdx.x * S::kWarps + warp) * 2 + 1, {0, 0}};
+        if (f >= 0 && !ends && warp == f && lane == 0)
+            a.joins[blockIdx.x] = AttnJoin{w.s.row0, w.tile * kRows, w.head, w.others(), rows, (int)(blockIdx.x * S::kWarps + f) * 2 + 1, {0, 0}};
     }
 }
 
@@ -427,8 +435,8 @@ int launch_attention(const fq_ctx* ctx, const AttnArgs& a, cudaStream_t st)
 int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
 // Query rows of a unit, by how many a key head has.  (Measured, us; "warps" is this file's kernel.)
-//   Up to 16, heads of up to 128: warps.  48 sequences of 4096, 40 heads, 1 row: 316, tensor cores 371; 64 of 1000, 8 heads, 8 rows: 37 and 56, 16 rows 47 and 56; one
-//   of 4000, 32 heads, 1 row: 20.5 and 26.7.  Larger heads: tensor cores (16 sequences of 4000, 8 heads of 256, 1 row: 77, warps 82; 8 rows of 32 x 2000: 74 and 94).
+//   Up to 16, heads of up to 128: warps.  48 sequences of 4096, 40 heads, 1 row: 326, tensor cores 414; 64 of 1000, 8 heads, 8 rows: 37 and 59, 16 rows 45 and 59; one
+//   of 4000, 32 heads, 1 row: 20.6 and 26.7, 8 heads, 16 rows: 22 and 25.  Larger heads: tensor cores (16 sequences of 4000, 8 heads of 256, 1 row: 77, warps 82; 8 rows of 32 x 2000: 74 and 94).
 //   Up to 256: one tile of 128 query rows at a time.  16 sequences of 16000, 8 heads, 32 rows: 106, warps 144; 5 of 40000, 240 rows: 156, two tiles 156.  More:
 //   two tiles side by side, which read keys once for both.  480 rows of 5 x 40000: 230, one tile at a time 308; 320 rows: 218 and 237; four prompts of up to 2048:
 //   144 and 155; 300 rows of 2 x 8000 cells, 32 heads: 108 and 110.
