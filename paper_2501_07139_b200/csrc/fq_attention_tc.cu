@@ -293,7 +293,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);              // (32 lanes a warp, in the address's upper half)
         const uint32_t o_at = lanes + S::kTmemO + q * DP;
         unsigned n_tiles = 0;                                                    // of this query tile so far
-        uint32_t turn = 0;
+        uint32_t turn = 0, o_turn = 0;
         int unit = 0;                                                            // (those that have key tiles)
         for (bool more = true; more && ok; more = w.next(a)) {
             if (!w.any()) continue;
@@ -310,7 +310,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 const uint32_t buf = S::kBufs == 2 ? n_tiles & 1 : (uint32_t)q, phase = (S::kBufs == 2 ? n_tiles >> 1 : n_tiles) & 1;
                 if (!wait(s_full + 8 * buf, phase)) break;
                 if (idle) {                      // (whatever stands for weights there: no row has anything from another)
-                    if (tile > t0 && !wait(pv_done + 8 * q, (n_tiles - 1) & 1)) break;
+                    if (S::kBufs == 2 && tile > t0 && !wait(pv_done + 8 * q, (n_tiles - 1) & 1)) break;
                     if (lane == 0) mbar_arrive(p_full + 8 * buf);
                     continue;
                 }
@@ -349,7 +349,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 }
                 const bool late = tile > t0 && __any_sync(0xffffffffu, far);
                 if (late) {
-                    if (!wait(pv_done + 8 * q, (n_tiles - 1) & 1)) break;
+                    if (S::kBufs == 2 && !wait(pv_done + 8 * q, (n_tiles - 1) & 1)) break;
                     tc_after();
 #pragma unroll 1
                     for (int c = 0; c < DP; c += 32) {
@@ -377,8 +377,9 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 }
                 l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                 tmem_st_wait();
-                // (every product's end is waited for in its turn: a parity tells it from the one before it only)
-                if (tile > t0 && !late && !wait(pv_done + 8 * q, (n_tiles - 1) & 1)) break;
+                // (every product's end is waited for in its turn: a parity tells it from the one before it only.  With one buffer these scores were
+                // issued behind that product, and what tells of them tells of it.)
+                if (S::kBufs == 2 && tile > t0 && !late && !wait(pv_done + 8 * q, (n_tiles - 1) & 1)) break;
                 tc_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full + 8 * buf);
@@ -386,7 +387,8 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             if (!ok) break;
             // ---- the part's end
             if (t1 > t0) {
-                if (!wait(pv_done + 8 * q, (n_tiles - 1) & 1)) break;
+                if (!wait(pv_done + 8 * q, S::kBufs == 2 ? (n_tiles - 1) & 1 : o_turn)) break;
+                o_turn ^= 1;
                 tc_after();
             }
             const bool whole = w.whole(), odd = spoilt[unit & 7] == unit;
@@ -594,13 +596,13 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             }
             umma_commit(s_full + 8 * buf);
         };
-        const auto values = [&](int q, uint32_t buf, bool accumulate) {
+        const auto values = [&](int q, uint32_t buf, bool accumulate, bool last) {
             const uint32_t v_tile = ring + v_at.slot * S::kSlotBytes;
 #pragma unroll
             for (int k = 0; k < S::kKeys / 16; k++)
                 mma_ts(tmem + S::kTmemO + q * DP, tmem + S::kTmemS + buf * S::kKeys + k * 8, desc_values(v_tile + k * 2048, S::kKeys * 128), id_o,
                        accumulate || k > 0);
-            umma_commit(pv_done + 8 * q);
+            if (S::kBufs == 2 || last) umma_commit(pv_done + 8 * q);
         };
         const auto buffer = [](int q, unsigned n) { return S::kBufs == 2 ? n & 1 : (uint32_t)q; };
         const auto two_on = [](Place<S::kSlots>& p) { p.next(); p.next(); };
@@ -643,7 +645,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     if (mine && !wait(p_full + 8 * buf, phase)) break;
                     tc_after();
                     if (elect_one()) {
-                        if (mine) values(q, buf, tile > t0);
+                        if (mine) values(q, buf, tile > t0, tile + 1 == end[q]);
                         if (S::kBufs == 1 && tile + 1 < end[q]) scores(q, buf);  // (behind the product that reads the weights there)
                         if (last) {
                             umma_commit(empty(v_at.slot));
