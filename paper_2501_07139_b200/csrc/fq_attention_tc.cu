@@ -4,7 +4,7 @@
 //   warps 0 .. 4 NQ - 1   softmax, a thread a row: scores from TMEM, weights back into the same columns, running maximum and sum in registers; values
 //                         are rescaled only when a maximum has risen by more than a factor of 2^8 (rare behind a row's first tiles), so that nobody
 //                         waits for the product in between
-//   1 warp                brings the query rows, and looks through value tiles that not all rows see for infinities and NaNs
+//   1 warp                says which unit is next, brings the query rows, and looks through value tiles that not all rows see for infinities and NaNs
 //   2 warps               TMA, keys and values: runs of cells that lie together in a block (as many as divide both the block and the tile) into the 128-byte swizzled rows that the
 //                         tensor core reads; a ring of key and value tiles that runs ahead over units
 //   1 warp                issues tcgen05.mma: scores = Q K^T (both from shared memory), values += P V (P in TMEM, V as it lies, d contiguous)
@@ -37,16 +37,28 @@ struct TcShape {
     static constexpr int kSlots = (224 * 1024 - NQ * kQBytes) / kSlotBytes < 10 ? (224 * 1024 - NQ * kQBytes) / kSlotBytes : 10;
     static constexpr int oRing = NQ * kQBytes;
     static constexpr int oBars = oRing + kSlots * kSlotBytes;
-    // full[slots] empty[slots] raw[slots] q_full q_empty s_full[4] p_full[4] pv_done[2] unit_begun
-    static constexpr int kBars = 3 * kSlots + 13;
+    // full[slots] empty[slots] raw[slots] q_full q_empty s_full[4] p_full[4] pv_done[2] unit_full[2] unit_empty[2]
+    static constexpr int kBars = 3 * kSlots + 16;
     static constexpr int oSums = oBars + kBars * 8;
     static constexpr int oMisc = oSums + (kWarps + 3) * 8;                   // TMEM address, abort flag, spoilt[8]
-    static constexpr int kTotal = oMisc + 48 + 1024;                         // (tiles start at a multiple of 1024)
+    static constexpr int oUnits = (oMisc + 40 + 15) / 16 * 16;               // Unit [2]
+    static constexpr int kTotal = oUnits + 2 * 64 + 1024;                    // (tiles start at a multiple of 1024)
     static constexpr int kTmemS = 0;                                         // scores of the query tiles, then their values
     static constexpr int kTmemO = kBufs * NQ * kKeys;
     static_assert(kTmemO + NQ * DP <= 512, "TMEM columns");
     static_assert(kTotal <= 232448, "shared memory over the per-CTA limit");
 };
+
+// What the softmax warps and the one that issues products know of a unit.  One warp works it out ahead of time: between units that takes some 4000
+// cycles, while the tensor core idled.  (Prompts of up to 2048: 128 us, 136 where each warp did it for itself; trees of 60 over 40000 cells 220 and 236.)
+struct Unit {
+    int there, whole;                            // 0: no more units
+    int t0, t1, end[2];                          // key tiles of the part; up to where the rows of a query tile see any
+    int b, tile, head;
+    int row0, fresh, len, ctx;                   // of the sequence
+    int pad[3];
+};
+static_assert(sizeof(Unit) == 64, "TcShape::oUnits");
 
 __device__ __forceinline__ void to_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -231,10 +243,12 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     const auto full = [&](int slot) { return bars + slot * 8; };
     const auto empty = [&](int slot) { return bars + (S::kSlots + slot) * 8; };
     const auto raw = [&](int slot) { return bars + (2 * S::kSlots + slot) * 8; };
-    const uint32_t q_full = bars + 3 * S::kSlots * 8, q_empty = q_full + 8, s_full = q_full + 16, p_full = q_full + 48, pv_done = q_full + 80, unit_begun = q_full + 96;
+    const uint32_t q_full = bars + 3 * S::kSlots * 8, q_empty = q_full + 8, s_full = q_full + 16, p_full = q_full + 48, pv_done = q_full + 80;
+    const uint32_t unit_full = q_full + 96, unit_empty = q_full + 112;
     uint32_t* tmem_at = reinterpret_cast<uint32_t*>(smem + S::oMisc);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::oMisc + 4);
     volatile int* spoilt = reinterpret_cast<volatile int*>(smem + S::oMisc + 8);
+    Unit* units = reinterpret_cast<Unit*>(smem + S::oUnits);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");              // (the joining kernel waits for this one's end)
     if (tid == 0) {
         AttnJoin none{};
@@ -248,12 +262,15 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         }
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
-        mbar_init(unit_begun, S::kSoftmax);
         for (int i = 0; i < 4; i++) {
             mbar_init(s_full + 8 * i, 1);
             mbar_init(p_full + 8 * i, 4);
         }
-        for (int i = 0; i < 2; i++) mbar_init(pv_done + 8 * i, 1);
+        for (int i = 0; i < 2; i++) {
+            mbar_init(pv_done + 8 * i, 1);
+            mbar_init(unit_full + 8 * i, 1);
+            mbar_init(unit_empty + 8 * i, S::kSoftmax + 1);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == S::kWarps - 1) {
@@ -279,6 +296,15 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         return ok = __all_sync(0xffffffffu, ok);
     };
 
+    // The nth unit, for the softmax warps and the one that issues products.  Nobody is more than two units ahead of another.
+    const auto take_unit = [&](int nth, Unit& u) {
+        if (!wait(unit_full + 8 * (nth & 1), nth >> 1 & 1)) return false;
+        u = units[nth & 1];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(unit_empty + 8 * (nth & 1));
+        return u.there != 0;
+    };
+
     // With two query tiles a softmax thread holds 128 scores and needs more registers than the 168 that all got; the last four warps give theirs
     // up: 8 x 32 x 208 + 4 x 32 x 88 = 12 x 32 x 168.
     if constexpr (NQ == 2) {
@@ -293,18 +319,18 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);              // (32 lanes a warp, in the address's upper half)
         const uint32_t o_at = lanes + S::kTmemO + q * DP;
         unsigned n_tiles = 0;                                                    // of this query tile so far
-        uint32_t turn = 0, o_turn = 0;
+        uint32_t o_turn = 0;
         int unit = 0;                                                            // (those that have key tiles)
-        for (bool more = true; more && ok; more = w.next(a)) {
-            if (!w.any()) continue;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(unit_begun);
-            const int n = w.tile * S::kRows + q * 128 + r, rows = w.s.fresh * a.share;
+        Unit u;
+        for (int nth = 0; take_unit(nth, u); nth++) {
+            Seq s;
+            s.row0 = u.row0; s.fresh = u.fresh; s.len = u.len; s.ctx = u.ctx;
+            const int n = u.tile * S::kRows + q * 128 + r, rows = s.fresh * a.share;
             const bool real = n < rows, idle = n - lane >= rows;                 // idle: the warp has no row at all
-            const int t = min(n, rows - 1) / a.share, row = w.s.row0 + t;
-            const int t0 = w.t0(), t1 = tiles_end<NQ, S::kKeys>(a, w, q);
+            const int t = min(n, rows - 1) / a.share, row = s.row0 + t;
+            const int t0 = u.t0, t1 = q == 0 ? u.end[0] : u.end[1];
             // cells before this one are seen by all rows of the tile
-            const int all_see = a.mask ? w.s.ctx : w.s.ctx + (w.tile * S::kRows + q * 128) / a.share + 1;
+            const int all_see = a.mask ? s.ctx : s.ctx + (u.tile * S::kRows + q * 128) / a.share + 1;
             float m = -INFINITY, l = 0.0f;                                       // m: of the raw scores
             for (int tile = t0; tile < t1; tile++, n_tiles++) {
                 const uint32_t buf = S::kBufs == 2 ? n_tiles & 1 : (uint32_t)q, phase = (S::kBufs == 2 ? n_tiles >> 1 : n_tiles) & 1;
@@ -330,7 +356,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     if (partial) {
 #pragma unroll
                         for (int b = 0; b < 64; b += 32) {
-                            const uint32_t in = seen32(a, w.s, t, row, cell0 + 64 * c + b);
+                            const uint32_t in = seen32(a, s, t, row, cell0 + 64 * c + b);
 #pragma unroll
                             for (int j = 0; j < 32; j++) v[c][b + j] = in >> j & 1 ? v[c][b + j] : -INFINITY;
                         }
@@ -391,9 +417,9 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 o_turn ^= 1;
                 tc_after();
             }
-            const bool whole = w.whole(), odd = spoilt[unit & 7] == unit;
+            const bool whole = u.whole, odd = spoilt[unit & 7] == unit;
             const float by = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
-            const int h = w.head * a.share + n % a.share;
+            const int h = u.head * a.share + n % a.share;
             T* out = static_cast<T*>(a.out) + row * a.out_token + h * a.out_head;
             float* part = a.parts + (long long)(blockIdx.x * 2 + (t0 == 0)) * S::kRows * (DP + 2);
 #pragma unroll 1
@@ -421,7 +447,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             if (odd && real) {
 #pragma unroll 1
                 for (int d = 0; d < a.head_dim; d++) {
-                    const float x = spoilt_value<T>(a, w.s, w.b, w.head, t, d, t0 * S::kKeys, w.t1() * S::kKeys);
+                    const float x = spoilt_value<T>(a, s, u.b, u.head, t, d, t0 * S::kKeys, u.t1 * S::kKeys);
                     if (x == 0.0f) continue;
                     if (whole) out[d] = (T)x;
                     else part[(d / 4 * S::kRows + q * 128 + r) * 4 + d % 4] = x;
@@ -434,21 +460,39 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             } else if (real && a.lse) {
                 a.lse[(long long)row * (a.kv_heads * a.share) + h] = l == 0.0f ? -INFINITY : (top + log2f(l)) * 0.69314718055994531f;
             }
-            if (tid == 0 && !whole && t0 == 0)
-                a.joins[blockIdx.x] = AttnJoin{w.s.row0, w.tile * S::kRows, w.head, w.others(), min(rows - w.tile * S::kRows, S::kRows), (int)blockIdx.x * 2 + 1, {0, 0}};
-            if (w.t1() > t0) unit++;
-            // nobody is two units ahead of another (the flags of units that hold infinities have eight places)
+            if (u.t1 > t0) unit++;
             tc_before();
-            if (!wait(unit_begun, turn)) break;
-            turn ^= 1;
         }
     } else if (some && warp == S::kSoftmax) {
         // ------------------------------------------------------------------------------------------------ queries, values that not all see
         const int pieces = a.head_dim / 8;
         int pos = 0, unit = 0;                   // tiles of the ring so far
         uint32_t raw_phase = 0;                  // a bit a slot
-        for (bool more = true; more && ok; more = w.next(a)) {
+        int nth = 0;
+        for (bool more = true; ok; more = w.next(a)) {
+            if (more && !w.any()) continue;
+            if (!wait(unit_empty + 8 * (nth & 1), (nth >> 1 & 1) ^ 1)) break;
             const int t0 = w.t0(), t1 = w.t1();
+            if (lane == 0) {
+                Unit u{};
+                u.there = more;
+                if (more) {
+                    u.whole = w.whole();
+                    u.t0 = t0; u.t1 = t1;
+#pragma unroll
+                    for (int q = 0; q < NQ; q++) u.end[q] = tiles_end<NQ, S::kKeys>(a, w, q);
+                    u.b = w.b; u.tile = w.tile; u.head = w.head;
+                    u.row0 = w.s.row0; u.fresh = w.s.fresh; u.len = w.s.len; u.ctx = w.s.ctx;
+                }
+                units[nth & 1] = u;
+                mbar_arrive(unit_full + 8 * (nth & 1));
+                if (more && !u.whole && t0 == 0)
+                    a.joins[blockIdx.x] = AttnJoin{w.s.row0, w.tile * S::kRows, w.head, w.others(), min(w.s.fresh * a.share - w.tile * S::kRows, S::kRows),
+                                                   (int)blockIdx.x * 2 + 1, {0, 0}};
+            }
+            __syncwarp();
+            if (!more) break;
+            nth++;
             if (t1 <= t0) continue;
             // once the unit before has formed its last scores
             if (!wait(q_empty, (unit & 1) ^ 1)) break;
@@ -606,12 +650,11 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         };
         const auto buffer = [](int q, unsigned n) { return S::kBufs == 2 ? n & 1 : (uint32_t)q; };
         const auto two_on = [](Place<S::kSlots>& p) { p.next(); p.next(); };
-        for (bool more = true; more && ok; more = w.next(a)) {
-            if (!w.any() || w.t1() <= w.t0()) continue;
-            const int t0 = w.t0(), t1 = w.t1();
-            int end[NQ];
-#pragma unroll
-            for (int q = 0; q < NQ; q++) end[q] = tiles_end<NQ, S::kKeys>(a, w, q);
+        Unit u;
+        for (int nth = 0; take_unit(nth, u); nth++) {
+            const int t0 = u.t0, t1 = u.t1;
+            if (t1 <= t0) continue;
+            const int end[2] = {u.end[0], u.end[1]};
             if (!wait(full(k_at.slot), k_at.phase) || !wait(q_full, unit & 1)) break;
             tc_after();
             if (elect_one()) {
