@@ -31,7 +31,7 @@ struct TcShape {
     static constexpr int kSoftmax = 4 * NQ;                                  // warps
     static constexpr int kWarps = kSoftmax + 4;
     static constexpr int kThreads = kWarps * 32;
-    static constexpr int kEnds = 640 / kKeys;                                // key tiles' time that a unit's ends take
+    static constexpr int kEnds = 512 / kKeys;                                // key tiles' time that a unit's ends take
     static constexpr int kQBytes = 128 * DP * 2;                             // of a query tile
     static constexpr int kSlotBytes = kKeys * DP * 2;
     static constexpr int kSlots = (224 * 1024 - NQ * kQBytes) / kSlotBytes < 10 ? (224 * 1024 - NQ * kQBytes) / kSlotBytes : 10;
