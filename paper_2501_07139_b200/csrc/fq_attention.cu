@@ -435,11 +435,11 @@ int launch_attention(const fq_ctx* ctx, const AttnArgs& a, cudaStream_t st)
 int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
 // Query rows of a unit, by how many a key head has.  (Measured, us; "warps" is this file's kernel.)
-//   Up to 16, heads of up to 128: warps.  48 sequences of 4096, 40 heads, 1 row: 326, tensor cores 414; 64 of 1000, 8 heads, 8 rows: 37 and 59, 16 rows 45 and 59; one
-//   of 4000, 32 heads, 1 row: 20.6 and 26.7, 8 heads, 16 rows: 22 and 25.  Larger heads: tensor cores (16 sequences of 4000, 8 heads of 256, 1 row: 77, warps 82; 8 rows of 32 x 2000: 74 and 94).
-//   Up to 256: one tile of 128 query rows at a time.  16 sequences of 16000, 8 heads, 32 rows: 106, warps 144; 5 of 40000, 240 rows: 156, two tiles 156.  More:
-//   two tiles side by side, which read keys once for both.  480 rows of 5 x 40000: 230, one tile at a time 308; 320 rows: 218 and 237; four prompts of up to 2048:
-//   144 and 155; 300 rows of 2 x 8000 cells, 32 heads: 108 and 110.
+//   Up to 16, heads of up to 128: warps.  48 sequences of 4096, 40 heads, 1 row: 339, tensor cores 411; 64 of 1000, 8 heads, 8 rows: 37 and 59, 16 rows 44 and 59; one
+//   of 4000, 32 heads, 1 row: 20.5 and 28.5, 8 heads, 16 rows: 22 and 25.  Larger heads: tensor cores (16 sequences of 4000, 8 heads of 256, 1 row: 77, warps 82; 8 rows of 32 x 2000: 74 and 94).
+//   Up to 256: one tile of 128 query rows at a time.  16 sequences of 16000, 8 heads, 32 rows: 114, two tiles 134; 256 rows of 16 x 4000: 55 and 65; 240 rows of 5 x
+//   40000: 153 and 144.  More: two tiles side by side, which read keys once for both.  480 rows of 5 x 40000: 222, one tile at a time 293; 320 rows: 200 and 238; four
+//   prompts of up to 2048: 129 and 151; 300 rows of 2 x 8000 cells, 32 heads: 101 and 109.
 int unit_rows(int new_tokens, int share, int dp)
 {
     const long long rows = (long long)new_tokens * share;
