@@ -243,9 +243,10 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
 #pragma unroll
                     for (int i = 0; i < 4; i++)
                         if (!sees(a, w.s, t[i >> 1], row[i >> 1], cell0 + n * 8 + 2 * c + (i & 1))) sc[n][i] = -INFINITY;
-                // values that not all rows see: none may be infinite or NaN in the product
+                // values that not all rows see: none may be infinite or NaN in the product.  (Those of the cells before stay as they are.)
 #pragma unroll 1
                 for (int i = 0; i < kChunk * kUnits / 32; i++) {
+                    if (cell0 + (i * 32 + lane) / kUnits < all_see) continue;
                     const uint32_t at = vs + (uint32_t)(i * 32 + lane) * 16;
                     const uint4 v = lds128(at);
                     if (finite16<T>(v.x) && finite16<T>(v.y) && finite16<T>(v.z) && finite16<T>(v.w)) continue;
