@@ -333,8 +333,9 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
                 const int r = i / a.head_dim, d = i - r * a.head_dim, n = w.tile * kRows + r, tok = n / a.share;
                 const float x = spoilt_value<T>(a, w.s, w.b, w.head, tok, d, t0 * kChunk, t1 * kChunk);
                 if (x == 0.0f) continue;
-                if (whole) static_cast<T*>(a.out)[(long long)(w.s.row0 + tok) * a.out_token + (w.head * a.share + n - tok * a.share) * a.out_head + d] = (T)x;
-                else part[r * DP + d] = x;
+                T& out = static_cast<T*>(a.out)[(long long)(w.s.row0 + tok) * a.out_token + (w.head * a.share + n - tok * a.share) * a.out_head + d];
+                if (whole) out = (T)((float)out + x);        // (cells that all rows see may have left an infinity there)
+                else part[r * DP + d] += x;
             }
         }
         if (!whole && t0 > 0) {

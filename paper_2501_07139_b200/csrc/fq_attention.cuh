@@ -277,7 +277,7 @@ template <> __device__ __forceinline__ bool finite16<__nv_bfloat16>(uint32_t v) 
 template <> __device__ __forceinline__ bool finite16<__half>(uint32_t v) { return (v & 0x7c00u) != 0x7c00u && (v & 0x7c000000u) != 0x7c000000u; }
 
 // Infinities and NaNs among the values of new tokens are taken out before the product, where a weight of 0 would spread them to rows that do not
-// see them; this says what value d of a row becomes by those that it does see (0: nothing), cells [cell0, cell1).  Units that had any come here, once their
+// see them; this says what they add to value d of a row that does see them (0: nothing), cells [cell0, cell1).  Units that had any come here, once their
 // values are written.
 template <class T>
 __device__ __forceinline__ float spoilt_value(const AttnArgs& a, const Seq& s, int b, int head, int t, int d, int cell0, int cell1)

@@ -449,8 +449,8 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 for (int d = 0; d < a.head_dim; d++) {
                     const float x = spoilt_value<T>(a, s, u.b, u.head, t, d, t0 * S::kKeys, u.t1 * S::kKeys);
                     if (x == 0.0f) continue;
-                    if (whole) out[d] = (T)x;
-                    else part[(d / 4 * S::kRows + q * 128 + r) * 4 + d % 4] = x;
+                    if (whole) out[d] = (T)((float)out[d] + x);      // (cells that all rows see may have left an infinity there)
+                    else part[(d / 4 * S::kRows + q * 128 + r) * 4 + d % 4] += x;
                 }
             }
             const float top = m * a.scale;       // (-inf stays)

@@ -64,6 +64,25 @@ def test_cached_values(fq, dt, tree, dim, heads, kv, new):
     assert fq.fq_status() == 0
 
 
+@pytest.mark.parametrize("heads,kv,new", ROWS)
+@pytest.mark.parametrize("tree", [False, True])
+def test_cached_and_new_values(fq, heads, kv, new, tree):
+    """Both in one tile, of both signs, whichever kernel the number of new tokens asks for; single sequences, whose work is cut, and many, whose work is whole."""
+    for n in (1, 3, 600):
+        ctx = [(37 * b) % 83 + 2 for b in range(n)]
+        s = make(ctx, [new] * n, heads, kv, 64, 16, torch.bfloat16, tree, words=1)
+        hits = []
+        for b in range(0, n, 2):
+            hits += [(b, ctx[b] - 1, 5, math.inf), (b, ctx[b] - 2, 6, math.nan), (b, ctx[b] + b % new, 5, -math.inf), (b, ctx[b] + new - 1, 9, math.inf)]
+        t = spoil(s, hits)
+        want = defined(t)
+        for hint in (None, 1, 30, 500):
+            clean, _ = call(fq, s, new=hint)
+            got, _ = call(fq, t, new=hint)
+            agree(want, clean, got)
+    assert fq.fq_status() == 0
+
+
 @pytest.mark.parametrize("length", [4003, 4007, 4015, 4016])
 @pytest.mark.parametrize("hint", [1, 100])
 def test_long_cache(fq, length, hint):
