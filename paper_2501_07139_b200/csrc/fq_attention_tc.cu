@@ -584,13 +584,15 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             const int all_see = a.mask ? w.s.ctx : w.s.ctx + w.tile * S::kRows / a.share + 1;
             // a block behind the cache reads as zeros: for cells that are not there, and numbers that cannot be
             const auto entry = [&](int cell) { return cell < w.s.len ? a.table[w.b * a.ld + cell / a.block_size] : a.blocks; };
-            const auto block_of = [&](int block) {
-                if ((unsigned)block > (unsigned)a.blocks) atomicCAS(a.status, 0, FQ_ERR_INDEX);
-                return (unsigned)block < (unsigned)a.blocks ? block : a.blocks;
+            const auto block_of = [&](int block, int cell) {                     // (looked at only when it is needed: the load is on its way until then)
+                const bool good = (unsigned)block < (unsigned)a.blocks;
+                if (!good && cell < w.s.len) atomicCAS(a.status, 0, FQ_ERR_INDEX);
+                return good ? block : a.blocks;
             };
+            const auto looked_up = [&](int cell) { return block_of(entry(cell), cell); };
             int ahead = lane < boxes ? entry(t0 * S::kKeys + lane * run) : a.blocks;
             for (int tile = t0; tile < t1; tile++) {
-                const int now = block_of(ahead);
+                const int now = block_of(ahead, lane < boxes ? tile * S::kKeys + lane * run : w.s.len);
                 if (tile + 1 < t1 && lane < boxes) ahead = entry((tile + 1) * S::kKeys + lane * run);            // (on its way meanwhile)
                 if (!wait(empty(at.slot), at.phase ^ 1)) break;
                 const bool look = values && (tile + 1) * S::kKeys > all_see;
@@ -603,7 +605,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     int in[8], cell[8];
 #pragma unroll
                     for (int i = 0; i < 8; i++) {
-                        in[i] = i0 < 32 ? __shfl_sync(0xffffffffu, now, i0 + i) : i0 + i < boxes ? block_of(entry(tile * S::kKeys + (i0 + i) * run)) : 0;
+                        in[i] = i0 < 32 ? __shfl_sync(0xffffffffu, now, i0 + i) : i0 + i < boxes ? looked_up(tile * S::kKeys + (i0 + i) * run) : 0;
                         cell[i] = in_block;
                         in_block += run;
                         if (in_block >= a.block_size) in_block = 0;
