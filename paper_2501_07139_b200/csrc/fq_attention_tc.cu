@@ -533,18 +533,19 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 const int slot = (pos + 2 * (tile - t0) + 1) % S::kSlots;
                 if (!wait(raw(slot), raw_phase >> slot & 1)) break;
                 raw_phase ^= 1u << slot;
-                // cells that all rows see need no look, those behind the sequence's last block were read as zeros
-                const int from = max(0, all_see - tile * S::kKeys), to = min(S::kKeys, (w.s.len + run - 1) / run * run - tile * S::kKeys);
+                const auto piece = [&](int r, int u) { return ring + slot * S::kSlotBytes + (u >> 3) * (S::kKeys * 128) + r * 128 + ((u ^ r) & 7) * 16; };
+                // Cells that all rows see need no look.  Those behind the sequence's last one are nobody's, whatever lies there; behind its last box zeros were read.
+                const int from = max(0, all_see - tile * S::kKeys), there = min(S::kKeys, w.s.len - tile * S::kKeys);
+                const int read = min(S::kKeys, (w.s.len + run - 1) / run * run - tile * S::kKeys);
+                for (int n = there * kUnits + lane; n < read * kUnits; n += 32) sts128(piece(n / kUnits, n % kUnits), make_uint4(0, 0, 0, 0));
                 bool odd = false;
-                for (int r0 = from; r0 < to; r0 += 8 * 32 / kUnits) {
+                for (int r0 = from; r0 < there; r0 += 8 * 32 / kUnits) {
                     uint4 v[8];
-                    uint32_t x[8];
                     typename Pair<T>::Type most = Pair<T>::zero();
 #pragma unroll
                     for (int i = 0; i < 8; i++) {
-                        const int n = i * 32 + lane, r = min(r0 + n / kUnits, to - 1), u = n % kUnits;
-                        x[i] = ring + slot * S::kSlotBytes + (u >> 3) * (S::kKeys * 128) + r * 128 + ((u ^ r) & 7) * 16;
-                        v[i] = lds128(x[i]);
+                        const int n = i * 32 + lane;
+                        v[i] = lds128(piece(min(r0 + n / kUnits, there - 1), n % kUnits));
                     }
 #pragma unroll
                     for (int i = 0; i < 8; i++) Pair<T>::take(most, v[i]);
@@ -552,8 +553,8 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     odd = true;
 #pragma unroll 1
                     for (int i = 0; i < 8; i++) {
-                        const int n = i * 32 + lane, r = min(r0 + n / kUnits, to - 1), u = n % kUnits;
-                        const uint32_t at = ring + slot * S::kSlotBytes + (u >> 3) * (S::kKeys * 128) + r * 128 + ((u ^ r) & 7) * 16;
+                        const int n = i * 32 + lane;
+                        const uint32_t at = piece(min(r0 + n / kUnits, there - 1), n % kUnits);
                         const uint4 y = lds128(at);
                         const uint32_t in[4] = {y.x, y.y, y.z, y.w};
                         uint32_t out[4];
