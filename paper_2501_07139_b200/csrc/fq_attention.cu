@@ -31,7 +31,8 @@ struct Shape {                                   // DP: head_dim, rounded up to 
     using Work = Deal<kRows, kChunk, 2, kThreads, kWarps, 4>;
     static constexpr int oSums = kWarps * kStages * kStageBytes;             // long long [Work::kSums]
     static constexpr int oLeft = oSums + Work::kSums * 8;                    // Left [warps]
-    static constexpr int kTotal = oLeft + kWarps * 32;
+    static constexpr int oOdd = oLeft + kWarps * 32;                         // bits [warps][kOddWords]
+    static constexpr int kTotal = oOdd + kWarps * kOddWords * 4;
     static_assert(kTotal <= 232448, "shared memory over the per-CTA limit");
 };
 // What a warp leaves: a part of the unit that it continues, whether that ends here, a part of a unit that ends elsewhere; rows of the first, and the
@@ -120,6 +121,8 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     const uint32_t ring = smem_u32(smem) + warp * S::kStages * S::kStageBytes;
     volatile Left* left = reinterpret_cast<volatile Left*>(smem + S::oLeft);
+    uint32_t* odd_cells = reinterpret_cast<uint32_t*>(smem + S::oOdd) + warp * kOddWords;
+    odd_cells[lane] = 0;                         // (begin() has a barrier)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");              // (the joining kernel waits for this one's end)
     if (tid == 0) {
         AttnJoin none{};
@@ -246,16 +249,12 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
                 // values that not all rows see: none may be infinite or NaN in the product.  (Those of the cells before stay as they are.)
 #pragma unroll 1
                 for (int i = 0; i < kChunk * kUnits / 32; i++) {
-                    if (cell0 + (i * 32 + lane) / kUnits < all_see) continue;
+                    const int cell = cell0 + (i * 32 + lane) / kUnits;
                     const uint32_t at = vs + (uint32_t)(i * 32 + lane) * 16;
-                    const uint4 v = lds128(at);
-                    if (finite16<T>(v.x) && finite16<T>(v.y) && finite16<T>(v.z) && finite16<T>(v.w)) continue;
-                    odd = true;
-                    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-                    uint32_t out[4];
-#pragma unroll
-                    for (int j = 0; j < 4; j++) out[j] = (finite16<T>(in[j] & 0xffffu) ? in[j] & 0xffffu : 0u) | (finite16<T>(in[j] & 0xffff0000u) ? in[j] & 0xffff0000u : 0u);
-                    sts128(at, make_uint4(out[0], out[1], out[2], out[3]));
+                    uint4 v = lds128(at);
+                    const bool mine = cell >= all_see && take_out<T>(v);
+                    if (mine) sts128(at, v);
+                    odd |= note_odd<kUnits>(odd_cells, mine, cell - all_see);
                 }
                 __syncwarp();
             }
@@ -326,17 +325,21 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
                 }
             }
         }
-        if (__any_sync(0xffffffffu, odd)) {
+        if (odd) {
             __syncwarp();
+            const int per_row = (a.head_dim + 31) / 32;
 #pragma unroll 1
-            for (int i = lane; i < rows * a.head_dim; i += 32) {
-                const int r = i / a.head_dim, d = i - r * a.head_dim, n = w.tile * kRows + r, tok = n / a.share;
-                const float x = spoilt_value<T>(a, w.s, w.b, w.head, tok, d, t0 * kChunk, t1 * kChunk);
-                if (x == 0.0f) continue;
-                T& out = static_cast<T*>(a.out)[(long long)(w.s.row0 + tok) * a.out_token + (w.head * a.share + n - tok * a.share) * a.out_head + d];
-                if (whole) out = (T)((float)out + x);        // (cells that all rows see may have left an infinity there)
-                else part[r * DP + d] += x;
+            for (int i = lane; i < rows * per_row; i += 32) {
+                const int r = i / per_row, n = w.tile * kRows + r, tok = n / a.share;
+                T* out = static_cast<T*>(a.out) + (long long)(w.s.row0 + tok) * a.out_token + (w.head * a.share + n - tok * a.share) * a.out_head;
+                give_back<T>(a, w.s, w.b, w.head, tok, all_see, odd_cells, i % per_row * 32, [&](int d, float x) {
+                    if (whole) out[d] = (T)((float)out[d] + x);              // (cells that all rows see may have left an infinity there)
+                    else part[r * DP + d] += x;
+                });
             }
+            __syncwarp();
+            odd_cells[lane] = 0;
+            __syncwarp();
         }
         if (!whole && t0 > 0) {
             flag |= t1 == w.tiles ? kContinues | kEnds : kContinues;

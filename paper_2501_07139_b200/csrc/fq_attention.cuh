@@ -9,6 +9,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <cmath>
 #include <type_traits>
 
 #include "fq_internal.cuh"
@@ -276,21 +277,70 @@ template <class T> __device__ __forceinline__ bool finite16(uint32_t two);      
 template <> __device__ __forceinline__ bool finite16<__nv_bfloat16>(uint32_t v) { return (v & 0x7f80u) != 0x7f80u && (v & 0x7f800000u) != 0x7f800000u; }
 template <> __device__ __forceinline__ bool finite16<__half>(uint32_t v) { return (v & 0x7c00u) != 0x7c00u && (v & 0x7c000000u) != 0x7c000000u; }
 
-// Infinities and NaNs among the values of new tokens are taken out before the product, where a weight of 0 would spread them to rows that do not
-// see them; this says what they add to value d of a row that does see them (0: nothing), cells [cell0, cell1).  Units that had any come here, once their
-// values are written.
+// Infinities and NaNs among values that not all rows of a unit see are taken out before the product, where a weight of 0 would spread them to rows that do
+// not see them.  The cells that had any are noted, a bit each, from the first cell on that not all rows see; once a unit's values are written, a row gets
+// back what is in those that it sees.  (Tree bits reach kOddCells new tokens; without them a unit ends, with its last row and key tile, well before
+// that.  Looking through all new cells instead took 10 ms for one infinity among 2000 new tokens of 4 heads, which take 43 us without it.)
+constexpr int kOddWords = 2 * FQ_MAX_TREE_WORDS, kOddCells = 32 * kOddWords;
+
+// Zeros in place of infinities and NaNs; true if there were any.
 template <class T>
-__device__ __forceinline__ float spoilt_value(const AttnArgs& a, const Seq& s, int b, int head, int t, int d, int cell0, int cell1)
+__device__ __forceinline__ bool take_out(uint4& v)
 {
-    float sum = 0.0f;
-    for (int cell = max(cell0, s.ctx); cell < min(cell1, s.len); cell++) {
-        if (!sees(a, s, t, s.row0 + t, cell)) continue;
-        const long long place = cell_place(a, b, cell);
-        if (place < 0) continue;
-        const float v = (float)static_cast<const T*>(a.v)[place + head * a.head_stride + d];
-        if (!isfinite(v)) sum += v;
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        any |= !finite16<T>(w[j]);
+        w[j] = (finite16<T>(w[j] & 0xffffu) ? w[j] & 0xffffu : 0u) | (finite16<T>(w[j] & 0xffff0000u) ? w[j] & 0xffff0000u : 0u);
     }
-    return sum;
+    v = make_uint4(w[0], w[1], w[2], w[3]);
+    return any;
+}
+// All lanes: `mine`: this lane's piece had some.  UNITS lanes in a row hold a cell's pieces: cell `nth` from the first one that is noted on.
+template <int UNITS>
+__device__ __forceinline__ bool note_odd(uint32_t* words, bool mine, int nth)
+{
+    const uint32_t who = __ballot_sync(0xffffffffu, mine), lane = threadIdx.x & 31;
+    if (lane % UNITS == 0 && (who >> lane & (UNITS == 32 ? 0xffffffffu : (1u << (UNITS & 31)) - 1)) && nth < kOddCells) atomicOr(words + (nth >> 5), 1u << (nth & 31));
+    return who != 0;
+}
+// What the noted cells, from cell `first` on, add to values d0 .. d0 + 31 of new token t: add(d, infinity or NaN).
+template <class T, class Add>
+__device__ __forceinline__ void give_back(const AttnArgs& a, const Seq& s, int b, int head, int t, int first, const volatile uint32_t* words, int d0, Add add)
+{
+    const int there = min(32, a.head_dim - d0);
+    const uint32_t all = there == 32 ? 0xffffffffu : (1u << there) - 1;
+    uint32_t up = 0, down = 0;                   // +inf or NaN, -inf or NaN: both are a NaN, which nothing changes any more
+#pragma unroll 1
+    for (int i = 0; i < kOddWords; i++) {
+#pragma unroll 1
+        for (uint32_t left = words[i]; left && (up & down) != all; left &= left - 1) {
+            const int cell = first + i * 32 + __ffs((int)left) - 1;
+            if (!sees(a, s, t, s.row0 + t, cell)) continue;
+            const long long place = cell_place(a, b, cell);
+            if (place < 0) continue;
+            const T* v = static_cast<const T*>(a.v) + place + head * a.head_stride + d0;
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                if (8 * u >= there) break;
+                const uint4 x = *reinterpret_cast<const uint4*>(v + 8 * u);
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const uint32_t h = w[e / 2] >> 16 * (e & 1) & 0xffffu;
+                    if (finite16<T>(h)) continue;
+                    const bool nan = h & (std::is_same<T, __half>::value ? 0x3ffu : 0x7fu), minus = h & 0x8000u;
+                    up |= (uint32_t)(nan || !minus) << (8 * u + e);
+                    down |= (uint32_t)(nan || minus) << (8 * u + e);
+                }
+            }
+        }
+    }
+    for (uint32_t left = up | down; left; left &= left - 1) {
+        const int d = __ffs((int)left) - 1;
+        add(d0 + d, (up & down) >> d & 1 ? NAN : up >> d & 1 ? INFINITY : -INFINITY);
+    }
 }
 
 // rows: 128 or 256 to a unit; dp: head_dim rounded up to 64, 128 or 256 (128 rows alone)

@@ -40,9 +40,12 @@ struct TcShape {
     // full[slots] empty[slots] raw[slots] q_full q_empty s_full[4] p_full[4] pv_done[2] unit_full[2] unit_empty[2]
     static constexpr int kBars = 3 * kSlots + 16;
     static constexpr int oSums = oBars + kBars * 8;
-    static constexpr int oMisc = oSums + (kWarps + 3) * 8;                   // TMEM address, abort flag, spoilt[8]
-    static constexpr int oUnits = (oMisc + 40 + 15) / 16 * 16;               // Unit [2]
-    static constexpr int kTotal = oUnits + 2 * 64 + 1024;                    // (tiles start at a multiple of 1024)
+    // Units whose noted cells are kept: the warp that notes them is no more than two ahead of those that give them back.
+    static constexpr int kOddUnits = 4;
+    static constexpr int oMisc = oSums + (kWarps + 3) * 8;                   // TMEM address, abort flag, spoilt[kOddUnits]
+    static constexpr int oUnits = (oMisc + 8 + kOddUnits * 4 + 15) / 16 * 16;             // Unit [2]
+    static constexpr int oOdd = oUnits + 2 * 64;                             // bits [kOddUnits][kOddWords]
+    static constexpr int kTotal = oOdd + kOddUnits * kOddWords * 4 + 1024;   // (tiles start at a multiple of 1024)
     static constexpr int kTmemS = 0;                                         // scores of the query tiles, then their values
     static constexpr int kTmemO = kBufs * NQ * kKeys;
     static_assert(kTmemO + NQ * DP <= 512, "TMEM columns");
@@ -249,12 +252,13 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::oMisc + 4);
     volatile int* spoilt = reinterpret_cast<volatile int*>(smem + S::oMisc + 8);
     Unit* units = reinterpret_cast<Unit*>(smem + S::oUnits);
+    const auto odd_cells = [&](int unit) { return reinterpret_cast<uint32_t*>(smem + S::oOdd) + unit % S::kOddUnits * kOddWords; };
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");              // (the joining kernel waits for this one's end)
     if (tid == 0) {
         AttnJoin none{};
         a.joins[blockIdx.x] = none;
         *abort_flag = 0;
-        for (int i = 0; i < 8; i++) spoilt[i] = -1;
+        for (int i = 0; i < S::kOddUnits; i++) spoilt[i] = -1;
         for (int i = 0; i < S::kSlots; i++) {
             mbar_init(full(i), 1);
             mbar_init(empty(i), 1);
@@ -417,7 +421,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 o_turn ^= 1;
                 tc_after();
             }
-            const bool whole = u.whole, odd = spoilt[unit & 7] == unit;
+            const bool whole = u.whole, odd = spoilt[unit % S::kOddUnits] == unit;
             const float by = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
             const int h = u.head * a.share + n % a.share;
             T* out = static_cast<T*>(a.out) + row * a.out_token + h * a.out_head;
@@ -445,13 +449,13 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 __syncwarp();                    // (the next load is the whole warp's)
             }
             if (odd && real) {
+                const int first = a.mask ? s.ctx : s.ctx + u.tile * S::kRows / a.share + 1;          // (of the unit, not of its query tile)
 #pragma unroll 1
-                for (int d = 0; d < a.head_dim; d++) {
-                    const float x = spoilt_value<T>(a, s, u.b, u.head, t, d, t0 * S::kKeys, u.t1 * S::kKeys);
-                    if (x == 0.0f) continue;
-                    if (whole) out[d] = (T)((float)out[d] + x);      // (cells that all rows see may have left an infinity there)
-                    else part[(d / 4 * S::kRows + q * 128 + r) * 4 + d % 4] += x;
-                }
+                for (int d0 = 0; d0 < a.head_dim; d0 += 32)
+                    give_back<T>(a, s, u.b, u.head, t, first, odd_cells(unit), d0, [&](int d, float x) {
+                        if (whole) out[d] = (T)((float)out[d] + x);          // (cells that all rows see may have left an infinity there)
+                        else part[(d / 4 * S::kRows + q * 128 + r) * 4 + d % 4] += x;
+                    });
             }
             const float top = m * a.scale;       // (-inf stays)
             if (!whole) {
@@ -529,6 +533,8 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 if (lane == 0) mbar_arrive(q_full);
             }
             const int all_see = a.mask ? w.s.ctx : w.s.ctx + w.tile * S::kRows / a.share + 1;
+            odd_cells(unit)[lane] = 0;
+            __syncwarp();
             for (int tile = max(t0, all_see / S::kKeys); tile < t1; tile++) {
                 const int slot = (pos + 2 * (tile - t0) + 1) % S::kSlots;
                 if (!wait(raw(slot), raw_phase >> slot & 1)) break;
@@ -549,22 +555,19 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     }
 #pragma unroll
                     for (int i = 0; i < 8; i++) Pair<T>::take(most, v[i]);
-                    if (Pair<T>::finite(most)) continue;
+                    if (__all_sync(0xffffffffu, Pair<T>::finite(most))) continue;
                     odd = true;
 #pragma unroll 1
                     for (int i = 0; i < 8; i++) {
-                        const int n = i * 32 + lane;
-                        const uint32_t at = piece(min(r0 + n / kUnits, there - 1), n % kUnits);
-                        const uint4 y = lds128(at);
-                        const uint32_t in[4] = {y.x, y.y, y.z, y.w};
-                        uint32_t out[4];
-#pragma unroll
-                        for (int j = 0; j < 4; j++)
-                            out[j] = (finite16<T>(in[j] & 0xffffu) ? in[j] & 0xffffu : 0u) | (finite16<T>(in[j] & 0xffff0000u) ? in[j] & 0xffff0000u : 0u);
-                        sts128(at, make_uint4(out[0], out[1], out[2], out[3]));
+                        const int n = i * 32 + lane, r = min(r0 + n / kUnits, there - 1);
+                        const uint32_t at = piece(r, n % kUnits);
+                        uint4 y = lds128(at);
+                        const bool mine = take_out<T>(y);
+                        if (mine) sts128(at, y);
+                        note_odd<kUnits>(odd_cells(unit), mine, tile * S::kKeys + r - all_see);
                     }
                 }
-                if (odd) spoilt[unit & 7] = unit;
+                if (odd) spoilt[unit % S::kOddUnits] = unit;
                 to_async_proxy();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(full(slot));

@@ -1,10 +1,11 @@
-"""What lies in cells that no token uses costs no time."""
+"""What lies in cells that no token uses, and infinities or NaNs among the values of a prompt, cost no time."""
 import math
 
 import pytest
 import torch
 
 from test_gpu_attention import call, make
+from test_gpu_attention_odd_values import agree, defined, spoil
 
 pytestmark = pytest.mark.gpu
 
@@ -59,3 +60,49 @@ def test_unused_cells(fq, ctx, new, heads, kv, dim, block, tree):
         assert torch.equal(a, b)
     assert least_us(fq, nans) <= 2 * least_us(fq, zeros) + 10
     assert fq.fq_status() == 0
+
+
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+@pytest.mark.parametrize("hint", [1, 100, 2000])
+def test_one_value_of_a_prompt(fq, value, hint):
+    """One infinity, or NaN, among 2000 new tokens of 4 heads: twice the time is enough."""
+    s = make([0], [2000], 4, 4, 128, 64, torch.bfloat16)
+    clean, _ = call(fq, s, new=hint)
+    for cell in (0, 700, 1990):
+        hits = [(0, cell, 5, value)]
+        t = spoil(s, hits)
+        got, _ = call(fq, t, new=hint)
+        agree(defined(t), clean, got)
+        assert least_us(fq, t, new=hint) <= 2 * least_us(fq, s, new=hint) + 10
+    assert fq.fq_status() == 0
+
+
+@pytest.mark.parametrize("hint", [1, 100, 2000])
+def test_a_prompt_of_nans(fq, hint):
+    """Every value is a NaN, as a model's are that has overflowed.  A unit's cells are all noted and every row but its first sees one: some 50 thousand cycles for a unit that
+    takes 10 to 30 thousand without."""
+    s = make([0], [2000], 4, 4, 128, 64, torch.bfloat16)
+    t = dict(s, v=torch.full_like(s["v"], math.nan))
+    got, lse = call(fq, t, new=hint)
+    assert bool(got[:2000].isnan().all()) and torch.equal(lse, call(fq, s, new=hint)[1])
+    assert least_us(fq, t, new=hint) <= 8 * least_us(fq, s, new=hint) + 10
+    assert fq.fq_status() == 0
+
+
+@pytest.mark.parametrize("dt,tree,value", [(torch.bfloat16, False, math.inf), (torch.float16, False, math.nan), (torch.bfloat16, True, -math.inf)])
+def test_one_value_of_many(fq, dt, tree, value):
+    """100 thousand new tokens, or a tree of a thousand: within the limits of the waits, and no other row changes."""
+    new = 1000 if tree else 100000
+    s = make([30], [new], 1, 1, 64, 64, dt, tree, words=16)
+    clean, _ = call(fq, s)
+    nth, d = new // 3, 11
+    cell = 30 + nth
+    got, _ = call(fq, spoil(s, [(0, cell, d, value)]))
+    assert fq.fq_status() == 0
+    rows = torch.arange(new, device="cuda")
+    sees = (s["mask"][:new, nth // 64] >> (nth % 64) & 1).bool() if tree else rows >= nth
+    changed = got.clone()
+    changed[:new][sees, 0, d] = clean[:new][sees, 0, d]
+    assert torch.equal(changed, clean)
+    left = got[:new][sees, 0, d].double()
+    assert bool(sees.any()) and bool((left.isnan() if math.isnan(value) else (left == value) | left.isnan()).all())
