@@ -429,7 +429,8 @@ int fq_cache_step(fq_ctx* ctx, const fq_cache_step_args* args, void* stream);
 /* The accepted branch of every sequence's drafted tokens is moved together, in n_caches caches (keys or values of a layer each): the key or value of new token
  * kept[b][i] goes to cell before + i, where `before` = lens[b] less the sequence's new tokens, for i < n_kept[b].  kept[b][0 .. n_kept) rises
  * and names new tokens of the sequence; else (FQ_ERR_INDEX) nothing of that sequence moves and keep is `before`.
- *   caches_host   host array of n_caches device pointers, each a cache as in fq_cache (dtype, strides and sizes are those of all)
+ *   caches_host   host array of n_caches device pointers, each a cache as in fq_cache (dtype, strides and sizes are those of all), none of them twice
+ *                 (FQ_ERR_ARG) or overlapping another
  *   kept_dev      int [n_seqs][ld_kept >= max_kept], n_kept_dev int [n_seqs];  1 <= max_kept <= 1024
  *   keep_dev      int [n_seqs]                before + n_kept: what fq_cache_step is to keep next (written) */
 typedef struct fq_cache_move_args {

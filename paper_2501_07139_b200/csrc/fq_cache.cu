@@ -5,7 +5,10 @@
 // it: every CTA forms the sums for itself, each phase's writes are dealt to all of them, and a cluster barrier stands between phases.  The rows of
 // a large batch, which depend on nothing but the new tables, are a kernel of their own over all SMs (150 thousand rows, 300 sequences: 41 us by the
 // cluster).
-#include <atomic>
+#include <algorithm>
+#include <functional>
+#include <memory>
+#include <new>
 
 #include "fq_cluster.cuh"
 #include "fq_internal.cuh"
@@ -292,6 +295,19 @@ __global__ void __launch_bounds__(kMoveThreads) cache_move_kernel(const __grid_c
     }
 }
 
+// Is an address among them twice?  -1: no memory to find out.  (64 of them: under a microsecond.)
+int any_twice(void* const* p, int n)
+{
+    constexpr int kHere = 256;
+    const void* here[kHere];
+    std::unique_ptr<const void*[]> more(n > kHere ? new (std::nothrow) const void*[n] : nullptr);
+    if (n > kHere && !more) return -1;
+    const void** all = n > kHere ? more.get() : here;
+    std::copy(p, p + n, all);
+    std::sort(all, all + n, std::less<const void*>());
+    return std::adjacent_find(all, all + n) != all + n;
+}
+
 }  // namespace
 
 int check_table(const int* table, long long ld, int n_seqs, int max_blocks, int block_size)
@@ -368,6 +384,8 @@ int fq_cache_move(fq_ctx* ctx, const fq_cache_move_args* args, void* stream)
     if (rc != FQ_OK) return rc;
     if (!aligned(x.starts_dev, 4) || !aligned(x.lens_dev, 4) || !aligned(x.kept_dev, 4) || !aligned(x.n_kept_dev, 4) || !aligned(x.keep_dev, 4))
         return FQ_ERR_ALIGN;
+    const int twice = any_twice(x.caches_host, n_caches);
+    if (twice) return twice < 0 ? FQ_ERR_CUDA : FQ_ERR_ARG;
     const fq_cache* layout = &x.layout;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;

@@ -624,7 +624,7 @@ class FlexQ:
     def fq_cache_move(self, caches: Sequence[torch.Tensor], table: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor, kept: torch.Tensor,
                       n_kept: torch.Tensor):
         """Moves the accepted branch of every sequence's new tokens together, in all `caches` (keys and values of all layers, [blocks][block size][heads][values] each, of
-        one shape and type): new token kept[b][i] goes to the i-th cell behind what was cached before, i < n_kept[b].  kept int32 [n][most], rising.
+        one shape and type, none twice): new token kept[b][i] goes to the i-th cell behind what was cached before, i < n_kept[b].  kept int32 [n][most], rising.
         -> keep int32 [n], what fq_cache_step is to keep."""
         caches = list(caches)
         if not caches:
