@@ -432,7 +432,7 @@ int fq_cache_step(fq_ctx* ctx, const fq_cache_step_args* args, void* stream);
  *   caches_host   host array of n_caches device pointers, each a cache as in fq_cache (dtype, strides and sizes are those of all), none of them twice
  *                 (FQ_ERR_ARG) or overlapping another
  *   kept_dev      int [n_seqs][ld_kept >= max_kept], n_kept_dev int [n_seqs];  1 <= max_kept <= 1024
- *   keep_dev      int [n_seqs]                before + n_kept: what fq_cache_step is to keep next (written) */
+ *   keep_dev      int [n_seqs]                before + n_kept: what fq_cache_step is to keep next (written); memory of its own, not lens_dev (FQ_ERR_ARG) */
 typedef struct fq_cache_move_args {
     void* const* caches_host;
     fq_cache layout;            /* k_dev and v_dev are not looked at */

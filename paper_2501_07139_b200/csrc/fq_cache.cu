@@ -384,6 +384,8 @@ int fq_cache_move(fq_ctx* ctx, const fq_cache_move_args* args, void* stream)
     if (rc != FQ_OK) return rc;
     if (!aligned(x.starts_dev, 4) || !aligned(x.lens_dev, 4) || !aligned(x.kept_dev, 4) || !aligned(x.n_kept_dev, 4) || !aligned(x.keep_dev, 4))
         return FQ_ERR_ALIGN;
+    for (const int* read : {x.starts_dev, x.lens_dev, x.kept_dev, x.n_kept_dev, x.table_dev})    // (while other CTAs write keep)
+        if (read == x.keep_dev) return FQ_ERR_ARG;
     const int twice = any_twice(x.caches_host, n_caches);
     if (twice) return twice < 0 ? FQ_ERR_CUDA : FQ_ERR_ARG;
     const fq_cache* layout = &x.layout;

@@ -51,3 +51,11 @@ def test_a_cache_moved_twice(n, first, second):
     pointers = [far((i * 7919) % n) for i in range(n)]
     pointers[second] = pointers[first]
     assert code("fq_cache_move", apart(MOVE), pointers) == ARG
+
+
+@pytest.mark.parametrize("field", ["lens", "n_kept", "starts", "kept", "table"])
+def test_what_is_kept_has_its_own_memory(field):
+    """Other parts of the call read these while keep is written."""
+    args = apart(MOVE)
+    args["keep"] = args[field]
+    assert code("fq_cache_move", args, [far(0), far(1)]) == ARG
