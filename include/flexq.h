@@ -489,7 +489,7 @@ int fq_rotary_cache(fq_ctx* ctx, const fq_rotary_cache_args* args, void* stream)
  * Query heads share key heads in groups: head h uses key head h / (q heads / cache heads).  A token sees all cells before the new ones and, of the new ones,
  * those of its bits in mask_dev; with mask_dev NULL those up to itself (single tokens, drafted chains, prompts).  A row that sees nothing: out 0,
  * lse -inf; a score of -inf counts as a cell that it does not see.  What a row does not see does not touch it, an infinity or a NaN in it neither; one that it sees makes its values infinite or NaN.
- *   q, out        dtype fp16 or bf16, [tokens][q heads][head_dim]; 16-byte aligned, strides multiples of 8; out may not overlap q
+ *   q, out        dtype fp16 or bf16, [tokens][q heads][head_dim]; 16-byte aligned, strides multiples of 8; out may not overlap q (at the same address: FQ_ERR_ARG)
  *   cache         of the same dtype
  *   starts_dev    int [n_seqs + 1]: rows of the sequences' new tokens (may be none); rows behind the last are left as they are
  *   lens_dev      int [n_seqs]: tokens in the cache, the new ones among them

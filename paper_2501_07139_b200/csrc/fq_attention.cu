@@ -512,6 +512,7 @@ int fq_tree_attention(fq_ctx* ctx, const fq_attention_args* args, void* stream)
         !aligned(x.mask_dev, 8) || !aligned(x.lse_dev, 4) || (many && (q.token_stride % 8 || out.token_stride % 8)) ||
         (wide && (q.head_stride % 8 || out.head_stride % 8)))
         return FQ_ERR_ALIGN;
+    if (out.dev == q.dev) return FQ_ERR_ARG;     // (several CTAs read a unit's queries)
     if (x.scratch_bytes < fq_tree_attention_scratch(ctx, x.n_seqs, x.tokens, q.heads, cache.heads, x.head_dim, x.new_tokens)) return FQ_ERR_SCRATCH;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return FQ_ERR_CUDA;

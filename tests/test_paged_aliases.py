@@ -59,3 +59,10 @@ def test_what_is_kept_has_its_own_memory(field):
     args = apart(MOVE)
     args["keep"] = args[field]
     assert code("fq_cache_move", args, [far(0), far(1)]) == ARG
+
+
+def test_outputs_in_place_of_queries():
+    """A unit's queries are read by several CTAs, which write as they end."""
+    args = apart(ATTENTION)
+    args["out"]["dev"] = args["q"]["dev"]
+    assert code("fq_tree_attention", args) == ARG
