@@ -458,7 +458,7 @@ int fq_rotary_table(int rot_dim, double base, double factor, int context, double
 /* Rotary positions.  Of every head the first rot_dim values are turned in pairs (x_i, x_{i + rot_dim/2}), or (x_2i, x_{2i+1}) if `interleaved`:
  *   y = magnitude (x cos a - x' sin a),   y' = magnitude (x sin a + x' cos a),   a = angle of pair i at the token's position;
  * the others are copied.  `inverse` turns the other way, which with the same magnitude is the gradient.  fp32 arithmetic, one rounding.
- *   x, y          n (1 or 2) tensors and where they go; y[i] may be x[i] itself, with the same strides
+ *   x, y          n (1 or 2) tensors and where they go; y[i] may be x[i] itself, with the same strides, and overlaps nothing else (the other x or y: FQ_ERR_ARG)
  *   positions_dev int32 or int64 [tokens] (id_bytes 4 or 8)
  *   turns_dev     uint64 [rot_dim / 2], 8-byte aligned, from fq_rotary_table
  * rot_dim even, 2 <= rot_dim <= head_dim <= 1024; 1 <= tokens <= FQ_MAX_ROWS; up to 1024 heads; any alignment to the type. */
@@ -471,8 +471,9 @@ typedef struct fq_rotary_args {
 } fq_rotary_args;
 int fq_rotary(fq_ctx* ctx, const fq_rotary_args* args, void* stream);
 
-/* The same in a serving step: q is turned into q_out (may be q), k is turned and stored with v in the layer's cache, at slots_dev int64 [tokens].  Tokens with a
- * negative slot are not stored; nor are those with a slot outside the cache (FQ_ERR_INDEX).  No two tokens may have the same slot. */
+/* The same in a serving step: q is turned into q_out (may be q, not k or v: FQ_ERR_ARG), k is turned and stored with v in the layer's caches (two of them:
+ * FQ_ERR_ARG), at slots_dev int64 [tokens].  Tokens with a negative slot are not stored; nor are those with a slot outside the cache (FQ_ERR_INDEX).  No two tokens
+ * may have the same slot. */
 typedef struct fq_rotary_cache_args {
     fq_heads q, q_out, k, v;
     fq_cache cache;

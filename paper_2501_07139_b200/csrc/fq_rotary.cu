@@ -311,6 +311,8 @@ int fq_rotary(fq_ctx* ctx, const fq_rotary_args* args, void* stream)
         if (rc != FQ_OK) return rc;
         a.t[i] = tensor(x.x + i, x.y + i, x.tokens, x.rot_dim);
     }
+    // one tensor's output is neither the other's output nor its source
+    if (x.n == 2 && (x.y[0].dev == x.y[1].dev || x.y[0].dev == x.x[1].dev || x.y[1].dev == x.x[0].dev)) return FQ_ERR_ARG;
     a.n = x.n; a.head_dim = x.head_dim; a.half = x.rot_dim / 2;
     a.positions = x.positions_dev; a.wide_positions = x.id_bytes == 8; a.turns = x.turns_dev;
     a.magnitude = x.magnitude; a.side = x.inverse ? -1.0f : 1.0f; a.status = ctx->status_dev;
@@ -330,6 +332,7 @@ int fq_rotary_cache(fq_ctx* ctx, const fq_rotary_cache_args* args, void* stream)
     if (!x.slots_dev) return FQ_ERR_ARG;
     if (x.k.heads != x.cache.heads || x.v.heads != x.cache.heads) return FQ_ERR_SHAPE;
     if (!aligned(x.slots_dev, 8)) return FQ_ERR_ALIGN;
+    if (x.q_out.dev == x.k.dev || x.q_out.dev == x.v.dev || x.cache.k_dev == x.cache.v_dev) return FQ_ERR_ARG;
     RotaryArgs a{};
     a.t[0] = tensor(&x.q, &x.q_out, x.tokens, x.rot_dim);
     a.t[1] = to_cache(&x.k, &x.cache, x.tokens, x.rot_dim);

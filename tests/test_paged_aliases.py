@@ -66,3 +66,21 @@ def test_outputs_in_place_of_queries():
     args = apart(ATTENTION)
     args["out"]["dev"] = args["q"]["dev"]
     assert code("fq_tree_attention", args) == ARG
+
+
+@pytest.mark.parametrize("output,other", [("y", "y1"), ("y", "x1"), ("y1", "x")])
+def test_turned_tensors_have_their_own_memory(output, other):
+    """In place is cell for cell: one tensor's output is not the other's output or source."""
+    args = apart(ROTARY)
+    args[output]["dev"] = args[other]["dev"]
+    assert code("fq_rotary", args) == ARG
+
+
+@pytest.mark.parametrize("other", ["k", "v", "caches"])
+def test_a_step_stores_to_memory_of_its_own(other):
+    args = apart(STORE)
+    if other == "caches":
+        args["cache"]["k_dev"] = args["cache"]["v_dev"]
+    else:
+        args["q_out"]["dev"] = args[other]["dev"]
+    assert code("fq_rotary_cache", args) == ARG
