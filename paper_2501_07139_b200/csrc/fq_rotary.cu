@@ -30,7 +30,6 @@ struct RotaryArgs {
     Tensor t[kMaxTensors];
     int n, items;                        // pieces of a token, all tensors
     int head_dim, half;                  // half: rot_dim / 2
-    int per_cta;                         // items of a CTA
     const void* positions;
     int wide_positions;
     const uint64_t* turns;
