@@ -327,16 +327,12 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
         }
         if (odd) {
             __syncwarp();
-            const int per_row = (a.head_dim + 31) / 32;
-#pragma unroll 1
-            for (int i = lane; i < rows * per_row; i += 32) {
-                const int r = i / per_row, n = w.tile * kRows + r, tok = n / a.share;
-                T* out = static_cast<T*>(a.out) + (long long)(w.s.row0 + tok) * a.out_token + (w.head * a.share + n - tok * a.share) * a.out_head;
-                give_back<T>(a, w.s, w.b, w.head, tok, all_see, odd_cells, i % per_row * 32, [&](int d, float x) {
-                    if (whole) out[d] = (T)((float)out[d] + x);              // (cells that all rows see may have left an infinity there)
-                    else part[r * DP + d] += x;
-                });
-            }
+            const int r = min(lane, rows - 1), n = w.tile * kRows + r, tok = n / a.share;
+            T* out = static_cast<T*>(a.out) + (long long)(w.s.row0 + tok) * a.out_token + (w.head * a.share + n - tok * a.share) * a.out_head;
+            give_back<T>(a, w.s, w.b, w.head, tok, lane < rows, all_see, odd_cells, [&](int d, float x) {
+                if (whole) out[d] = (T)((float)out[d] + x);                  // (cells that all rows see may have left an infinity there)
+                else part[r * DP + d] += x;
+            });
             __syncwarp();
             odd_cells[lane] = 0;
             __syncwarp();

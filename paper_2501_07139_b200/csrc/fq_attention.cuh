@@ -262,6 +262,26 @@ __device__ __forceinline__ bool sees(const AttnArgs& a, const Seq& s, int t, int
     return (nth >> 6) < a.words && (a.mask[(long long)row * a.words + (nth >> 6)] >> (nth & 63) & 1);
 }
 
+// Which of the cells cell0 .. + 31 a new token sees.
+__device__ __forceinline__ uint32_t seen32(const AttnArgs& a, const Seq& s, int t, int row, int cell0)
+{
+    const int left = s.len - cell0;
+    uint32_t in = left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1;
+    const int nth = cell0 - s.ctx;               // new token of the first
+    if (nth <= -32) return in;
+    if (!a.mask) {
+        const int n = t + 1 - nth;               // cells seen from the first on
+        return in & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1);
+    }
+    const uint64_t* bits = a.mask + (long long)row * a.words;
+    const int from = max(nth, 0), w = from >> 6, shift = from & 63;
+    uint64_t v = w < a.words ? bits[w] >> shift : 0;
+    if (shift > 32 && w + 1 < a.words) v |= bits[w + 1] << (64 - shift);
+    uint32_t b = (uint32_t)v;
+    if (nth < 0) b = b << -nth | ((1u << -nth) - 1);
+    return in & b;
+}
+
 // Offset (in values) of a cell's row in the cache, or -1 (recorded) where its block is not one.
 __device__ __forceinline__ long long cell_place(const AttnArgs& a, int b, int cell)
 {
@@ -305,41 +325,57 @@ __device__ __forceinline__ bool note_odd(uint32_t* words, bool mine, int nth)
     if (lane % UNITS == 0 && (who >> lane & (UNITS == 32 ? 0xffffffffu : (1u << (UNITS & 31)) - 1)) && nth < kOddCells) atomicOr(words + (nth >> 5), 1u << (nth & 31));
     return who != 0;
 }
-// What the noted cells, from cell `first` on, add to values d0 .. d0 + 31 of new token t: add(d, infinity or NaN).
+// What the noted cells, from cell `first` on, add to the values of new token t, a lane's row (`real`: it has one): add(d, infinity or NaN).  A lane looks
+// through 32 values of a cell and hands what it finds to the lanes whose row sees that cell, so that 32 cells are on their way at a time.  (Each lane by itself, cell after cell: prompts
+// of up to 2048 tokens of which one value in each head is infinite took 6.8 ms, those of NaNs 1.4.)
 template <class T, class Add>
-__device__ __forceinline__ void give_back(const AttnArgs& a, const Seq& s, int b, int head, int t, int first, const volatile uint32_t* words, int d0, Add add)
+__device__ __forceinline__ void give_back(const AttnArgs& a, const Seq& s, int b, int head, int t, bool real, int first, const volatile uint32_t* words, Add add)
 {
-    const int there = min(32, a.head_dim - d0);
-    const uint32_t all = there == 32 ? 0xffffffffu : (1u << there) - 1;
-    uint32_t up = 0, down = 0;                   // +inf or NaN, -inf or NaN: both are a NaN, which nothing changes any more
+    const int lane = threadIdx.x & 31;
 #pragma unroll 1
-    for (int i = 0; i < kOddWords; i++) {
+    for (int d0 = 0; d0 < a.head_dim; d0 += 32) {
+        const int there = min(32, a.head_dim - d0);
+        const uint32_t all = there == 32 ? 0xffffffffu : (1u << there) - 1;
+        uint32_t up = 0, down = 0;               // +inf or NaN, -inf or NaN: both are a NaN, which nothing changes any more
 #pragma unroll 1
-        for (uint32_t left = words[i]; left && (up & down) != all; left &= left - 1) {
-            const int cell = first + i * 32 + __ffs((int)left) - 1;
-            if (!sees(a, s, t, s.row0 + t, cell)) continue;
-            const long long place = cell_place(a, b, cell);
-            if (place < 0) continue;
-            const T* v = static_cast<const T*>(a.v) + place + head * a.head_stride + d0;
+        for (int i = 0; i < kOddWords; i++) {
+            const uint32_t noted = __shfl_sync(0xffffffffu, words[i], 0);
+            if (!noted) continue;
+            const uint32_t seen = real && (up & down) != all ? noted & seen32(a, s, t, s.row0 + t, first + i * 32) : 0;
+            if (!__any_sync(0xffffffffu, seen != 0)) continue;
+            uint32_t here_up = 0, here_down = 0;
+            const long long place = noted >> lane & 1 ? cell_place(a, b, first + i * 32 + lane) : -1;
+            if (place >= 0) {
+                const T* v = static_cast<const T*>(a.v) + place + head * a.head_stride + d0;
+                uint4 x[4];
 #pragma unroll
-            for (int u = 0; u < 4; u++) {
-                if (8 * u >= there) break;
-                const uint4 x = *reinterpret_cast<const uint4*>(v + 8 * u);
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                for (int u = 0; u < 4; u++) x[u] = 8 * u < there ? *reinterpret_cast<const uint4*>(v + 8 * u) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    const uint32_t h = w[e / 2] >> 16 * (e & 1) & 0xffffu;
-                    if (finite16<T>(h)) continue;
-                    const bool nan = h & (std::is_same<T, __half>::value ? 0x3ffu : 0x7fu), minus = h & 0x8000u;
-                    up |= (uint32_t)(nan || !minus) << (8 * u + e);
-                    down |= (uint32_t)(nan || minus) << (8 * u + e);
+                for (int u = 0; u < 4; u++) {
+                    const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        const uint32_t h = w[e / 2] >> 16 * (e & 1) & 0xffffu;
+                        const bool odd = !finite16<T>(h), nan = h & (std::is_same<T, __half>::value ? 0x3ffu : 0x7fu), minus = h & 0x8000u;
+                        here_up |= (uint32_t)(odd && (nan || !minus)) << (8 * u + e);
+                        here_down |= (uint32_t)(odd && (nan || minus)) << (8 * u + e);
+                    }
+                }
+            }
+            for (uint32_t left = __ballot_sync(0xffffffffu, here_up | here_down); left; left &= left - 1) {
+                const int j = __ffs((int)left) - 1;
+                const uint32_t u = __shfl_sync(0xffffffffu, here_up, j), n = __shfl_sync(0xffffffffu, here_down, j);
+                if (seen >> j & 1) {
+                    up |= u;
+                    down |= n;
                 }
             }
         }
-    }
-    for (uint32_t left = up | down; left; left &= left - 1) {
-        const int d = __ffs((int)left) - 1;
-        add(d0 + d, (up & down) >> d & 1 ? NAN : up >> d & 1 ? INFINITY : -INFINITY);
+        for (uint32_t left = up | down; left; left &= left - 1) {
+            const int d = __ffs((int)left) - 1;
+            add(d0 + d, (up & down) >> d & 1 ? NAN : up >> d & 1 ? INFINITY : -INFINITY);
+        }
+        __syncwarp();
     }
 }
 

@@ -203,26 +203,6 @@ __device__ __forceinline__ int tiles_end(const AttnArgs& a, const Work& w, int q
     return max(w.t0(), min(w.t1(), key_tiles<128, KEYS>(a, w.s, w.tile * NQ + q)));
 }
 
-// Which of the cells cell0 .. + 31 a new token sees.
-__device__ __forceinline__ uint32_t seen32(const AttnArgs& a, const Seq& s, int t, int row, int cell0)
-{
-    const int left = s.len - cell0;
-    uint32_t in = left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1;
-    const int nth = cell0 - s.ctx;               // new token of the first
-    if (nth <= -32) return in;
-    if (!a.mask) {
-        const int n = t + 1 - nth;               // cells seen from the first on
-        return in & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1);
-    }
-    const uint64_t* bits = a.mask + (long long)row * a.words;
-    const int from = max(nth, 0), w = from >> 6, shift = from & 63;
-    uint64_t v = w < a.words ? bits[w] >> shift : 0;
-    if (shift > 32 && w + 1 < a.words) v |= bits[w + 1] << (64 - shift);
-    uint32_t b = (uint32_t)v;
-    if (nth < 0) b = b << -nth | ((1u << -nth) - 1);
-    return in & b;
-}
-
 // Cells lie in a cache as [block][key head][cell of the block][value], whatever their strides.
 __device__ __forceinline__ void tma_cells(uint32_t dst, const CUtensorMap* map, int value, int cell, int head, int block, uint32_t bar)
 {
@@ -448,14 +428,12 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 }
                 __syncwarp();                    // (the next load is the whole warp's)
             }
-            if (odd && real) {
+            if (__any_sync(0xffffffffu, odd)) {
                 const int first = a.mask ? s.ctx : s.ctx + u.tile * S::kRows / a.share + 1;          // (of the unit, not of its query tile)
-#pragma unroll 1
-                for (int d0 = 0; d0 < a.head_dim; d0 += 32)
-                    give_back<T>(a, s, u.b, u.head, t, first, odd_cells(unit), d0, [&](int d, float x) {
-                        if (whole) out[d] = (T)((float)out[d] + x);          // (cells that all rows see may have left an infinity there)
-                        else part[(d / 4 * S::kRows + q * 128 + r) * 4 + d % 4] += x;
-                    });
+                give_back<T>(a, s, u.b, u.head, t, real, first, odd_cells(unit), [&](int d, float x) {
+                    if (whole) out[d] = (T)((float)out[d] + x);              // (cells that all rows see may have left an infinity there)
+                    else part[(d / 4 * S::kRows + q * 128 + r) * 4 + d % 4] += x;
+                });
             }
             const float top = m * a.scale;       // (-inf stays)
             if (!whole) {
