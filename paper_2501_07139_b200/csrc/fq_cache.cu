@@ -344,7 +344,7 @@ int fq_cache_step(fq_ctx* ctx, const fq_cache_step_args* args, void* stream)
                x.parents_dev, tokens, x.starts_dev, x.slots_dev, x.positions_dev, x.mask_dev, x.words, 1, tokens <= 4096, ctx->status_dev};
     if (n_seqs > 64 || tokens > 512) a.n_cta = kMaxCluster;
     const size_t smem = 3 * sizeof(int) * (size_t)n_seqs;
-    if (smem > 48 * 1024) {
+    if (smem > 47 * 1024) {                      // (48 KB without asking, of which the kernel's own variables take a part)
         // (a setting of the kernel on this device; asking for it again costs a microsecond, and only very large batches do)
         if (cudaFuncSetAttribute(cache_step_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * (int)sizeof(int) * FQ_MAX_SEQS) != cudaSuccess ||
             cudaFuncSetAttribute(cache_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(int) * FQ_MAX_SEQS) != cudaSuccess)
