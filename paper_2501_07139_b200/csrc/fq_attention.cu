@@ -275,6 +275,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1) attention_kernel(const
                     for (int e = 0; e < 2; e++) p[n][2 * h + e] = exp2_fast(sc[n][2 * h + e] - base);
                 l[h] = l[h] * rise[h] + ((p[0][2 * h] + p[0][2 * h + 1]) + (p[1][2 * h] + p[1][2 * h + 1]));
             }
+            // (the product takes 16-bit weights: half a step of each, as much as an output's own rounding; the sum above has them in full)
             const uint32_t pf[4] = {pack2<T>(p[0][0], p[0][1]), pack2<T>(p[0][2], p[0][3]), pack2<T>(p[1][0], p[1][1]), pack2<T>(p[1][2], p[1][3])};
             const int vrow = ((lane >> 3) & 1) * 8 + (lane & 7), vunit = lane >> 4;
             const bool risen = rise[0] != 1.0f || rise[1] != 1.0f;

@@ -4,7 +4,8 @@
 //   warps 0 .. 4 NQ - 1   softmax, a thread a row: scores from TMEM, weights back into the same columns, running maximum and sum in registers; values
 //                         are rescaled only when a maximum has risen by more than a factor of 2^8 (rare behind a row's first tiles), so that nobody
 //                         waits for the product in between
-//   1 warp                says which unit is next, brings the query rows, and looks through value tiles that not all rows see for infinities and NaNs
+//   1 warp                says which unit is next, brings the query rows, looks through value tiles that not all rows see for infinities and NaNs, and clears
+//                         what lies behind a sequence's last cell
 //   2 warps               TMA, keys and values: runs of cells that lie together in a block (as many as divide both the block and the tile) into the 128-byte swizzled rows that the
 //                         tensor core reads; a ring of key and value tiles that runs ahead over units
 //   1 warp                issues tcgen05.mma: scores = Q K^T (both from shared memory), values += P V (P in TMEM, V as it lies, d contiguous)
@@ -381,7 +382,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                         const float2 e = fma2(make_float2(v[c][j], v[c][j + 1]), by, minus);
                         const float2 w2 = make_float2(exp2_fast(e.x), exp2_fast(e.y));
                         sum[j / 2 & 1] = add2(sum[j / 2 & 1], w2);
-                        p[j / 2] = pack2<T>(w2.x, w2.y);
+                        p[j / 2] = pack2<T>(w2.x, w2.y);                     // (the product takes 16-bit weights: half a step of each, as much as an output's own rounding)
                     }
                     tmem_st32(s_at + 32 * c, p); // (columns whose scores have been read)
                 }

@@ -710,8 +710,9 @@ class FlexQ:
         """Attention of every sequence's new tokens over its paged cache, whose last cells they are: q [tokens][heads][values], rows starts[b] .. starts[b + 1] of
         sequence b, caches [blocks][block size][key heads][values], table int32 [n][blocks], lens int32 [n] (the new tokens counted).  A token sees what was cached
         before and, of the new tokens, those of its bits in `mask` int64 [tokens][words] (from fq_cache_step), or those up to itself.  `scale`:
-        values^-1/2 if not given.  `new`: how many new tokens a sequence has, about (tokens / n if not given).  Log-sum-exps go to `lse` fp32
-        [tokens][heads] if it is given.  -> out, new if not given; rows behind the last new token are left as they are."""
+        values^-1/2 if not given.  `new`: how many new tokens a sequence has, about (tokens / n if not given); rows are dealt for that many, so that many single
+        tokens and a long prompt are faster in a call each.  Log-sum-exps go to `lse` fp32 [tokens][heads] if it is given.  10 to 39 MB of scratch are taken from
+        torch's allocator for the call.  -> out, new if not given (not q); rows behind the last new token are left as they are."""
         tokens, heads, dim = q.shape if q.dim() == 3 else (0, 0, 0)
         hq = self._heads(q, "q", _HALF)
         if out is None:
