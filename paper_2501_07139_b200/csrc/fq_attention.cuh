@@ -302,6 +302,7 @@ template <> __device__ __forceinline__ bool finite16<__half>(uint32_t v) { retur
 // back what is in those that it sees.  (Tree bits reach kOddCells new tokens; without them a unit ends, with its last row and key tile, well before
 // that.  Looking through all new cells instead took 10 ms for one infinity among 2000 new tokens of 4 heads, which take 43 us without it.)
 constexpr int kOddWords = 2 * FQ_MAX_TREE_WORDS, kOddCells = 32 * kOddWords;
+static_assert(kOddWords == 32, "a word a lane clears them");
 
 // Zeros in place of infinities and NaNs; true if there were any.
 template <class T>
